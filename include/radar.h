@@ -513,6 +513,133 @@ radar_status radar_draft_rerank_batch(const int32_t *pool_tokens, const float *p
                                       int32_t *tree_depth, int32_t *tree_pool_idx, int32_t *n_nodes_out,
                                       void *workspace, size_t workspace_bytes, void *stream);
 
+/* --------------------------------------------------------------------------
+ * Paged key/value cache in 4 bits: the memory that the target's layers keep
+ * their keys and values in, in place of the dense bf16 caches above, for many
+ * sequences and long contexts (a quarter of the bytes and nothing reserved for
+ * rows that are not there).  A verification pass makes, in this order,
+ *   radar_kvq_blocks              room for the batch's trees, and where each row goes
+ *   radar_kvq_append              per layer: the trees' keys and values into the cache
+ *   radar_tree_attention_kvq      per layer: every node over its prefix and ancestors
+ *   radar_kvq_commit              after the walk: the accepted path's rows into place
+ * and radar_kvq_read gives rows back as bf16, e.g. to hand a prefix on.
+ *
+ * Format.  32 consecutive values x of a row of a head share a scale 2^e and are
+ * 4-bit codes (sign; 0, 0.5, 1, 1.5, 2, 3, 4, 6).  With amax the largest |x|, e is
+ * the smallest whole number for which amax < 7 * 2^e, kept within [-126, 125];
+ * x * 2^-e is rounded to the nearest code, ties to the even one, larger ones to
+ * +-6 (only where e was limited to 125).  No value is off by more than 2^e then.
+ * The scale is kept as the byte e + 127.  A block that holds an infinity or NaN
+ * has byte 255 and stands for 32 NaNs.  What codes stand for is exact in bf16
+ * (bytes 253 and 254, which are never written, reach past its largest number).
+ *
+ * Layout.  The cache is n_blocks blocks of block_rows rows per layer, every block
+ * [Hkv] chunks of radar_kvq_block_bytes(block_rows, D) = block_rows * (D + D/16)
+ * bytes.  With R = block_rows a chunk is
+ *     K codes [R][D/2]  V codes [R/8][D/8][8][4]  K scales [R/8][D/32][8]  V scales [R/8][D/32][8]
+ * (V codes: 8 rows next to each other for every 8 values of the head; an even
+ * value is the low half of its byte).  A row's SLOT is block * R + row in block.
+ * Row j of sequence b is row j % R of block block_tables[b][j / R].
+ *
+ * Limits for all of them: D in {64, 128}; block_rows in {16, 32, 64, 128};
+ * n_blocks * block_rows < 2^31; Hkv <= 65535; cache and layer_stride multiples
+ * of 16 bytes.  Block numbers and slots that are out of range are not
+ * dereferenced: such a row is not there. */
+typedef struct radar_kvq_desc {
+    int32_t n_blocks, block_rows, Hkv, D;
+    int32_t layers;          /* radar_kvq_commit and radar_kvq_read: how many layers the call covers */
+    int64_t layer_stride;    /* bytes from one layer's cache to the next; 0 => dense */
+} radar_kvq_desc;
+
+/* Bytes of one KV head's rows of one block; 0 where the limits are not met. */
+size_t radar_kvq_block_bytes(int32_t block_rows, int32_t D);
+
+/* Block tables and slot maps from the sequences' lengths.  Sequence b asks for
+ * w = ceil((ctx_lens[b] + n_new[b]) / block_rows) blocks, none if ctx_lens[b] < 0
+ * (a sequence that has ended), and has owned[b].  First every sequence with
+ * owned[b] > w gives entries [w, owned[b]) of its table back: they are put onto the
+ * free stack free_blocks[0 .. *n_free) in order of b and then of the entry.  Then
+ * sequences that ask for more take theirs off the top of the stack, in order of b
+ * and then of the entry, as long as what all of them up to and including b ask for
+ * is there: granted[b] = 1, owned_out[b] = w.  Where it is not, granted[b] = 0 and
+ * the sequence keeps what it has (so do all later ones that ask for more); a
+ * sequence that asks for more than max_blocks is refused without counting.
+ * slots[b,i] is the slot of row ctx_lens[b] + i for i < n_new[b] (clamped to
+ * [0, T_max]), -1 for other i and for sequences that were not granted.
+ * block_tables i32 [B,max_blocks] and free_blocks i32 [n_blocks] are updated in
+ * place; entries behind the owned ones and the stack's height are left as they
+ * were.  owned_out and n_free_out may be owned and n_free, or other arrays: as
+ * long as they are, the call may be repeated with the same result.
+ * ctx_lens, owned, granted, owned_out i32 [B]; n_new i32 [B] or NULL (= T_max);
+ * n_free, n_free_out i32 [1]; slots i32 [B,T_max].  No workspace; one kernel, or
+ * two where B * T_max is large. */
+typedef struct radar_kvq_blocks_desc {
+    int32_t B, T_max, max_blocks, n_blocks, block_rows;
+} radar_kvq_blocks_desc;
+
+radar_status radar_kvq_blocks(const int32_t *ctx_lens, const int32_t *n_new, int32_t *block_tables,
+                              const int32_t *owned, int32_t *free_blocks, const int32_t *n_free,
+                              int32_t *owned_out, int32_t *n_free_out, int32_t *slots, int32_t *granted,
+                              const radar_kvq_blocks_desc *desc, void *stream);
+
+/* N rows of keys and values into one layer's cache, row n at slots[n] (rows whose
+ * slot is out of range are dropped; of two rows with the same slot either may
+ * leave any of its parts there).  k, v bf16 [N,Hkv,D], D contiguous, strides in
+ * elements, the same for both, 0 => dense, rows 16-byte aligned; slots i32 [N];
+ * cache: the layer's first block.  N >= 0.  One kernel. */
+radar_status radar_kvq_append(const void *k, const void *v, const int32_t *slots, void *cache, int64_t N,
+                              int64_t stride_n, int64_t stride_h, const radar_kvq_desc *desc, void *stream);
+
+/* The rows at slots[N] of desc->layers layers as the values they stand for; rows
+ * that are not there as zeros.  k, v bf16 [layers,N,Hkv,D], dense.  One kernel. */
+radar_status radar_kvq_read(const void *cache, const int32_t *slots, void *k, void *v, int64_t N,
+                            const radar_kvq_desc *desc, void *stream);
+
+/* After radar_verify_accept: in each of desc->layers layers, row ctx_lens[b] + s of
+ * sequence b becomes what row ctx_lens[b] + accept_path[b,s] was, for
+ * 1 <= s <= accept_len[b] (any path: all rows are read before any is written),
+ * codes and scales unchanged; other rows are left as they were.
+ * new_ctx_lens[b] = ctx_lens[b] + accept_len[b] + 1 (the root is kept too), or
+ * ctx_lens[b] if that is negative.  accept_path i32 [B,path_len] as
+ * radar_verify_accept writes it (path_len = D_max + 1); accept_len is clamped to
+ * [0, path_len - 1]; entries outside [0, RADAR_T_MAX) and rows that are not there
+ * are skipped.  new_ctx_lens i32 [B] or NULL; not ctx_lens itself.  Sequences
+ * must not share the blocks that hold their rows from ctx_lens[b] on.
+ * Limits: 1 <= path_len <= RADAR_T_MAX; B <= 65535.  One kernel. */
+radar_status radar_kvq_commit(void *cache, const int32_t *block_tables, int32_t max_blocks, const int32_t *ctx_lens,
+                              const int32_t *accept_len, const int32_t *accept_path, int32_t path_len, int32_t B,
+                              int32_t *new_ctx_lens, const radar_kvq_desc *desc, void *stream);
+
+/* radar_tree_attention over the paged cache in 4 bits: the same formula, with the
+ * values that the codes stand for.  Rows j < ctx_lens[b] and the rows of node i's
+ * ancestors and its own, ctx_lens[b] + a, that are among the first S_max and in
+ * blocks that are there.  A sequence with ctx_lens[b] < 0 is not there: its rows
+ * of out and lse are written as zero, as are rows i >= n_nodes[b].  Where no row is
+ * allowed, out is zero and lse -inf.  A row that is not allowed has no influence,
+ * whatever it holds (NaN blocks included).
+ * T_max = 1 is the form for single tokens; parents == NULL: node i hangs under
+ * node i - 1 (a chain: causal attention of up to RADAR_T_MAX rows).
+ * cache: the layer's first block; block_tables i32 [B,max_blocks]; S_max: the rows
+ * that the call is planned for, at most max_blocks * block_rows (the longest
+ * ctx_lens[b] + T_max where it is known).  Other arguments and limits as for
+ * radar_tree_attention; q and out 16-byte aligned rows. */
+typedef struct radar_kvq_attn_desc {
+    radar_kvq_desc cache;    /* layers and layer_stride are ignored */
+    int32_t B, T_max, Hq, max_blocks, S_max;
+    int32_t rows_per_split;  /* 0 => chosen by the library; else a multiple of 64: the least rows that one
+                                workgroup takes before partial results are merged */
+    int64_t q_stride_b, q_stride_t, q_stride_h;
+    int64_t out_stride_b, out_stride_t, out_stride_h;
+    float   softmax_scale;   /* 0 => 1/sqrt(D); must not be negative */
+} radar_kvq_attn_desc;
+
+size_t radar_tree_attention_kvq_workspace_bytes(const radar_kvq_attn_desc *desc);
+
+radar_status radar_tree_attention_kvq(const void *q, const void *cache, const int32_t *block_tables,
+                                      const int32_t *parents, const int32_t *ctx_lens, const int32_t *n_nodes,
+                                      void *out, float *lse_out, const radar_kvq_attn_desc *desc,
+                                      void *workspace, size_t workspace_bytes, void *stream);
+
 /* Counts, per call, the nodes i < n_nodes[b] whose parent breaks the tree
  * convention; *bad_count_out (device i32) is overwritten.  parents i32
  * [B,T_max]; n_nodes i32 [B] or NULL. */

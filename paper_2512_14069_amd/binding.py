@@ -69,6 +69,24 @@ class AcceptQDesc(ctypes.Structure):
                 ("walk_spin_limit", ctypes.c_int32)]
 
 
+class KvqDesc(ctypes.Structure):
+    _fields_ = [("n_blocks", ctypes.c_int32), ("block_rows", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("layers", ctypes.c_int32), ("layer_stride", ctypes.c_int64)]
+
+
+class KvqBlocksDesc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("T_max", ctypes.c_int32), ("max_blocks", ctypes.c_int32), ("n_blocks", ctypes.c_int32),
+                ("block_rows", ctypes.c_int32)]
+
+
+class KvqAttnDesc(ctypes.Structure):
+    _fields_ = [("cache", KvqDesc), ("B", ctypes.c_int32), ("T_max", ctypes.c_int32), ("Hq", ctypes.c_int32), ("max_blocks", ctypes.c_int32),
+                ("S_max", ctypes.c_int32), ("rows_per_split", ctypes.c_int32),
+                ("q_stride_b", ctypes.c_int64), ("q_stride_t", ctypes.c_int64), ("q_stride_h", ctypes.c_int64),
+                ("out_stride_b", ctypes.c_int64), ("out_stride_t", ctypes.c_int64), ("out_stride_h", ctypes.c_int64),
+                ("softmax_scale", ctypes.c_float)]
+
+
 class PolicyParams(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("w_ih", "w_hh", "b_ih", "b_hh", "w1", "b1", "w2", "b2")] + \
                [("k", ctypes.c_int32), ("H", ctypes.c_int32), ("M", ctypes.c_int32)]
@@ -88,6 +106,8 @@ EXPORTS = [
     "radar_verify_accept_workspace_bytes", "radar_verify_accept",
     "radar_accept_length_distribution", "radar_policy_step",
     "radar_verify_accept_q_workspace_bytes", "radar_verify_accept_q",
+    "radar_kvq_block_bytes", "radar_kvq_blocks", "radar_kvq_append", "radar_kvq_read", "radar_kvq_commit",
+    "radar_tree_attention_kvq_workspace_bytes", "radar_tree_attention_kvq",
     "radar_debug_validate_tree", "radar_profile_begin", "radar_profile_end", "radar_probe_hbm_read",
 ]
 
@@ -148,6 +168,21 @@ def load():
     lib.radar_verify_accept_q_workspace_bytes.argtypes = [ctypes.POINTER(AcceptQDesc)]
     lib.radar_verify_accept_q.restype = i32
     lib.radar_verify_accept_q.argtypes = [vp] * 10 + [ctypes.POINTER(AcceptQDesc), vp, sz, vp]
+    i64 = ctypes.c_int64
+    lib.radar_kvq_block_bytes.restype = sz
+    lib.radar_kvq_block_bytes.argtypes = [i32, i32]
+    lib.radar_kvq_blocks.restype = i32
+    lib.radar_kvq_blocks.argtypes = [vp] * 10 + [ctypes.POINTER(KvqBlocksDesc), vp]
+    lib.radar_kvq_append.restype = i32
+    lib.radar_kvq_append.argtypes = [vp] * 4 + [i64, i64, i64, ctypes.POINTER(KvqDesc), vp]
+    lib.radar_kvq_read.restype = i32
+    lib.radar_kvq_read.argtypes = [vp] * 4 + [i64, ctypes.POINTER(KvqDesc), vp]
+    lib.radar_kvq_commit.restype = i32
+    lib.radar_kvq_commit.argtypes = [vp, vp, i32, vp, vp, vp, i32, i32, vp, ctypes.POINTER(KvqDesc), vp]
+    lib.radar_tree_attention_kvq_workspace_bytes.restype = sz
+    lib.radar_tree_attention_kvq_workspace_bytes.argtypes = [ctypes.POINTER(KvqAttnDesc)]
+    lib.radar_tree_attention_kvq.restype = i32
+    lib.radar_tree_attention_kvq.argtypes = [vp] * 8 + [ctypes.POINTER(KvqAttnDesc), vp, sz, vp]
     lib.radar_policy_step.restype = i32
     lib.radar_policy_step.argtypes = [vp] * 3 + [ctypes.POINTER(PolicyParams)] + [vp] * 6 + [i32, vp]
     lib.radar_debug_validate_tree.restype = i32
@@ -651,6 +686,216 @@ def radar_draft_rerank_batch(pool, N, root_tokens, states=None, pool_count_max=N
         wp, wn, _stream())
     return _finish("radar_draft_rerank_batch", load().radar_draft_rerank_batch, args, (pool, states, root_tokens, out, workspace),
                    out, prepared)
+
+
+# ------------------------------------------------------------ paged cache in 4 bits
+
+def radar_kvq_block_bytes(block_rows, D):
+    return int(load().radar_kvq_block_bytes(int(block_rows), int(D)))
+
+
+class KvqCache:
+    """Caller-owned cache of one or more layers: data uint8 [layers, n_blocks, Hkv, radar_kvq_block_bytes(block_rows, D)].
+    data: an existing tensor of that shape (a layer's blocks packed, layers at any stride of 16 bytes)."""
+
+    def __init__(self, n_blocks=None, block_rows=16, Hkv=None, D=128, layers=1, device="cuda", data=None):
+        chunk = radar_kvq_block_bytes(block_rows, D)
+        if chunk == 0:
+            raise ValueError(f"block_rows {block_rows}, D {D}: not a shape of the cache")
+        if data is None:
+            data = torch.zeros((layers, n_blocks, Hkv, chunk), dtype=torch.uint8, device=device)
+        if data.dim() != 4 or data.dtype != torch.uint8 or data.shape[3] != chunk or not data[0].is_contiguous():
+            raise ValueError(f"data: expected uint8 [layers, n_blocks, Hkv, {chunk}], each layer contiguous")
+        self.data, self.block_rows, self.D = data, int(block_rows), int(D)
+        self.layers, self.n_blocks, self.Hkv = (int(n) for n in data.shape[:3])
+
+    def desc(self):
+        d = KvqDesc()
+        d.n_blocks, d.block_rows, d.Hkv, d.D, d.layers = self.n_blocks, self.block_rows, self.Hkv, self.D, self.layers
+        d.layer_stride = self.data.stride(0) if self.layers > 1 else 0
+        return d
+
+
+class KvqTables:
+    """Caller-owned block tables of B sequences and the stack of free blocks: block_tables i32 [B, max_blocks], owned i32 [B],
+    free_blocks i32 [n_blocks], n_free i32 [1].  Made new, every block of the cache is free."""
+
+    def __init__(self, B=None, max_blocks=None, n_blocks=None, block_rows=16, device="cuda", block_tables=None, owned=None, free_blocks=None,
+                 n_free=None):
+        i32 = dict(dtype=torch.int32, device=device)
+        self.block_tables = torch.full((B, max_blocks), -1, **i32) if block_tables is None else block_tables
+        self.owned = torch.zeros(self.block_tables.shape[0], **i32) if owned is None else owned
+        self.free_blocks = torch.arange(n_blocks - 1, -1, -1, **i32) if free_blocks is None else free_blocks
+        self.n_free = torch.full((1,), self.free_blocks.numel(), **i32) if n_free is None else n_free
+        self.block_rows = int(block_rows)
+
+
+def _here(*tensors):
+    """All of the tensors on the current device, whose stream the call goes to."""
+    for t in tensors:
+        if t is not None and t.is_cuda and t.device.index != torch.cuda.current_device():
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _sized(t, shape, name):
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t
+
+
+def _i32p(t, name):
+    return _ptr(None if t is None else _dense(t, name), torch.int32, name)
+
+
+def radar_kvq_blocks(ctx_lens, tables, T, n_new=None, slots=None, granted=None, owned_out=None, n_free_out=None, prepared=False):
+    """Room for T (n_new i32 [B]: so many) new rows of every sequence behind its ctx_lens i32 [B] rows (negative: it has ended) in
+    `tables` (KvqTables, updated; owned and n_free too unless owned_out and n_free_out are given).
+    Returns (slots i32 [B,T], granted i32 [B])."""
+    B, M = tables.block_tables.shape
+    dev = ctx_lens.device
+    for t, shape, name in ((ctx_lens, (B,), "ctx_lens"), (n_new, (B,), "n_new"), (tables.owned, (B,), "owned"), (owned_out, (B,), "owned_out"),
+                           (tables.n_free, (1,), "n_free"), (n_free_out, (1,), "n_free_out"), (slots, (B, T), "slots"), (granted, (B,), "granted")):
+        _sized(t, shape, name)
+    if tables.free_blocks.dim() != 1:
+        raise ValueError("free_blocks: expected one dimension")
+    ptrs = [_i32p(t, n) for t, n in ((ctx_lens, "ctx_lens"), (n_new, "n_new"), (tables.block_tables, "block_tables"), (tables.owned, "owned"),
+                                     (tables.free_blocks, "free_blocks"), (tables.n_free, "n_free"))]
+    _here(ctx_lens, n_new, tables.block_tables, tables.owned, tables.free_blocks, tables.n_free, owned_out, n_free_out, slots, granted)
+    slots = torch.empty((B, T), dtype=torch.int32, device=dev) if slots is None else slots
+    granted = torch.empty((B,), dtype=torch.int32, device=dev) if granted is None else granted
+    owned_out = tables.owned if owned_out is None else owned_out
+    n_free_out = tables.n_free if n_free_out is None else n_free_out
+    d = KvqBlocksDesc()
+    d.B, d.T_max, d.max_blocks, d.n_blocks, d.block_rows = B, int(T), M, tables.free_blocks.numel(), tables.block_rows
+    args = (*ptrs, _i32p(owned_out, "owned_out"), _i32p(n_free_out, "n_free_out"), _i32p(slots, "slots"), _i32p(granted, "granted"),
+            ctypes.byref(d), _stream())
+    keep = (ctx_lens, n_new, tables, owned_out, n_free_out, slots, granted, d, tables.block_tables, tables.owned, tables.free_blocks, tables.n_free)
+    return _finish("radar_kvq_blocks", load().radar_kvq_blocks, args, keep, (slots, granted), prepared)
+
+
+def _rows_stride(t, name):
+    """Elements from row to row of [..., Hkv, D] whose leading dimensions are one long row axis."""
+    step = None
+    for size, stride in zip(reversed(t.shape[:-2]), reversed(t.stride()[:-2])):
+        if size == 1:
+            continue
+        if step is None:
+            first, step = stride, stride * size
+        elif stride != step:
+            raise ValueError(f"{name}: its rows are not evenly spaced")
+        else:
+            step *= size
+    return 0 if step is None else first
+
+
+def _layer(cache, layer):
+    if not 0 <= layer < cache.layers:
+        raise ValueError(f"layer {layer} of {cache.layers}")
+    return cache.data[layer]
+
+
+def radar_kvq_append(cache, k, v, slots, layer=0, prepared=False):
+    """k, v bf16 [..., Hkv, D] (one row axis of any number of dimensions, evenly spaced: a slice of a projection's output will do; the same
+    strides for both, D contiguous); slots i32, as many as rows.  Writes the rows into `layer` of the KvqCache; returns it."""
+    if tuple(k.shape) != tuple(v.shape) or tuple(k.shape[-2:]) != (cache.Hkv, cache.D) or k.dim() < 3:
+        raise ValueError(f"k, v: expected [..., {cache.Hkv}, {cache.D}], got {tuple(k.shape)} and {tuple(v.shape)}")
+    N = k.numel() // (cache.Hkv * cache.D)
+    if slots.numel() != N:
+        raise ValueError(f"slots: expected {N}, got {slots.numel()}")
+    if k.stride() != v.stride() or k.stride(-1) != 1:
+        raise ValueError("innermost axis must be contiguous and k and v must share strides")
+    data = _layer(cache, layer)
+    _here(k, v, slots, data)
+    d = cache.desc()
+    step, head = _rows_stride(k, "k"), k.stride(-2)
+    if (N > 1 and step == 0) or (cache.Hkv > 1 and head == 0):
+        raise ValueError("k, v: broadcast rows or heads; make them contiguous")
+    args = (_ptr(k, torch.bfloat16, "k"), _ptr(v, torch.bfloat16, "v"), _i32p(slots, "slots"), _ptr(data, torch.uint8, "cache"), N,
+            step, head if cache.Hkv > 1 else 0, ctypes.byref(d), _stream())
+    if N == 0:
+        args = (ctypes.c_void_p(data.data_ptr()), ctypes.c_void_p(data.data_ptr()), ctypes.c_void_p(data.data_ptr())) + args[3:]
+    return _finish("radar_kvq_append", load().radar_kvq_append, args, (cache, k, v, slots, data, d), cache, prepared)
+
+
+def radar_kvq_read(cache, slots, k=None, v=None, layer=None, prepared=False):
+    """The rows at `slots` (i32, any shape, N of them) of every layer, or of one, as (k, v) bf16 [layers, N, Hkv, D]; zeros for
+    slots out of range."""
+    N = slots.numel()
+    data = cache.data if layer is None else _layer(cache, layer)[None]
+    shape = (data.shape[0], N, cache.Hkv, cache.D)
+    k = torch.empty(shape, dtype=torch.bfloat16, device=slots.device) if k is None else _sized(k, shape, "k")
+    v = torch.empty(shape, dtype=torch.bfloat16, device=slots.device) if v is None else _sized(v, shape, "v")
+    _here(slots, k, v, data)
+    d = cache.desc()
+    d.layers = data.shape[0]
+    args = (_ptr(data, torch.uint8, "cache"), _i32p(slots, "slots"), _ptr(_dense(k, "k"), torch.bfloat16, "k"),
+            _ptr(_dense(v, "v"), torch.bfloat16, "v"), N, ctypes.byref(d), _stream())
+    if N == 0:
+        args = args[:1] + (ctypes.c_void_p(data.data_ptr()),) * 3 + args[4:]
+    return _finish("radar_kvq_read", load().radar_kvq_read, args, (cache, slots, k, v, data, d), (k, v), prepared)
+
+
+def radar_kvq_commit(cache, block_tables, ctx_lens, accept_len, accept_path, new_ctx_lens=None, prepared=False):
+    """The accepted path's rows of every layer into place: accept_len i32 [B], accept_path i32 [B, D_max+1] as radar_verify_accept
+    gives them; block_tables i32 [B,M], ctx_lens i32 [B].  Returns new_ctx_lens i32 [B] (not ctx_lens itself)."""
+    B, M = block_tables.shape
+    _sized(ctx_lens, (B,), "ctx_lens"), _sized(accept_len, (B,), "accept_len"), _sized(new_ctx_lens, (B,), "new_ctx_lens")
+    if accept_path.dim() != 2 or accept_path.shape[0] != B:
+        raise ValueError(f"accept_path: expected [{B}, D_max+1], got {tuple(accept_path.shape)}")
+    new_ctx_lens = torch.empty_like(ctx_lens) if new_ctx_lens is None else new_ctx_lens
+    _here(cache.data, block_tables, ctx_lens, accept_len, accept_path, new_ctx_lens)
+    d = cache.desc()
+    args = (_ptr(cache.data, torch.uint8, "cache"), _i32p(block_tables, "block_tables"), M, _i32p(ctx_lens, "ctx_lens"),
+            _i32p(accept_len, "accept_len"), _i32p(accept_path, "accept_path"), accept_path.shape[1], B, _i32p(new_ctx_lens, "new_ctx_lens"),
+            ctypes.byref(d), _stream())
+    keep = (cache, cache.data, block_tables, ctx_lens, accept_len, accept_path, new_ctx_lens, d)
+    return _finish("radar_kvq_commit", load().radar_kvq_commit, args, keep, new_ctx_lens, prepared)
+
+
+def kvq_attn_desc(q, cache, max_blocks, S_max=None, out=None, rows_per_split=0, softmax_scale=0.0):
+    d = KvqAttnDesc()
+    d.cache = cache.desc()
+    d.B, d.T_max, d.Hq, _ = q.shape
+    d.max_blocks = int(max_blocks)
+    d.S_max = d.max_blocks * cache.block_rows if S_max is None else int(S_max)
+    d.rows_per_split, d.softmax_scale = int(rows_per_split), float(softmax_scale)
+    d.q_stride_b, d.q_stride_t, d.q_stride_h = q.stride()[:3]
+    if out is not None:
+        d.out_stride_b, d.out_stride_t, d.out_stride_h = out.stride()[:3]
+    return d
+
+
+def radar_tree_attention_kvq_workspace_bytes(desc):
+    return int(load().radar_tree_attention_kvq_workspace_bytes(ctypes.byref(desc)))
+
+
+def radar_tree_attention_kvq(q, cache, block_tables, ctx_lens, parents=None, n_nodes=None, layer=0, S_max=None, out=None, lse_out=None,
+                             workspace=None, rows_per_split=0, softmax_scale=0.0, prepared=False):
+    """radar_tree_attention over `layer` of a KvqCache: q bf16 [B,T,Hq,D]; block_tables i32 [B,M]; ctx_lens i32 [B]; parents i32 [B,T]
+    or None (a chain); n_nodes i32 [B] or None; S_max: the rows in use (the longest ctx_lens + T), default all that the tables
+    hold.  Returns out bf16 [B,T,Hq,D]."""
+    if q.dim() != 4 or q.shape[3] != cache.D or q.stride(3) != 1:
+        raise ValueError(f"q: expected [B, T, Hq, {cache.D}], the innermost axis contiguous")
+    B, T, Hq, _ = q.shape
+    M = _sized(block_tables, (B, block_tables.shape[-1]), "block_tables").shape[1]
+    for t, shape, name in ((ctx_lens, (B,), "ctx_lens"), (n_nodes, (B,), "n_nodes"), (parents, (B, T), "parents"), (out, q.shape, "out"),
+                           (lse_out, (B, T, Hq), "lse_out")):
+        _sized(t, shape, name)
+    if out is None:
+        out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+    if out.stride(3) != 1:
+        raise ValueError("out: the innermost axis must be contiguous")
+    data = _layer(cache, layer)
+    _here(q, data, block_tables, ctx_lens, parents, n_nodes, out, lse_out, workspace)
+    desc = kvq_attn_desc(q, cache, M, S_max, out, rows_per_split, softmax_scale)
+    if workspace is None:
+        workspace = new_workspace(radar_tree_attention_kvq_workspace_bytes(desc), q.device)
+    wp, wn = _ws_args(workspace)
+    args = (_ptr(q, torch.bfloat16, "q"), _ptr(data, torch.uint8, "cache"), _i32p(block_tables, "block_tables"), _i32p(parents, "parents"),
+            _i32p(ctx_lens, "ctx_lens"), _i32p(n_nodes, "n_nodes"), _ptr(out, torch.bfloat16, "out"),
+            _ptr(None if lse_out is None else _dense(lse_out, "lse_out"), torch.float32, "lse_out"), ctypes.byref(desc), wp, wn, _stream())
+    keep = (q, cache, data, block_tables, parents, ctx_lens, n_nodes, out, lse_out, desc, workspace)
+    return _finish("radar_tree_attention_kvq", load().radar_tree_attention_kvq, args, keep, out, prepared)
 
 
 # ------------------------------------------------------------ verification
