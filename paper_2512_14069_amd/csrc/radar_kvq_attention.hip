@@ -16,6 +16,7 @@
 namespace radar {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
@@ -32,6 +33,10 @@ struct KqArgs {
     int B, T, Hq, Hkv, G, M, S, rbits, n_blocks;
     int64_t q_sb, q_st, q_sh, o_sb, o_st, o_sh;
     float scale_log2;
+    int64_t block_bytes;                       // of a block, all heads
+    int workgroups, least, shift, max_cgs;     // least share of the line; log2 steps per unit of it; column blocks of a KV head
+    float *part;                               // [2 * workgroups] partial results: outputs, maxima (log2 units), sums, in fp32
+    uint32_t *unit_tab;                        // first and last workgroup of a unit; alike: it is written already
 };
 
 // A sequence: rows of its prefix, nodes of its tree, rows that may be attended to.  There is none: nn = 0.
@@ -61,6 +66,13 @@ __device__ __forceinline__ uint64_t kq_ancestors(const int32_t *parents, int nn)
     return (uint64_t)hi << 32 | lo;
 }
 
+typedef const __attribute__((address_space(1))) unsigned char *kq_bytes;      // global memory
+__device__ __forceinline__ uint64_t kq_scalar(const void *p) {
+    const uint64_t v = (uint64_t)(uintptr_t)p;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v), hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+    return (uint64_t)hi << 32 | lo;
+}
+
 // The larger (the sum) over the four lanes that share a column: lane ^ 16, lane ^ 32.
 __device__ __forceinline__ float kq_column_max(float v) {
     uint32_t u = __float_as_uint(v);
@@ -79,211 +91,550 @@ __device__ __forceinline__ float kq_column_sum(float v) {
     return __uint_as_float(t[0]) + __uint_as_float(t[1]);
 }
 
-// What a lane loads for a step of 32 keys: two keys' codes and scales of K (tile t: key 8 * (r/4) + 4t + r%4, r = lane % 16), eight keys' of V.
+// Four outputs of a row, from their weighted sum, the reference and the weights' sum; with the first four the row's log-sum-exp.
+__device__ __forceinline__ void kq_write(const KqArgs &a, int b, int i, int h, int d, floatx4 acc, float M, float l) {
+    const float inv = l == 0.f ? 0.f : 1.0f / l;                     // (no key seen)
+    bf16x4 o;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = (__bf16)(acc[e] * inv);
+    *reinterpret_cast<bf16x4 *>(a.out + (size_t)b * a.o_sb + (size_t)i * a.o_st + (size_t)h * a.o_sh + d) = o;
+    if (a.lse && d == 0) a.lse[((size_t)b * a.T + i) * a.Hq + h] = l == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(l)) * kqLn2;
+}
+
+// What a lane holds for a step of 32 keys: two keys' codes and scales of K (tile t: key 8 * (r/4) + 4t + r%4, r = lane % 16), eight keys' of V
+// (8 * (lane / 16) + e).
 template <int D>
-struct KqStep {
-    uint32_t k[2][D / 32];
-    uint32_t ks[2];
-    uint32_t v[8];
-    u32x2 vs;
-    uint32_t there;                            // bit e: key 8 * (lane / 16) + e is there
-};
+struct KqK { uint32_t code[2][D / 32]; u32x2 scale; };     // (scales of the eight rows that the lane's two are among: word t, byte r % 4)
+struct KqV { uint32_t code[8]; u32x2 scale; };
+
+// The blocks of a step's first and second 16 keys (blocks are 16 rows or more): their numbers, the same in every lane.
+struct KqIds { int a, b; };
+__device__ __forceinline__ KqIds kq_ids(const KqArgs &a, const int32_t *table, int key0, int total) {
+    const int last = total - 1;
+    return KqIds{uniform_word(table, min(key0, last) >> a.rbits), uniform_word(table, min(key0 + 16, last) >> a.rbits)};
+}
+__device__ __forceinline__ bool kq_there(const KqArgs &a, int blk) { return (uint32_t)blk < (uint32_t)a.n_blocks; }
+
+// Where the two halves' codes and scales begin: a row is D/2 bytes of codes further on, K's or V's, and D/32 bytes of scales.  All of it in
+// scalar registers; a lane adds the place of its own rows, worked out once.
+struct KqBase { kq_bytes code_a, code_b, scale_a, scale_b; };
+template <int D>
+__device__ __forceinline__ KqBase kq_base(const KqArgs &a, kq_bytes base, KqIds id, int key0) {
+    const int R = 1 << a.rbits, row_a = key0 & (R - 1), row_b = (key0 + 16) & (R - 1);
+    const kq_bytes ca = base + (uint64_t)(kq_there(a, id.a) ? (uint32_t)id.a : 0u) * (uint64_t)a.block_bytes;
+    const kq_bytes cb = base + (uint64_t)(kq_there(a, id.b) ? (uint32_t)id.b : 0u) * (uint64_t)a.block_bytes;
+    return KqBase{ca + row_a * (D / 2), cb + row_b * (D / 2), ca + R * D + row_a * (D / 32), cb + R * D + row_b * (D / 32)};
+}
+__device__ __forceinline__ kq_bytes kq_half(kq_bytes a, kq_bytes b, bool second) { return second ? b : a; }
+template <typename T>
+__device__ __forceinline__ T kq_read(kq_bytes p) { return *reinterpret_cast<const __attribute__((address_space(1))) T *>(p); }
 
 template <int D>
-__device__ __forceinline__ void kq_load(KqStep<D> &s, const KqArgs &a, const int32_t *table, int hk, int key0, int total) {
+__device__ __forceinline__ void kq_load_k(KqK<D> &k, KqBase s) {
     using C = KvqChunk<D>;
-    const int lane = lane_id(), r = lane & 15, grp = lane >> 4, R = 1 << a.rbits;
-    auto chunk_of = [&](int key, bool *there) {
-        const int blk = table[min(key, total - 1) >> a.rbits];
-        *there = key < total && (uint32_t)blk < (uint32_t)a.n_blocks;
-        return a.cache + ((size_t)((uint32_t)blk < (uint32_t)a.n_blocks ? blk : 0) * a.Hkv + hk) * C::bytes(R);
-    };
+    const int lane = lane_id(), r = lane & 15, grp = lane >> 4, group = (r >> 2) & 1, blk = D == 128 ? grp : grp >> 1;
+    const kq_bytes w = kq_half(s.code_a, s.code_b, r >= 8) + (uint32_t)(C::k_row(8 * group + (r & 3)) + (D / 8) * grp);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-        const int key = key0 + 8 * (r >> 2) + 4 * t + (r & 3), row = key & (R - 1);
-        bool there;
-        const unsigned char *const c = chunk_of(key, &there);
         if constexpr (D == 128) {
-            const u32x4 w = *reinterpret_cast<const u32x4 *>(c + C::k_row(row) + 16 * grp);
+            const u32x4 x = kq_read<u32x4>(w + t * C::k_row(4));
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s.k[t][i] = w[i];
-            s.ks[t] = c[C::k_scale(R, row, grp)];
+            for (int i = 0; i < 4; ++i) k.code[t][i] = x[i];
         } else {
-            const u32x2 w = *reinterpret_cast<const u32x2 *>(c + C::k_row(row) + 8 * grp);
-            s.k[t][0] = w[0]; s.k[t][1] = w[1];
-            s.ks[t] = c[C::k_scale(R, row, grp >> 1)];
+            const u32x2 x = kq_read<u32x2>(w + t * C::k_row(4));
+            k.code[t][0] = x[0]; k.code[t][1] = x[1];
         }
     }
-    const int key = key0 + 8 * grp, row = key & (R - 1);
-    bool there;
-    const unsigned char *const c = chunk_of(key, &there);
-    const int n = there ? min(total - key, 8) : 0;
-    s.there = (1u << n) - 1;
-    const u32x4 lo = *reinterpret_cast<const u32x4 *>(c + C::v_piece(R, row, D == 128 ? r : r >> 1));
-    const u32x4 hi = *reinterpret_cast<const u32x4 *>(c + C::v_piece(R, row, D == 128 ? r : r >> 1) + 16);
-    s.vs = *reinterpret_cast<const u32x2 *>(c + C::v_scale(R, row, D == 128 ? r >> 2 : r >> 3));
+    k.scale = kq_read<u32x2>(kq_half(s.scale_a, s.scale_b, r >= 8) + (uint32_t)((group * C::kScales + blk) * 8));
+}
+template <int D>
+__device__ __forceinline__ void kq_load_v(KqV &v, const KqArgs &a, KqBase s) {
+    using C = KvqChunk<D>;
+    const int lane = lane_id(), r = lane & 15, grp = lane >> 4, piece = D == 128 ? r : r >> 1, blk = D == 128 ? r >> 2 : r >> 3;
+    const kq_bytes w = kq_half(s.code_a, s.code_b, grp >= 2) + (((D / 2) << a.rbits) + (uint32_t)(((grp & 1) * C::kPieces + piece) * 32));
+    const u32x4 lo = kq_read<u32x4>(w), hi = kq_read<u32x4>(w + 16);
+    v.scale = kq_read<u32x2>(kq_half(s.scale_a, s.scale_b, grp >= 2) + (((D / 32) << a.rbits) + (uint32_t)(((grp & 1) * C::kScales + blk) * 8)));
 #pragma unroll
-    for (int e = 0; e < 4; ++e) { s.v[e] = lo[e]; s.v[4 + e] = hi[e]; }
-    if (n < 8) {                                                     // rows that are not there hold anything: zeros in V (K is masked)
+    for (int e = 0; e < 4; ++e) { v.code[e] = lo[e]; v.code[4 + e] = hi[e]; }
+}
+
+// Of the lane's eight V rows the first n are there; the others hold anything and become zeros (K's scores are masked).
+__device__ __forceinline__ void kq_clear_v(KqV &s, int n) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s.v[e] = e < n ? s.v[e] : 0u;
-        uint64_t both = (uint64_t)s.vs[1] << 32 | s.vs[0];
-        both &= n > 0 ? ~0ull >> (64 - 8 * n) : 0ull;
-        s.vs = u32x2{(uint32_t)both, (uint32_t)(both >> 32)};
-    }
+    for (int e = 0; e < 8; ++e) s.code[e] = e < n ? s.code[e] : 0u;
+    uint64_t both = (uint64_t)s.scale[1] << 32 | s.scale[0];
+    both &= n > 0 ? ~0ull >> (64 - 8 * n) : 0ull;
+    s.scale = u32x2{(uint32_t)both, (uint32_t)(both >> 32)};
 }
 
 // A NaN block of V under a probability of zero would make NaN of queries that may not see it.  Only rows of the tree are hidden from anybody, so
 // in a step that reaches them NaN blocks become zeros, and NaN is put where a query does see one.  A lane's outputs are d = D/4 * (lane / 16) ...,
-// all of one block of 32.  allow: the lane's eight keys that its column sees.  All lanes call.
+// all of one block of 32.  Returns which of the step's 32 keys have a NaN in that block; all lanes call.
 template <int D>
-__device__ __forceinline__ bool kq_hide_nan(KqStep<D> &s, uint32_t allow) {
-    const int lane = lane_id(), grp = lane >> 4;
+__device__ __forceinline__ uint32_t kq_hide_nan(KqV &s, int grp) {
     uint32_t bad = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-        if (((s.vs[e >> 2] >> (8 * (e & 3))) & 255u) == kScaleNaN) {
+        if (((s.scale[e >> 2] >> (8 * (e & 3))) & 255u) == kScaleNaN) {
             bad |= 1u << e;
-            s.v[e] = 0;
-            s.vs[e >> 2] &= ~(255u << (8 * (e & 3)));
+            s.code[e] = 0;
+            s.scale[e >> 2] &= ~(255u << (8 * (e & 3)));
         }
-    if (__ballot(bad != 0) == 0ull) return false;
+    if (__ballot(bad != 0) == 0ull) return 0;
     const int holder = D == 128 ? 4 * grp : 8 * (grp >> 1);           // a lane that has the scales of this lane's outputs
-    bool seen = false;
-    for (int g = 0; g < 4; ++g) {
-        const uint32_t b = (uint32_t)__shfl((int)bad, 16 * g + holder), see = (uint32_t)__shfl((int)allow, 16 * g + (lane & 15));
-        seen |= (b & see) != 0;
-    }
-    return seen;
+    uint32_t all = 0;
+    for (int g = 0; g < 4; ++g) all |= (uint32_t)__shfl((int)bad, 16 * g + holder) << (8 * g);
+    return all;
 }
 
-// One wavefront: 32 keys against 16 query columns.
-template <int D>
-__device__ __forceinline__ void kq_step(KqStep<D> &s, const bf16x8 (&qop)[D / 32], floatx4 (&oacc)[D / 16], float &m_run, float &l_run,
-                                        uint64_t anc, int key0, int L, float scale_log2) {
-    const int lane = lane_id(), r = lane & 15, grp = lane >> 4;
-    floatx4 sacc[2];
+// Which of the step's 32 keys a column sees.  first: the step's first key, counted from the tree's first row.
+__device__ __forceinline__ uint32_t kq_allowed(uint64_t anc, int first) {
+    if (first >= 64) return 0;
+    if (first >= 0) return (uint32_t)(anc >> first);
+    if (first <= -32) return ~0u;
+    return (uint32_t)(anc << -first) | ((1u << -first) - 1);
+}
+// ===================================================================== one workgroup
+// A workgroup takes one KV head's rows, or a range of them, for 16 * NC query columns; its eight wavefronts take the steps of 32 keys in turn and
+// meet in LDS at the end.  Nobody waits for anybody before that: there is no tile to share.  What a wavefront spends on turning codes into
+// operands (about 115 vector instructions a step) is shared by its columns only, hence as many as registers allow: with 64 columns the outputs
+// take 128 registers, and the queries' operands stay in LDS.
+constexpr int kKqWaves = 8, kKqThreads = kKqWaves * kWave;
+constexpr float kKqSlack = 8.0f;               // how far a column's maximum may pass its reference (log2 units) before sums are rescaled
+constexpr float kKqNone = 3.0e38f;             // negated reference of a column that has seen no key yet
+
+template <int D, int NC>
+struct KqShape {
+    static constexpr int NM = D / 16, CH = D / 32, COLS = 16 * NC;   // output tiles; steps of the scores' product; columns
+    static constexpr int EP = 4 / NC, DP = D / NC;                   // the merge goes over the outputs in NC passes: registers, values of a pass
+    static constexpr int ROW = DP + 4;                               // of the merge's buffer: rows 16 bytes apart from a multiple of the banks
+    static constexpr int q_bytes() { return COLS * D * 2; }
+    static constexpr int merge_bytes() { return kKqWaves * COLS * ROW * 4; }
+    static constexpr int lds_bytes() { return merge_bytes() + (kKqWaves + 1) * COLS * 8 + (NC > 2 ? q_bytes() : 0); }
+    static constexpr int PART = COLS * D + 2 * COLS;                 // floats of a partial result: outputs, maxima, sums
+};
+
+// One wavefront, one step: scores of 32 keys, softmax against the running reference, outputs.  The loads of the wavefront's next step are
+// asked for as soon as the registers of this one's are free: K's after the scores, V's at the end.
+template <int D, int NC, typename QOp, typename NextK>
+__device__ __forceinline__ void kq_step(const KqK<D> &k, KqV &v, KqIds id, QOp qop, NextK next_k, floatx4 (&oacc)[D / 16][NC], float (&negref)[NC],
+                                        float (&l_run)[NC], const uint64_t *s_anc, const KqArgs &a, int key0, int L, int total) {
+    using S = KqShape<D, NC>;
+    const int lane = lane_id(), r = lane & 15;
+    floatx4 sacc[2][NC];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        sacc[t] = floatx4{0.f, 0.f, 0.f, 0.f};
-        const float f = kvq_scale(s.ks[t]);
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int c = 0; c < D / 32; ++c) {
-            uint32_t w[4];
-            kvq_decode8(s.k[t][c], f, w);
-            sacc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]}), qop[c], sacc[t], 0, 0, 0);
+        for (int n = 0; n < NC; ++n) sacc[t][n] = floatx4{0.f, 0.f, 0.f, 0.f};
+    const uint32_t pick = 0x0c0c0cu | (uint32_t)(r & 3) << 24;       // that byte on top, zeros under it
+    const float f[2] = {__uint_as_float(__builtin_amdgcn_perm(0u, k.scale[0], pick) >> 1), __uint_as_float(__builtin_amdgcn_perm(0u, k.scale[1], pick) >> 1)};
+    // (the queries' operands come from LDS where there are many: asked for two column blocks ahead)
+    constexpr int NQ = NC * S::CH, AHEAD = NC > 2 ? 2 : NQ;
+    bf16x8 q[AHEAD];
+#pragma unroll
+    for (int x = 0; x < AHEAD; ++x) q[x] = qop(x % NC, x / NC);
+#pragma unroll
+    for (int c = 0; c < S::CH; ++c) {
+        uint32_t w[2][4];
+        kvq_decode8(k.code[0][c], f[0], w[0]);
+        kvq_decode8(k.code[1][c], f[1], w[1]);
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+            const int x = c * NC + n;
+            const bf16x8 cur = q[x % AHEAD];
+            if (x + AHEAD < NQ) q[x % AHEAD] = qop((x + AHEAD) % NC, (x + AHEAD) / NC);
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+                sacc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{w[t][0], w[t][1], w[t][2], w[t][3]}), cur, sacc[t][n], 0, 0, 0);
+            if (NC > 2) __builtin_amdgcn_sched_barrier(0);
         }
     }
+    __builtin_amdgcn_sched_barrier(0);         // (the phases stay apart: run into each other they need twice the registers)
+    next_k();
     // this lane's eight keys: 8 * grp + e, e = 4 * tile + register
-    uint32_t allow = s.there;
-    const int first = key0 + 8 * grp - L;                            // the first of them, counted from the tree's first row
-    if (first + 8 > 0) {
-        const uint32_t tree = first >= 64 ? 0u : (uint32_t)(first >= 0 ? anc >> first : anc << -first);
-        allow &= first >= 0 ? tree : tree | ((1u << -first) - 1);
-    }
-    float x[8], mx = -INFINITY;
+    uint32_t nan_keys = 0;
+    const bool whole = key0 + 32 <= L && kq_there(a, id.a) && kq_there(a, id.b);      // all of it prefix: nothing to mask
+    if (!whole) {
+        int lane2 = lane;
+        asm volatile("" : "+v"(lane2));                              // (what only this needs is worked out here, and not kept in registers)
+        const int r = lane2 & 15, grp = lane2 >> 4;
+        const int n_there = kq_there(a, grp < 2 ? id.a : id.b) ? min(max(total - (key0 + 8 * grp), 0), 8) : 0;
+        kq_clear_v(v, n_there);
+        nan_keys = kq_hide_nan<D>(v, grp);
+        const uint32_t there = (1u << n_there) - 1;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        x[e] = (allow >> e) & 1u ? sacc[e >> 2][e & 3] * scale_log2 : -INFINITY;
-        mx = fmaxf(mx, x[e]);
-    }
-    mx = kq_column_max(mx);
-    const float m_new = fmaxf(m_run, mx), ref = m_new == -INFINITY ? 0.f : m_new;
-    const float alpha = __builtin_amdgcn_exp2f(m_run - ref);         // nothing yet: 0
-    m_run = m_new;
-    l_run *= alpha;
+        for (int n = 0; n < NC; ++n) {
+            const uint32_t mine = (kq_allowed(s_anc[n * 16 + r], key0 - L) >> (8 * grp)) & there;
 #pragma unroll
-    for (int m = 0; m < D / 16; ++m) oacc[m] *= alpha;
-    bf16x8 p;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float w = __builtin_amdgcn_exp2f(x[e] - ref);
-        l_run += w;
-        p[e] = (__bf16)w;
-    }
-    const bool nan = key0 + 32 > L && kq_hide_nan<D>(s, allow);
-    // V^T operands: product m of lane (r, grp) is d = D/16 * r + m, keys 8 * grp + 0..7
-    constexpr int NM = D / 16;
-    uint32_t vop[NM][4];
-#pragma unroll
-    for (int e = 0; e < 8; e += 2) {
-        const float f0 = kvq_scale((s.vs[e >> 2] >> (8 * (e & 3))) & 255u), f1 = kvq_scale((s.vs[(e + 1) >> 2] >> (8 * ((e + 1) & 3))) & 255u);
-        const uint32_t w0 = D == 128 ? s.v[e] : s.v[e] >> (16 * (r & 1)), w1 = D == 128 ? s.v[e + 1] : s.v[e + 1] >> (16 * (r & 1));
-        uint32_t a[4], b[4];
-        kvq_decode8(w0, f0, a);
-        kvq_decode8(w1, f1, b);
-#pragma unroll
-        for (int j = 0; j < NM / 2; ++j) {
-            vop[2 * j][e >> 1] = __builtin_amdgcn_perm(b[j], a[j], 0x05040100u);
-            vop[2 * j + 1][e >> 1] = __builtin_amdgcn_perm(b[j], a[j], 0x07060302u);
+            for (int e = 0; e < 8; ++e) sacc[e >> 2][n][e & 3] = (mine >> e) & 1u ? sacc[e >> 2][n][e & 3] : -INFINITY;
         }
     }
+    bf16x8 p[NC];
 #pragma unroll
-    for (int m = 0; m < NM; ++m)
-        oacc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{vop[m][0], vop[m][1], vop[m][2], vop[m][3]}), p, oacc[m], 0, 0, 0);
-    if (key0 + 32 > L)
+    for (int n = 0; n < NC; ++n) {
+        float mx = sacc[0][n][0];
 #pragma unroll
-        for (int m = 0; m < NM; ++m) oacc[m] = nan ? floatx4{NAN, NAN, NAN, NAN} : oacc[m];
+        for (int e = 1; e < 8; ++e) mx = fmaxf(mx, sacc[e >> 2][n][e & 3]);
+        // The reference follows the maximum only when that has risen by more than 8: then, and only then, do the four lanes of a column compare
+        // theirs and the sums get rescaled.  (A probability may be as large as 2^8 instead of 1: it keeps its eight bits.)
+        if (__any(__builtin_fmaf(mx, a.scale_log2, negref[n]) > kKqSlack)) {
+            const float neg = fminf(negref[n], -(kq_column_max(mx) * a.scale_log2)), alpha = __builtin_amdgcn_exp2f(neg - negref[n]);
+            negref[n] = neg;
+            l_run[n] *= alpha;
+#pragma unroll
+            for (int m = 0; m < S::NM; ++m) oacc[m][n] *= alpha;
+        }
+        float sum = l_run[n];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[e >> 2][n][e & 3], a.scale_log2, negref[n]));
+            sum += w;
+            p[n][e] = (__bf16)w;                                     // the matrix cores' operand; the sum is of the unrounded ones, in fp32
+        }
+        asm volatile("" : "+v"(sum));                                // (added up here: left to the end of the step all of them stay in registers)
+        l_run[n] = sum;
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    // V^T operands: product m of lane (r, grp) is d = D/16 * r + m, keys 8 * grp + 0..7; a byte of the codes has two products' values
+    float fv[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) fv[e] = kvq_scale((v.scale[e >> 2] >> (8 * (e & 3))) & 255u);
+    if constexpr (D == 64) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v.code[e] >>= 16 * (r & 1);
+    }
+#pragma unroll
+    for (int j = 0; j < S::NM / 2; ++j) {
+        uint32_t lo[4], hi[4];
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            uint32_t x, y;
+            if (j == 0) { x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v.code[e], fv[e], 0));
+                          y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v.code[e + 1], fv[e + 1], 0)); }
+            else if (j == 1) { x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v.code[e], fv[e], 1));
+                               y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v.code[e + 1], fv[e + 1], 1)); }
+            else if (j == 2) { x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v.code[e], fv[e], 2));
+                               y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v.code[e + 1], fv[e + 1], 2)); }
+            else { x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v.code[e], fv[e], 3));
+                   y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v.code[e + 1], fv[e + 1], 3)); }
+            lo[e >> 1] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+            hi[e >> 1] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+        }
+        const bf16x8 v0 = __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], lo[2], lo[3]}), v1 = __builtin_bit_cast(bf16x8, u32x4{hi[0], hi[1], hi[2], hi[3]});
+#pragma unroll
+        for (int n = 0; n < NC; ++n) oacc[2 * j][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, p[n], oacc[2 * j][n], 0, 0, 0);
+#pragma unroll
+        for (int n = 0; n < NC; ++n) oacc[2 * j + 1][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, p[n], oacc[2 * j + 1][n], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    if (!whole && __ballot(nan_keys != 0) != 0ull) {
+        int lane2 = lane;
+        asm volatile("" : "+v"(lane2));
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+            const bool sees = (nan_keys & kq_allowed(s_anc[n * 16 + (lane2 & 15)], key0 - L)) != 0;
+#pragma unroll
+            for (int m = 0; m < S::NM; ++m) oacc[m][n] = sees ? floatx4{NAN, NAN, NAN, NAN} : oacc[m][n];
+        }
+    }
 }
 
-constexpr int kKqThreads = 256;
-constexpr int kKqWaves = kKqThreads / kWave;
+// --------------------------------------------------------------------- dealing the rows out
+// The batch's work is one line: sequence by sequence, KV head by KV head, block of columns by block of columns (a unit), each as long as its
+// steps and a constant for what a unit costs besides.  Workgroup w takes the w-th of equal shares of the line, wherever the cuts
+// fall, one piece after the other.  A unit that one workgroup has all of is written at once; otherwise every piece of it leaves a
+// partial result: in the workgroup's second place if the unit goes on behind its share, else in its first.  Whatever the lengths, all
+// workgroups end together.  Workgroups go to the eight XCDs in turn, so their numbers are dealt such that an XCD takes a stretch of the
+// line: the column blocks of a KV head then find its rows in one L2.
+constexpr int kKqUnitCost = 4;                 // in steps
 
-template <int D>
-__global__ __launch_bounds__(kKqThreads) void kvq_attn_kernel(KqArgs a) {
-    constexpr int NM = D / 16;
-    __shared__ float s_m[kKqWaves][16], s_l[kKqWaves][16];
-    __shared__ float s_o[kKqWaves][16][D + 4];
-    const int b = blockIdx.z, hk = blockIdx.y, cb = blockIdx.x, lane = lane_id(), w = wave_id(), r = lane & 15, grp = lane >> 4;
+struct KqChunkPlan {                           // lane = sequence b0 + lane; the same in every wavefront
+    int b0;
+    uint32_t base, end;                        // the chunk's stretch of the line
+    int L, nn, total, cgs;
+    uint32_t len, start;                       // of a unit; where the sequence begins on the line
+};
+
+template <int NC>
+__device__ __forceinline__ void kq_plan_chunk(KqChunkPlan &c, const KqArgs &a, int b0, uint32_t base) {
+    const int lane = lane_id(), b = min(b0 + lane, a.B - 1);
     const KqSeq s = kq_seq(a, b);
-    const int col = cb * 16 + r, i = col / a.G, h = hk * a.G + col % a.G;
-    const bool live = i < s.nn;
-    bf16x8 qop[D / 32];                        // d = (D/4) * grp + 8 * c + 0..7
-#pragma unroll
-    for (int c = 0; c < D / 32; ++c) {
-        u32x4 x = {0, 0, 0, 0};
-        if (live) x = *reinterpret_cast<const u32x4 *>(a.q + (size_t)b * a.q_sb + (size_t)i * a.q_st + (size_t)h * a.q_sh + (D / 4) * grp + 8 * c);
-        qop[c] = __builtin_bit_cast(bf16x8, x);
+    c.b0 = b0; c.base = base;
+    c.L = s.L; c.nn = s.nn; c.total = s.total;
+    c.cgs = (s.nn * a.G + 16 * NC - 1) / (16 * NC);
+    const int steps = (s.total + 31) >> 5;
+    c.len = (uint32_t)((steps + (1 << a.shift) - 1) >> a.shift) + kKqUnitCost;
+    const uint32_t mine = b0 + lane < a.B && s.nn > 0 ? c.len * (uint32_t)(a.Hkv * c.cgs) : 0u;
+    if (mine == 0) c.len = 0;
+    const uint32_t incl = wave_scan_u32(mine);
+    c.start = base + incl - mine;
+    c.end = base + readlane_u32(incl, kWave - 1);
+}
+
+struct KqPiece { int b, hk, cg, L, nn, total, s0, s1, slot, unit; bool direct; };
+
+// The arguments, read where a phase of the kernel needs them: all of them at once are more than the scalar registers hold beside its state.
+__device__ __forceinline__ KqArgs kq_args_plan() {
+    const ArgBlock<KqArgs> g = args_from_here<KqArgs>(0);
+    KqArgs a;
+    a.ctx_lens = g->ctx_lens; a.n_nodes = g->n_nodes; a.B = g->B; a.T = g->T; a.Hkv = g->Hkv; a.G = g->G; a.S = g->S;
+    a.workgroups = g->workgroups; a.least = g->least; a.shift = g->shift; a.max_cgs = g->max_cgs; a.unit_tab = g->unit_tab;
+    return a;
+}
+__device__ __forceinline__ KqArgs kq_args_loop() {
+    const ArgBlock<KqArgs> g = args_from_here<KqArgs>(0);
+    KqArgs a;
+    a.tables = g->tables; a.cache = g->cache; a.M = g->M; a.rbits = g->rbits; a.n_blocks = g->n_blocks; a.block_bytes = g->block_bytes;
+    a.scale_log2 = g->scale_log2;
+    return a;
+}
+__device__ __forceinline__ KqArgs kq_args_query() {
+    const ArgBlock<KqArgs> g = args_from_here<KqArgs>(0);
+    KqArgs a;
+    a.q = g->q; a.q_sb = g->q_sb; a.q_st = g->q_st; a.q_sh = g->q_sh; a.G = g->G; a.T = g->T; a.parents = g->parents;
+    return a;
+}
+__device__ __forceinline__ KqArgs kq_args_end() {
+    const ArgBlock<KqArgs> g = args_from_here<KqArgs>(0);
+    KqArgs a;
+    a.out = g->out; a.o_sb = g->o_sb; a.o_st = g->o_st; a.o_sh = g->o_sh; a.lse = g->lse; a.G = g->G; a.T = g->T; a.Hq = g->Hq; a.part = g->part;
+    a.ctx_lens = g->ctx_lens; a.n_nodes = g->n_nodes; a.S = g->S; a.B = g->B; a.workgroups = g->workgroups;
+    return a;
+}
+
+template <int D, int NC>
+__global__ __launch_bounds__(kKqThreads, NC == 1 ? 4 : 2) void kvq_attn_kernel(KqArgs) {
+    using S = KqShape<D, NC>;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    float *const s_o = reinterpret_cast<float *>(smem);                               // [wavefront][column][ROW]
+    float *const s_m = reinterpret_cast<float *>(smem + S::merge_bytes()), *const s_l = s_m + kKqWaves * S::COLS;
+    uint64_t *const s_anc = reinterpret_cast<uint64_t *>(s_l + kKqWaves * S::COLS);   // the columns' ancestors
+    u32x4 *const s_q = reinterpret_cast<u32x4 *>(s_anc + S::COLS);           // [column block][chunk][lane], the lanes' operands
+    const int tid = threadIdx.x, lane = lane_id(), w = __builtin_amdgcn_readfirstlane(wave_id()), r = lane & 15, grp = lane >> 4;
+    KqArgs a = kq_args_plan();
+    const int wg = (int)(blockIdx.x & 7) * (a.workgroups >> 3) + (int)(blockIdx.x >> 3);             // (a multiple of eight)
+
+    // the line's length, and this workgroup's share of it
+    KqChunkPlan c;
+    uint32_t total_line = 0;
+    for (int b0 = 0; b0 < a.B; b0 += kWave) {
+        kq_plan_chunk<NC>(c, a, b0, total_line);
+        total_line = c.end;
     }
-    const uint64_t words = kq_ancestors(a.parents ? a.parents + (size_t)b * a.T : nullptr, s.nn);
-    const int ii = min(i, RADAR_T_MAX - 1);
-    uint64_t anc = (uint64_t)(uint32_t)__shfl((int)(uint32_t)words, ii) | (uint64_t)(uint32_t)__shfl((int)(uint32_t)(words >> 32), ii) << 32;
-    if (!live) anc = 0;
-    floatx4 oacc[NM];
-#pragma unroll
-    for (int m = 0; m < NM; ++m) oacc[m] = floatx4{0.f, 0.f, 0.f, 0.f};
-    float m_run = -INFINITY, l_run = 0.f;
-    const int32_t *const table = a.tables + (size_t)b * a.M;
-    if (cb * 16 < s.nn * a.G)
-        for (int key0 = w * 32; key0 < s.total; key0 += kKqWaves * 32) {
-            KqStep<D> st;
-            kq_load<D>(st, a, table, hk, key0, s.total);
-            kq_step<D>(st, qop, oacc, m_run, l_run, anc, key0, s.L, a.scale_log2);
+    uint32_t share = max((total_line + a.workgroups - 1) / a.workgroups, (uint32_t)a.least);
+    share = __builtin_amdgcn_readfirstlane(share);
+    uint32_t pos = min((uint64_t)wg * share, (uint64_t)total_line);
+    const uint32_t end = min((uint64_t)pos + share, (uint64_t)total_line);
+    int plan_b0 = 0;                                                 // where on the line the search for a piece goes on
+    uint32_t plan_base = 0;
+
+    auto next_piece = [&](KqPiece &p) -> bool {                      // all values the same in every lane
+        while (pos < end) {
+            const KqArgs a = kq_args_plan();
+            KqChunkPlan c;
+            kq_plan_chunk<NC>(c, a, plan_b0, plan_base);
+            while (pos >= c.end) kq_plan_chunk<NC>(c, a, c.b0 + kWave, c.end);
+            plan_b0 = c.b0; plan_base = c.base;
+            const uint64_t before = __ballot(c.len > 0 && c.start <= pos);
+            const int q = 63 - __clzll((long long)before);
+            const uint32_t len = readlane_u32(c.len, q), first = readlane_u32(c.start, q), u = __builtin_amdgcn_readfirstlane((pos - first) / len), at = first + u * len;
+            const int cgs = (int)readlane_u32((uint32_t)c.cgs, q);
+            p.b = c.b0 + q;
+            p.hk = __builtin_amdgcn_readfirstlane((int)u / cgs);     // (a quotient comes out of vector registers)
+            p.cg = __builtin_amdgcn_readfirstlane((int)u - p.hk * cgs);
+            p.L = (int)readlane_u32((uint32_t)c.L, q);
+            p.nn = (int)readlane_u32((uint32_t)c.nn, q);
+            p.total = (int)readlane_u32((uint32_t)c.total, q);
+            const int steps = (p.total + 31) >> 5;
+            const uint32_t from = pos - at, to = min(end - at, len);
+            p.s0 = min((int)(from > kKqUnitCost ? (from - kKqUnitCost) << a.shift : 0u), steps);
+            p.s1 = min((int)(to > kKqUnitCost ? (to - kKqUnitCost) << a.shift : 0u), steps);
+            p.direct = from == 0 && to == len;
+            p.slot = 2 * wg + (to < len ? 1 : 0);
+            p.unit = (p.b * a.Hkv + p.hk) * a.max_cgs + p.cg;
+            if (from == 0 && tid == 0)                               // for the merge: first and last workgroup
+                a.unit_tab[p.unit] = p.direct ? 0u : (uint32_t)wg << 16 | ((at + len - 1) / share);
+            pos = at + to;
+            return true;
         }
-    const float l = kq_column_sum(l_run);
-    if (grp == 0) { s_m[w][r] = m_run; s_l[w][r] = l; }
+        return false;
+    };
+
+    KqPiece p;
+    while (next_piece(p)) {
+        KqArgs a = kq_args_loop();
+        // (the same in every lane, which the compiler does not see behind the search for the piece)
+        const int32_t *const table = (const int32_t *)(uintptr_t)kq_scalar(a.tables + (size_t)p.b * a.M);
+        const kq_bytes base = (kq_bytes)(uintptr_t)kq_scalar(a.cache + (size_t)p.hk * KvqChunk<D>::bytes(1 << a.rbits));
+        const int mine = p.s0 + w, n_act = min(p.s1 - p.s0, kKqWaves);
+        const bool active = mine < p.s1;
+        // the first step's loads, before the queries
+        KqK<D> k;
+        KqV v;
+        KqIds id{0, 0}, nid{0, 0};
+        if (active) {
+            id = kq_ids(a, table, mine * 32, p.total);
+            nid = kq_ids(a, table, min(mine + kKqWaves, p.s1 - 1) * 32, p.total);
+            const KqBase at = kq_base<D>(a, base, id, mine * 32);
+            kq_load_k<D>(k, at);
+            kq_load_v<D>(v, a, at);
+        }
+        // this lane's columns: their queries' operands (d = D/4 * grp + 8 * c + 0..7) and ancestors
+        const KqArgs aq = kq_args_query();
+        auto query = [&](int n, int ch) {
+            const KqArgs &a = aq;
+            const int col = (p.cg * NC + n) * 16 + r, i = col / a.G;
+            u32x4 x = {0, 0, 0, 0};
+            if (i < p.nn) x = *reinterpret_cast<const u32x4 *>(a.q + (size_t)p.b * a.q_sb + (size_t)i * a.q_st + (size_t)(p.hk * a.G + col - i * a.G) * a.q_sh + (D / 4) * grp + 8 * ch);
+            return x;
+        };
+        bf16x8 q_regs[NC > 2 ? 1 : NC][S::CH];
+        if constexpr (NC > 2) {
+            for (int x = w; x < NC * S::CH; x += kKqWaves) s_q[x * kWave + lane] = query(x / S::CH, x % S::CH);
+        } else {
 #pragma unroll
-    for (int m = 0; m < NM; ++m)
+            for (int n = 0; n < NC; ++n)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s_o[w][r][(D / 4) * grp + NM * e + m] = oacc[m][e];
-    __syncthreads();
-    // a lane: D/16 values of one column
-    const int mc = threadIdx.x & 15, d0 = (threadIdx.x >> 4) * (D / 16), col2 = cb * 16 + mc, i2 = col2 / a.G, h2 = hk * a.G + col2 % a.G;
-    if (i2 >= a.T) return;
-    float M = -INFINITY, sum = 0.f, acc[D / 16];
-    for (int v = 0; v < kKqWaves; ++v) M = fmaxf(M, s_m[v][mc]);
-    const float ref = M == -INFINITY ? 0.f : M;
-    for (int d = 0; d < D / 16; ++d) acc[d] = 0.f;
-    for (int v = 0; v < kKqWaves; ++v) {
-        const float f = __builtin_amdgcn_exp2f(s_m[v][mc] - ref);
-        sum += s_l[v][mc] * f;
-        for (int d = 0; d < D / 16; ++d) acc[d] += s_o[v][mc][d0 + d] * f;
+                for (int ch = 0; ch < S::CH; ++ch) q_regs[n][ch] = __builtin_bit_cast(bf16x8, query(n, ch));
+        }
+        if (w < NC && p.s1 * 32 > p.L) {
+            const uint64_t words = kq_ancestors(aq.parents ? aq.parents + (size_t)p.b * aq.T : nullptr, p.nn);
+            const int i = ((p.cg * NC + w) * 16 + r) / aq.G, ii = min(i, RADAR_T_MAX - 1);
+            const uint32_t lo = (uint32_t)__shfl((int)(uint32_t)words, ii), hi = (uint32_t)__shfl((int)(uint32_t)(words >> 32), ii);
+            if (grp == 0) s_anc[w * 16 + r] = i < p.nn ? (uint64_t)hi << 32 | lo : 0ull;
+        }
+        floatx4 oacc[S::NM][NC];
+        float negref[NC], l_run[NC];
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+            negref[n] = kKqNone;
+            l_run[n] = 0.f;
+#pragma unroll
+            for (int m = 0; m < S::NM; ++m) oacc[m][n] = floatx4{0.f, 0.f, 0.f, 0.f};
+        }
+        __syncthreads();
+        auto qop = [&](int n, int ch) {
+            if constexpr (NC > 2) return __builtin_bit_cast(bf16x8, s_q[(n * S::CH + ch) * kWave + lane]);
+            else return q_regs[n][ch];
+        };
+        if (active)
+            for (int s = mine; s < p.s1; s += kKqWaves) {
+                const int next = min(s + kKqWaves, p.s1 - 1);        // (the last step asks for rows that are there, in vain)
+                KqIds nnid;
+                kq_step<D, NC>(k, v, id, qop, [&] {
+                    nnid = kq_ids(a, table, min(s + 2 * kKqWaves, p.s1 - 1) * 32, p.total);
+                    kq_load_k<D>(k, kq_base<D>(a, base, nid, next * 32));
+                }, oacc, negref, l_run, s_anc, a, s * 32, p.L, p.total);
+                kq_load_v<D>(v, a, kq_base<D>(a, base, nid, next * 32));
+                id = nid;
+                nid = nnid;
+            }
+
+        // the wavefronts' results, added up against their common reference, in NC passes over the outputs
+        a = kq_args_end();
+        int tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));                                // (addresses are worked out here, and not kept from the start)
+        const int r = tid & 15, grp = (tid >> 4) & 3;
+        __syncthreads();                                             // (the merge before, or nobody reads the queries any more)
+        if (w < n_act)
+#pragma unroll
+            for (int n = 0; n < NC; ++n) {
+                const float l = kq_column_sum(l_run[n]);
+                if (grp == 0) { s_m[w * S::COLS + n * 16 + r] = -negref[n]; s_l[w * S::COLS + n * 16 + r] = l; }
+            }
+        __syncthreads();
+        float scl[NC];
+#pragma unroll
+        for (int n = 0; n < NC; ++n) {
+            float M = -kKqNone;
+            for (int x = 0; x < n_act; ++x) M = fmaxf(M, s_m[x * S::COLS + n * 16 + r]);
+            scl[n] = __builtin_amdgcn_exp2f(-negref[n] - M);
+        }
+        // a lane of the pass: four outputs of a column, d = D/4 * part + (4 / NC * pass + e) * NM + m
+        constexpr int Q4 = S::DP / 4, ITEMS = S::COLS * Q4;
+#pragma unroll
+        for (int pass = 0; pass < NC; ++pass) {
+            if (w < n_act)
+#pragma unroll
+                for (int n = 0; n < NC; ++n)
+#pragma unroll
+                    for (int e = 0; e < S::EP; ++e)
+#pragma unroll
+                        for (int m = 0; m < S::NM; m += 4) {
+                            floatx4 x;
+#pragma unroll
+                            for (int y = 0; y < 4; ++y) x[y] = oacc[m + y][n][pass * S::EP + e] * scl[n];
+                            *reinterpret_cast<floatx4 *>(s_o + (w * S::COLS + n * 16 + r) * S::ROW + (grp * S::EP + e) * S::NM + m) = x;
+                        }
+            __syncthreads();
+            for (int item = tid; item < ITEMS; item += kKqThreads) {
+                const int col = item / Q4, x = item % Q4 * 4, part = x / (S::EP * S::NM), in = x % (S::EP * S::NM);
+                floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+                float M = -kKqNone, l = 0.f;
+                for (int y = 0; y < n_act; ++y) {
+                    acc += *reinterpret_cast<const floatx4 *>(s_o + (y * S::COLS + col) * S::ROW + x);
+                    M = fmaxf(M, s_m[y * S::COLS + col]);
+                }
+                for (int y = 0; y < n_act; ++y) l += s_l[y * S::COLS + col] * __builtin_amdgcn_exp2f(s_m[y * S::COLS + col] - M);
+                const int d = D / 4 * part + pass * S::EP * S::NM + in;
+                if (!p.direct) {
+                    float *const to = a.part + (size_t)p.slot * S::PART;
+                    *reinterpret_cast<floatx4 *>(to + (size_t)col * D + d) = acc;
+                    if (d == 0) { to[S::COLS * D + col] = M; to[S::COLS * D + S::COLS + col] = l; }
+                    continue;
+                }
+                const int gc = p.cg * S::COLS + col, i = gc / a.G, h = p.hk * a.G + gc - i * a.G;
+                if (i >= p.nn) continue;
+                kq_write(a, p.b, i, h, d, acc, M, l);
+            }
+            __syncthreads();
+        }
     }
-    const bool on = i2 < s.nn;
-    const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
-    __bf16 *const o = a.out + (size_t)b * a.o_sb + (size_t)i2 * a.o_st + (size_t)h2 * a.o_sh + d0;
-    for (int d = 0; d < D / 16; ++d) o[d] = (__bf16)(on ? acc[d] * inv : 0.f);
-    if (a.lse && d0 == 0) a.lse[((size_t)b * a.T + i2) * a.Hq + h2] = on ? (M + __builtin_amdgcn_logf(sum)) * kqLn2 : 0.f;
+
+    // rows behind a tree's end, and of sequences that are not there: zeros (a lane looks at one row, the wavefront fills those that are found)
+    a = kq_args_end();
+    const int rows = a.B * a.T, step = a.workgroups * kKqWaves;
+    for (int x0 = (int)blockIdx.x + a.workgroups * w; x0 < rows; x0 += step * kWave) {
+        const int x = (int)min((int64_t)x0 + (int64_t)step * lane, (int64_t)rows - 1);
+        uint64_t empty = __ballot((int64_t)x0 + (int64_t)step * lane < rows && x % a.T >= kq_seq(a, x / a.T).nn);
+        for (; empty != 0; empty &= empty - 1) {
+            const int y = x0 + step * (__ffsll((unsigned long long)empty) - 1), b = y / a.T, i = y - b * a.T;
+            __bf16 *const row = a.out + (size_t)b * a.o_sb + (size_t)i * a.o_st;
+            for (int z = lane; z < a.Hq * (D / 8); z += kWave) *reinterpret_cast<u32x4 *>(row + (size_t)(z / (D / 8)) * a.o_sh + z % (D / 8) * 8) = u32x4{0, 0, 0, 0};
+            if (a.lse)
+                for (int z = lane; z < a.Hq; z += kWave) a.lse[(size_t)y * a.Hq + z] = 0.f;
+        }
+    }
+}
+
+// The units that several workgroups had parts of.  A workgroup takes one block of 16 columns of a unit, a lane 4 (D = 64) or 8 outputs of one.
+template <int D, int NC>
+__global__ __launch_bounds__(256) void kvq_merge_kernel(KqArgs a) {
+    using S = KqShape<D, NC>;
+    constexpr int PER = D / 16;
+    const int unit = blockIdx.x, b = unit / (a.Hkv * a.max_cgs), hk = unit / a.max_cgs % a.Hkv, cg = unit % a.max_cgs, n = blockIdx.y;
+    const KqSeq s = kq_seq(a, b);
+    if ((cg * NC + n) * 16 >= s.nn * a.G) return;
+    const uint32_t tab = a.unit_tab[unit];
+    const int w0 = tab >> 16, w1 = tab & 0xffff;
+    if (w0 == w1) return;
+    const int col = n * 16 + threadIdx.x / 16, d = threadIdx.x % 16 * PER;
+    const int gc = cg * S::COLS + col, i = gc / a.G, h = hk * a.G + gc - i * a.G;
+    if (i >= s.nn) return;
+    float M = -kKqNone, l = 0.f;
+    floatx4 acc[PER / 4];
+#pragma unroll
+    for (int x = 0; x < PER / 4; ++x) acc[x] = floatx4{0.f, 0.f, 0.f, 0.f};
+    for (int w = w0; w <= w1; ++w) {
+        const float *const from = a.part + (size_t)(2 * w + (w < w1 ? 1 : 0)) * S::PART;
+        const float m = from[S::COLS * D + col], Mn = fmaxf(M, m), f0 = __builtin_amdgcn_exp2f(M - Mn), f1 = __builtin_amdgcn_exp2f(m - Mn);
+        M = Mn;
+        l = l * f0 + from[S::COLS * D + S::COLS + col] * f1;
+#pragma unroll
+        for (int x = 0; x < PER / 4; ++x) acc[x] = acc[x] * f0 + *reinterpret_cast<const floatx4 *>(from + (size_t)col * D + d + 4 * x) * f1;
+    }
+#pragma unroll
+    for (int x = 0; x < PER / 4; ++x) kq_write(a, b, i, h, d + 4 * x, acc[x], M, l);
 }
 
 }  // namespace radar
@@ -302,9 +653,47 @@ static radar_status check_kvq_attn(const radar_kvq_attn_desc *d) {
     return RADAR_OK;
 }
 
+struct KqPlan {
+    int nc, max_cgs, workgroups, least, shift;
+    bool merge;
+    size_t off_tab, off_part, bytes;
+};
+
+static KqPlan plan_kvq(const radar_kvq_attn_desc *d) {
+    KqPlan p;
+    const int cols = d->Hq / d->cache.Hkv * d->T_max, D = d->cache.D;
+    p.nc = cols <= 16 ? 1 : cols <= 32 ? 2 : 4;
+    p.max_cgs = (cols + 16 * p.nc - 1) / (16 * p.nc);
+    p.workgroups = p.nc == 1 ? 512 : 256;                  // what the chip holds at once
+    p.least = d->rows_per_split ? d->rows_per_split / 32 : 8;
+    // positions on the line stay within 31 bits
+    const int64_t units = (int64_t)d->B * d->cache.Hkv * p.max_cgs, steps = ((int64_t)d->S_max + 31) / 32;
+    p.shift = 0;
+    while (units * ((steps >> p.shift) + 1 + kKqUnitCost) >= (int64_t(1) << 31) && p.shift < 31) ++p.shift;
+    p.merge = steps > p.least;                             // else a share holds any unit... 
+    size_t off = 0;
+    auto take = [&](size_t bytes) { const size_t o = off; off += (bytes + 255) & ~size_t(255); return o; };
+    take(256);                                             // never empty: callers always pass a workspace
+    p.off_tab = take((size_t)units * sizeof(uint32_t));
+    p.off_part = take((size_t)2 * p.workgroups * (16 * p.nc * (D + 2)) * sizeof(float));
+    p.bytes = off;
+    return p;
+}
+
 extern "C" size_t radar_tree_attention_kvq_workspace_bytes(const radar_kvq_attn_desc *d) {
     if (check_kvq_attn(d) != RADAR_OK) return 0;
-    return 256;
+    return plan_kvq(d).bytes;
+}
+
+template <int D, int NC>
+static hipError_t launch_kvq(const KqArgs &a, const KqPlan &p, hipStream_t s) {
+    constexpr int bytes = KqShape<D, NC>::lds_bytes();
+    static const hipError_t configured = hipFuncSetAttribute(reinterpret_cast<const void *>(&kvq_attn_kernel<D, NC>),
+                                                             hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (configured != hipSuccess) return configured;
+    const hipError_t e = launch("kvq_attention", kvq_attn_kernel<D, NC>, dim3((unsigned)p.workgroups), dim3(kKqThreads), bytes, s, a);
+    if (e != hipSuccess) return e;
+    return launch("kvq_merge", kvq_merge_kernel<D, NC>, dim3((unsigned)(a.B * a.Hkv * a.max_cgs), (unsigned)NC), dim3(256), 0, s, a);
 }
 
 extern "C" radar_status radar_tree_attention_kvq(const void *q, const void *cache, const int32_t *block_tables, const int32_t *parents,
@@ -313,7 +702,8 @@ extern "C" radar_status radar_tree_attention_kvq(const void *q, const void *cach
     if (!q || !cache || !block_tables || !ctx_lens || !out || !workspace) return RADAR_INVALID_ARG;
     const radar_status st = check_kvq_attn(d);
     if (st != RADAR_OK) return st;
-    if (workspace_bytes < 256) return RADAR_WORKSPACE_TOO_SMALL;
+    const KqPlan p = plan_kvq(d);
+    if (workspace_bytes < p.bytes) return RADAR_WORKSPACE_TOO_SMALL;
     if (((uintptr_t)workspace & 255) != 0) return RADAR_INVALID_ARG;
     KqArgs a;
     a.q = static_cast<const __bf16 *>(q); a.cache = static_cast<const unsigned char *>(cache);
@@ -322,6 +712,7 @@ extern "C" radar_status radar_tree_attention_kvq(const void *q, const void *cach
     a.B = d->B; a.T = d->T_max; a.Hq = d->Hq; a.Hkv = d->cache.Hkv; a.G = a.Hq / a.Hkv; a.M = d->max_blocks; a.S = d->S_max;
     a.rbits = kvq_log2(d->cache.block_rows); a.n_blocks = d->cache.n_blocks;
     const int64_t D = d->cache.D;
+    a.block_bytes = (int64_t)a.Hkv * d->cache.block_rows * (D + D / 16);
     a.q_sh = d->q_stride_h ? d->q_stride_h : D;
     a.q_st = d->q_stride_t ? d->q_stride_t : D * d->Hq;
     a.q_sb = d->q_stride_b ? d->q_stride_b : D * d->Hq * d->T_max;
@@ -331,10 +722,14 @@ extern "C" radar_status radar_tree_attention_kvq(const void *q, const void *cach
     const uintptr_t al = (uintptr_t)q | (uintptr_t)cache | (uintptr_t)out;
     const int64_t strides = a.q_sh | a.q_st | a.q_sb | a.o_sh | a.o_st | a.o_sb;
     if ((al & 15) != 0 || (strides & 7) != 0 || strides < 0) return RADAR_INVALID_ARG;
+    if ((int64_t)d->B * d->cache.Hkv * p.max_cgs > INT32_MAX || (int64_t)d->B * d->T_max > INT32_MAX) return RADAR_UNSUPPORTED_SHAPE;
     a.scale_log2 = (d->softmax_scale != 0.f ? d->softmax_scale : 1.0f / sqrtf((float)D)) * kqLog2e;
-    const int64_t cols = (int64_t)a.T * a.G;
-    const dim3 grid((unsigned)((cols + 15) / 16), (unsigned)a.Hkv, (unsigned)a.B);
-    const hipError_t e = launch("kvq_attention", d->cache.D == 128 ? kvq_attn_kernel<128> : kvq_attn_kernel<64>, grid, dim3(kKqThreads), 0,
-                                static_cast<hipStream_t>(stream), a);
+    a.workgroups = p.workgroups; a.least = p.least; a.shift = p.shift; a.max_cgs = p.max_cgs;
+    char *ws = static_cast<char *>(workspace);
+    a.unit_tab = reinterpret_cast<uint32_t *>(ws + p.off_tab);
+    a.part = reinterpret_cast<float *>(ws + p.off_part);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const hipError_t e = D == 128 ? (p.nc == 1 ? launch_kvq<128, 1>(a, p, s) : p.nc == 2 ? launch_kvq<128, 2>(a, p, s) : launch_kvq<128, 4>(a, p, s))
+                                  : (p.nc == 1 ? launch_kvq<64, 1>(a, p, s) : p.nc == 2 ? launch_kvq<64, 2>(a, p, s) : launch_kvq<64, 4>(a, p, s));
     return e == hipSuccess ? RADAR_OK : RADAR_HIP_ERROR;
 }
