@@ -35,6 +35,7 @@ struct KqArgs {
     float scale_log2;
     int64_t block_bytes;                       // of a block, all heads
     int workgroups, least, shift, max_cgs;     // least share of the line; log2 steps per unit of it; column blocks of a KV head
+    int unit_cost, whole;                      // what a unit costs besides its steps; whole: units are not divided, and all alike
     float *part;                               // [2 * workgroups] partial results: outputs, maxima (log2 units), sums, in fp32
     uint32_t *unit_tab;                        // first and last workgroup of a unit; alike: it is written already
 };
@@ -116,44 +117,59 @@ __device__ __forceinline__ KqIds kq_ids(const KqArgs &a, const int32_t *table, i
 __device__ __forceinline__ bool kq_there(const KqArgs &a, int blk) { return (uint32_t)blk < (uint32_t)a.n_blocks; }
 
 // Where the two halves' codes and scales begin: a row is D/2 bytes of codes further on, K's or V's, and D/32 bytes of scales.  All of it in
-// scalar registers; a lane adds the place of its own rows, worked out once.
-struct KqBase { kq_bytes code_a, code_b, scale_a, scale_b; };
+// scalar registers; a lane adds the place of its own rows, worked out once.  Two blocks of a layer of less than 4 GB are at most 32 bits apart
+// (FAR: of any layer): a load then takes the lower of the two as its scalar base and an offset in one vector register.
+struct KqBase { kq_bytes code, scale; uint64_t code_up, scale_up; bool second_up; };       // the lower one, how far up the other is, which it is
 template <int D>
 __device__ __forceinline__ KqBase kq_base(const KqArgs &a, kq_bytes base, KqIds id, int key0) {
     const int R = 1 << a.rbits, row_a = key0 & (R - 1), row_b = (key0 + 16) & (R - 1);
-    const kq_bytes ca = base + (uint64_t)(kq_there(a, id.a) ? (uint32_t)id.a : 0u) * (uint64_t)a.block_bytes;
-    const kq_bytes cb = base + (uint64_t)(kq_there(a, id.b) ? (uint32_t)id.b : 0u) * (uint64_t)a.block_bytes;
-    return KqBase{ca + row_a * (D / 2), cb + row_b * (D / 2), ca + R * D + row_a * (D / 32), cb + R * D + row_b * (D / 32)};
+    const uint32_t ia = kq_there(a, id.a) ? (uint32_t)id.a : 0u, ib = kq_there(a, id.b) ? (uint32_t)id.b : 0u;
+    KqBase s;
+    s.second_up = ib >= ia;                                          // (of one block the second half's rows are the later ones)
+    const uint32_t lo = s.second_up ? ia : ib, apart = s.second_up ? ib - ia : ia - ib;
+    const int row = s.second_up ? row_a : row_b, rows = s.second_up ? row_b - row_a : row_a - row_b;
+    const kq_bytes c = base + (uint64_t)lo * (uint64_t)a.block_bytes;
+    const uint64_t up = (uint64_t)apart * (uint64_t)a.block_bytes;
+    s.code = c + row * (D / 2);
+    s.scale = c + R * D + row * (D / 32);
+    s.code_up = up + (int64_t)(rows * (D / 2));
+    s.scale_up = up + (int64_t)(rows * (D / 32));
+    return s;
 }
-__device__ __forceinline__ kq_bytes kq_half(kq_bytes a, kq_bytes b, bool second) { return second ? b : a; }
-template <typename T>
-__device__ __forceinline__ T kq_read(kq_bytes p) { return *reinterpret_cast<const __attribute__((address_space(1))) T *>(p); }
+template <typename T, bool FAR>
+__device__ __forceinline__ T kq_read(kq_bytes base, uint64_t up, bool is_up, uint32_t off) {
+    if constexpr (FAR) return *reinterpret_cast<const __attribute__((address_space(1))) T *>(base + (is_up ? up : 0) + off);
+    else return *reinterpret_cast<const __attribute__((address_space(1))) T *>(base + (uint32_t)((is_up ? (uint32_t)up : 0u) + off));
+}
 
-template <int D>
+template <int D, bool FAR>
 __device__ __forceinline__ void kq_load_k(KqK<D> &k, KqBase s) {
     using C = KvqChunk<D>;
     const int lane = lane_id(), r = lane & 15, grp = lane >> 4, group = (r >> 2) & 1, blk = D == 128 ? grp : grp >> 1;
-    const kq_bytes w = kq_half(s.code_a, s.code_b, r >= 8) + (uint32_t)(C::k_row(8 * group + (r & 3)) + (D / 8) * grp);
+    const bool is_up = (r >= 8) == s.second_up;
+    const uint32_t at = (uint32_t)(C::k_row(8 * group + (r & 3)) + (D / 8) * grp);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
         if constexpr (D == 128) {
-            const u32x4 x = kq_read<u32x4>(w + t * C::k_row(4));
+            const u32x4 x = kq_read<u32x4, FAR>(s.code + t * C::k_row(4), s.code_up, is_up, at);
 #pragma unroll
             for (int i = 0; i < 4; ++i) k.code[t][i] = x[i];
         } else {
-            const u32x2 x = kq_read<u32x2>(w + t * C::k_row(4));
+            const u32x2 x = kq_read<u32x2, FAR>(s.code + t * C::k_row(4), s.code_up, is_up, at);
             k.code[t][0] = x[0]; k.code[t][1] = x[1];
         }
     }
-    k.scale = kq_read<u32x2>(kq_half(s.scale_a, s.scale_b, r >= 8) + (uint32_t)((group * C::kScales + blk) * 8));
+    k.scale = kq_read<u32x2, FAR>(s.scale, s.scale_up, is_up, (uint32_t)((group * C::kScales + blk) * 8));
 }
-template <int D>
+template <int D, bool FAR>
 __device__ __forceinline__ void kq_load_v(KqV &v, const KqArgs &a, KqBase s) {
     using C = KvqChunk<D>;
     const int lane = lane_id(), r = lane & 15, grp = lane >> 4, piece = D == 128 ? r : r >> 1, blk = D == 128 ? r >> 2 : r >> 3;
-    const kq_bytes w = kq_half(s.code_a, s.code_b, grp >= 2) + (((D / 2) << a.rbits) + (uint32_t)(((grp & 1) * C::kPieces + piece) * 32));
-    const u32x4 lo = kq_read<u32x4>(w), hi = kq_read<u32x4>(w + 16);
-    v.scale = kq_read<u32x2>(kq_half(s.scale_a, s.scale_b, grp >= 2) + (((D / 32) << a.rbits) + (uint32_t)(((grp & 1) * C::kScales + blk) * 8)));
+    const bool is_up = (grp >= 2) == s.second_up;
+    const kq_bytes code = s.code + ((D / 2) << a.rbits);
+    const uint32_t at = (uint32_t)(((grp & 1) * C::kPieces + piece) * 32);
+    const u32x4 lo = kq_read<u32x4, FAR>(code, s.code_up, is_up, at), hi = kq_read<u32x4, FAR>(code + 16, s.code_up, is_up, at);
+    v.scale = kq_read<u32x2, FAR>(s.scale + ((D / 32) << a.rbits), s.scale_up, is_up, (uint32_t)(((grp & 1) * C::kScales + blk) * 8));
 #pragma unroll
     for (int e = 0; e < 4; ++e) { v.code[e] = lo[e]; v.code[4 + e] = hi[e]; }
 }
@@ -200,23 +216,24 @@ __device__ __forceinline__ uint32_t kq_allowed(uint64_t anc, int first) {
 // operands (about 115 vector instructions a step) is shared by its columns only, hence as many as registers allow: with 64 columns the outputs
 // take 128 registers, and the queries' operands stay in LDS.
 constexpr int kKqWaves = 8, kKqThreads = kKqWaves * kWave;
-constexpr float kKqSlack = 8.0f;               // how far a column's maximum may pass its reference (log2 units) before sums are rescaled
+constexpr float kKqMost = 2048.0f;             // what a lane's eight weights may add up to before the reference is moved
 constexpr float kKqNone = 3.0e38f;             // negated reference of a column that has seen no key yet
 
 template <int D, int NC>
 struct KqShape {
     static constexpr int NM = D / 16, CH = D / 32, COLS = 16 * NC;   // output tiles; steps of the scores' product; columns
-    static constexpr int EP = 4 / NC, DP = D / NC;                   // the merge goes over the outputs in NC passes: registers, values of a pass
+    static constexpr int PASSES = NC * D > 256 ? 2 : 1;              // the merge goes over the outputs in so many passes (its buffer is 139 KB at most)
+    static constexpr int EP = 4 / PASSES, DP = D / PASSES;           // registers, values of a pass
     static constexpr int ROW = DP + 4;                               // of the merge's buffer: rows 16 bytes apart from a multiple of the banks
     static constexpr int q_bytes() { return COLS * D * 2; }
     static constexpr int merge_bytes() { return kKqWaves * COLS * ROW * 4; }
-    static constexpr int lds_bytes() { return merge_bytes() + (kKqWaves + 1) * COLS * 8 + (NC > 2 ? q_bytes() : 0); }
+    static constexpr int lds_bytes() { return merge_bytes() + (kKqWaves + 2) * COLS * 8 + kKqWaves * 64 + (NC > 2 ? q_bytes() : 0); }
     static constexpr int PART = COLS * D + 2 * COLS;                 // floats of a partial result: outputs, maxima, sums
 };
 
 // One wavefront, one step: scores of 32 keys, softmax against the running reference, outputs.  The loads of the wavefront's next step are
 // asked for as soon as the registers of this one's are free: K's after the scores, V's at the end.
-template <int D, int NC, typename QOp, typename NextK>
+template <int D, int NC, int AHEAD, typename QOp, typename NextK>
 __device__ __forceinline__ void kq_step(const KqK<D> &k, KqV &v, KqIds id, QOp qop, NextK next_k, floatx4 (&oacc)[D / 16][NC], float (&negref)[NC],
                                         float (&l_run)[NC], const uint64_t *s_anc, const KqArgs &a, int key0, int L, int total) {
     using S = KqShape<D, NC>;
@@ -228,8 +245,8 @@ __device__ __forceinline__ void kq_step(const KqK<D> &k, KqV &v, KqIds id, QOp q
         for (int n = 0; n < NC; ++n) sacc[t][n] = floatx4{0.f, 0.f, 0.f, 0.f};
     const uint32_t pick = 0x0c0c0cu | (uint32_t)(r & 3) << 24;       // that byte on top, zeros under it
     const float f[2] = {__uint_as_float(__builtin_amdgcn_perm(0u, k.scale[0], pick) >> 1), __uint_as_float(__builtin_amdgcn_perm(0u, k.scale[1], pick) >> 1)};
-    // (the queries' operands come from LDS where there are many: asked for two column blocks ahead)
-    constexpr int NQ = NC * S::CH, AHEAD = NC > 2 ? 2 : NQ;
+    // (the queries' operands come from LDS where there are many: asked for AHEAD of them ahead)
+    constexpr int NQ = NC * S::CH;
     bf16x8 q[AHEAD];
 #pragma unroll
     for (int x = 0; x < AHEAD; ++x) q[x] = qop(x % NC, x / NC);
@@ -272,25 +289,33 @@ __device__ __forceinline__ void kq_step(const KqK<D> &k, KqV &v, KqIds id, QOp q
     bf16x8 p[NC];
 #pragma unroll
     for (int n = 0; n < NC; ++n) {
-        float mx = sacc[0][n][0];
+        // The eight scores' exponentials against the running reference; p is the matrix cores' operand, the sum is of the unrounded ones, in fp32.
+        auto weigh = [&] {
+            float sum = 0.f;
 #pragma unroll
-        for (int e = 1; e < 8; ++e) mx = fmaxf(mx, sacc[e >> 2][n][e & 3]);
-        // The reference follows the maximum only when that has risen by more than 8: then, and only then, do the four lanes of a column compare
-        // theirs and the sums get rescaled.  (A probability may be as large as 2^8 instead of 1: it keeps its eight bits.)
-        if (__any(__builtin_fmaf(mx, a.scale_log2, negref[n]) > kKqSlack)) {
+            for (int e = 0; e < 8; ++e) {
+                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[e >> 2][n][e & 3], a.scale_log2, negref[n]));
+                sum = e == 0 ? w : sum + w;
+                p[n][e] = (__bf16)w;
+            }
+            return sum;
+        };
+        float sum = weigh();
+        // The reference is the columns' maximum at the time when some lane's sum last went past 2^11 (for a column without a key: at once).  Only then
+        // do the four lanes of a column compare their maxima, and outputs and sums get rescaled: no step but a wavefront's first does it as a rule.
+        // Weights of up to 2^11 instead of 1 lose nothing: they keep bf16's eight bits, and sums and outputs are fp32.
+        if (__any(sum > kKqMost)) {
+            float mx = sacc[0][n][0];
+#pragma unroll
+            for (int e = 1; e < 8; ++e) mx = fmaxf(mx, sacc[e >> 2][n][e & 3]);
             const float neg = fminf(negref[n], -(kq_column_max(mx) * a.scale_log2)), alpha = __builtin_amdgcn_exp2f(neg - negref[n]);
             negref[n] = neg;
             l_run[n] *= alpha;
 #pragma unroll
             for (int m = 0; m < S::NM; ++m) oacc[m][n] *= alpha;
+            sum = weigh();
         }
-        float sum = l_run[n];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[e >> 2][n][e & 3], a.scale_log2, negref[n]));
-            sum += w;
-            p[n][e] = (__bf16)w;                                     // the matrix cores' operand; the sum is of the unrounded ones, in fp32
-        }
+        sum += l_run[n];
         asm volatile("" : "+v"(sum));                                // (added up here: left to the end of the step all of them stay in registers)
         l_run[n] = sum;
         __builtin_amdgcn_sched_barrier(0);
@@ -346,7 +371,6 @@ __device__ __forceinline__ void kq_step(const KqK<D> &k, KqV &v, KqIds id, QOp q
 // partial result: in the workgroup's second place if the unit goes on behind its share, else in its first.  Whatever the lengths, all
 // workgroups end together.  Workgroups go to the eight XCDs in turn, so their numbers are dealt such that an XCD takes a stretch of the
 // line: the column blocks of a KV head then find its rows in one L2.
-constexpr int kKqUnitCost = 4;                 // in steps
 
 struct KqChunkPlan {                           // lane = sequence b0 + lane; the same in every wavefront
     int b0;
@@ -354,6 +378,9 @@ struct KqChunkPlan {                           // lane = sequence b0 + lane; the
     int L, nn, total, cgs;
     uint32_t len, start;                       // of a unit; where the sequence begins on the line
 };
+
+// workgroups: a multiple of eight
+__device__ __forceinline__ int kq_number(const KqArgs &a) { return (int)(blockIdx.x & 7) * (a.workgroups >> 3) + (int)(blockIdx.x >> 3); }
 
 template <int NC>
 __device__ __forceinline__ void kq_plan_chunk(KqChunkPlan &c, const KqArgs &a, int b0, uint32_t base) {
@@ -363,7 +390,7 @@ __device__ __forceinline__ void kq_plan_chunk(KqChunkPlan &c, const KqArgs &a, i
     c.L = s.L; c.nn = s.nn; c.total = s.total;
     c.cgs = (s.nn * a.G + 16 * NC - 1) / (16 * NC);
     const int steps = (s.total + 31) >> 5;
-    c.len = (uint32_t)((steps + (1 << a.shift) - 1) >> a.shift) + kKqUnitCost;
+    c.len = a.whole ? 1u : (uint32_t)((steps + (1 << a.shift) - 1) >> a.shift) + (uint32_t)a.unit_cost;
     const uint32_t mine = b0 + lane < a.B && s.nn > 0 ? c.len * (uint32_t)(a.Hkv * c.cgs) : 0u;
     if (mine == 0) c.len = 0;
     const uint32_t incl = wave_scan_u32(mine);
@@ -371,7 +398,26 @@ __device__ __forceinline__ void kq_plan_chunk(KqChunkPlan &c, const KqArgs &a, i
     c.end = base + readlane_u32(incl, kWave - 1);
 }
 
-struct KqPiece { int b, hk, cg, L, nn, total, s0, s1, slot, unit; bool direct; };
+// A workgroup's place on the line and its piece, which wait in LDS (every wavefront has its own copy) while the loop needs the scalar registers.
+struct KqPlace { uint32_t pos, end, share; int b0; uint32_t base; };
+struct KqPiece { int b, hk, cg, nn, slot, L, total, s0, s1; };       // slot: of its partial result, -1: it is all of its unit
+constexpr int kKqState = 16;                   // words of a wavefront's copy: the place, then the piece
+template <typename T>
+__device__ __forceinline__ T kq_recall(const int *from) {            // the same in every lane
+    constexpr int N = sizeof(T) / 4;
+    int v[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = __builtin_amdgcn_readfirstlane(from[i]);
+    return __builtin_bit_cast(T, v);
+}
+template <typename T>
+__device__ __forceinline__ void kq_remember(int *to, T x) {
+    constexpr int N = sizeof(T) / 4;
+    int v[N];
+    __builtin_memcpy(v, &x, sizeof(T));
+#pragma unroll
+    for (int i = 0; i < N; ++i) to[i] = v[i];
+}
 
 // The arguments, read where a phase of the kernel needs them: all of them at once are more than the scalar registers hold beside its state.
 __device__ __forceinline__ KqArgs kq_args_plan() {
@@ -379,6 +425,7 @@ __device__ __forceinline__ KqArgs kq_args_plan() {
     KqArgs a;
     a.ctx_lens = g->ctx_lens; a.n_nodes = g->n_nodes; a.B = g->B; a.T = g->T; a.Hkv = g->Hkv; a.G = g->G; a.S = g->S;
     a.workgroups = g->workgroups; a.least = g->least; a.shift = g->shift; a.max_cgs = g->max_cgs; a.unit_tab = g->unit_tab;
+    a.unit_cost = g->unit_cost; a.whole = g->whole;
     return a;
 }
 __device__ __forceinline__ KqArgs kq_args_loop() {
@@ -402,71 +449,76 @@ __device__ __forceinline__ KqArgs kq_args_end() {
     return a;
 }
 
-template <int D, int NC>
+template <int D, int NC, bool FAR>
 __global__ __launch_bounds__(kKqThreads, NC == 1 ? 4 : 2) void kvq_attn_kernel(KqArgs) {
     using S = KqShape<D, NC>;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     float *const s_o = reinterpret_cast<float *>(smem);                               // [wavefront][column][ROW]
     float *const s_m = reinterpret_cast<float *>(smem + S::merge_bytes()), *const s_l = s_m + kKqWaves * S::COLS;
-    uint64_t *const s_anc = reinterpret_cast<uint64_t *>(s_l + kKqWaves * S::COLS);   // the columns' ancestors
-    u32x4 *const s_q = reinterpret_cast<u32x4 *>(s_anc + S::COLS);           // [column block][chunk][lane], the lanes' operands
-    const int tid = threadIdx.x, lane = lane_id(), w = __builtin_amdgcn_readfirstlane(wave_id()), r = lane & 15, grp = lane >> 4;
-    KqArgs a = kq_args_plan();
-    const int wg = (int)(blockIdx.x & 7) * (a.workgroups >> 3) + (int)(blockIdx.x >> 3);             // (a multiple of eight)
+    float *const s_M = s_l + kKqWaves * S::COLS, *const s_L = s_M + S::COLS;          // of all wavefronts
+    uint64_t *const s_anc = reinterpret_cast<uint64_t *>(s_L + S::COLS);              // the columns' ancestors
+    int *const s_state = reinterpret_cast<int *>(s_anc + S::COLS);
+    u32x4 *const s_q = reinterpret_cast<u32x4 *>(s_state + kKqWaves * kKqState);      // [column block][chunk][lane], the lanes' operands
+    const int lane = lane_id(), w = __builtin_amdgcn_readfirstlane(wave_id()), r = lane & 15, grp = lane >> 4;
+    int *const state = s_state + w * kKqState;
 
     // the line's length, and this workgroup's share of it
-    KqChunkPlan c;
-    uint32_t total_line = 0;
-    for (int b0 = 0; b0 < a.B; b0 += kWave) {
-        kq_plan_chunk<NC>(c, a, b0, total_line);
-        total_line = c.end;
-    }
-    uint32_t share = max((total_line + a.workgroups - 1) / a.workgroups, (uint32_t)a.least);
-    share = __builtin_amdgcn_readfirstlane(share);
-    uint32_t pos = min((uint64_t)wg * share, (uint64_t)total_line);
-    const uint32_t end = min((uint64_t)pos + share, (uint64_t)total_line);
-    int plan_b0 = 0;                                                 // where on the line the search for a piece goes on
-    uint32_t plan_base = 0;
-
-    auto next_piece = [&](KqPiece &p) -> bool {                      // all values the same in every lane
-        while (pos < end) {
-            const KqArgs a = kq_args_plan();
-            KqChunkPlan c;
-            kq_plan_chunk<NC>(c, a, plan_b0, plan_base);
-            while (pos >= c.end) kq_plan_chunk<NC>(c, a, c.b0 + kWave, c.end);
-            plan_b0 = c.b0; plan_base = c.base;
-            const uint64_t before = __ballot(c.len > 0 && c.start <= pos);
-            const int q = 63 - __clzll((long long)before);
-            const uint32_t len = readlane_u32(c.len, q), first = readlane_u32(c.start, q), u = __builtin_amdgcn_readfirstlane((pos - first) / len), at = first + u * len;
-            const int cgs = (int)readlane_u32((uint32_t)c.cgs, q);
-            p.b = c.b0 + q;
-            p.hk = __builtin_amdgcn_readfirstlane((int)u / cgs);     // (a quotient comes out of vector registers)
-            p.cg = __builtin_amdgcn_readfirstlane((int)u - p.hk * cgs);
-            p.L = (int)readlane_u32((uint32_t)c.L, q);
-            p.nn = (int)readlane_u32((uint32_t)c.nn, q);
-            p.total = (int)readlane_u32((uint32_t)c.total, q);
-            const int steps = (p.total + 31) >> 5;
-            const uint32_t from = pos - at, to = min(end - at, len);
-            p.s0 = min((int)(from > kKqUnitCost ? (from - kKqUnitCost) << a.shift : 0u), steps);
-            p.s1 = min((int)(to > kKqUnitCost ? (to - kKqUnitCost) << a.shift : 0u), steps);
-            p.direct = from == 0 && to == len;
-            p.slot = 2 * wg + (to < len ? 1 : 0);
-            p.unit = (p.b * a.Hkv + p.hk) * a.max_cgs + p.cg;
-            if (from == 0 && tid == 0)                               // for the merge: first and last workgroup
-                a.unit_tab[p.unit] = p.direct ? 0u : (uint32_t)wg << 16 | ((at + len - 1) / share);
-            pos = at + to;
-            return true;
+    {
+        const KqArgs a = kq_args_plan();
+        KqChunkPlan c;
+        uint32_t line = 0;
+        for (int b0 = 0; b0 < a.B; b0 += kWave) {
+            kq_plan_chunk<NC>(c, a, b0, line);
+            line = c.end;
         }
-        return false;
+        const uint32_t share = max((line + a.workgroups - 1) / a.workgroups, (uint32_t)a.least);
+        const uint32_t pos = min((uint64_t)kq_number(a) * share, (uint64_t)line);
+        kq_remember(state, KqPlace{pos, (uint32_t)min((uint64_t)pos + share, (uint64_t)line), share, 0, 0});
+    }
+    auto next_piece = [&]() -> bool {                                // all values the same in every lane
+        const KqArgs a = kq_args_plan();
+        KqPlace x = kq_recall<KqPlace>(state);
+        if (x.pos >= x.end) return false;
+        KqChunkPlan c;
+        kq_plan_chunk<NC>(c, a, x.b0, x.base);
+        while (x.pos >= c.end) kq_plan_chunk<NC>(c, a, c.b0 + kWave, c.end);
+        x.b0 = c.b0; x.base = c.base;
+        const uint64_t before = __ballot(c.len > 0 && c.start <= x.pos);
+        const int q = 63 - __clzll((long long)before);
+        const uint32_t len = readlane_u32(c.len, q), first = readlane_u32(c.start, q);
+        const uint32_t u = __builtin_amdgcn_readfirstlane((x.pos - first) / len), at = first + u * len;      // (a quotient comes out of vector registers)
+        const int cgs = (int)readlane_u32((uint32_t)c.cgs, q), wg = kq_number(a);
+        KqPiece p;
+        p.b = c.b0 + q;
+        p.hk = __builtin_amdgcn_readfirstlane((int)u / cgs);
+        p.cg = (int)u - p.hk * cgs;
+        p.L = (int)readlane_u32((uint32_t)c.L, q);
+        p.nn = (int)readlane_u32((uint32_t)c.nn, q);
+        p.total = (int)readlane_u32((uint32_t)c.total, q);
+        const int steps = (p.total + 31) >> 5;
+        const uint32_t from = x.pos - at, to = min(x.end - at, len), cost = (uint32_t)a.unit_cost;
+        if (a.whole) {
+            p.s0 = 0; p.s1 = steps;
+        } else {
+            p.s0 = min((int)(from > cost ? (from - cost) << a.shift : 0u), steps);
+            p.s1 = min((int)(to > cost ? (to - cost) << a.shift : 0u), steps);
+        }
+        p.slot = from == 0 && to == len ? -1 : 2 * wg + (to < len ? 1 : 0);
+        if (from == 0 && threadIdx.x == 0)                           // for the merge: first and last workgroup
+            a.unit_tab[(p.b * a.Hkv + p.hk) * a.max_cgs + p.cg] = p.slot < 0 ? 0u : (uint32_t)wg << 16 | ((at + len - 1) / x.share);
+        x.pos = at + to;
+        kq_remember(state, x);
+        kq_remember(state + sizeof(KqPlace) / 4, p);
+        return true;
     };
 
-    KqPiece p;
-    while (next_piece(p)) {
+    while (next_piece()) {
+        KqPiece p = kq_recall<KqPiece>(state + sizeof(KqPlace) / 4);
         KqArgs a = kq_args_loop();
         // (the same in every lane, which the compiler does not see behind the search for the piece)
         const int32_t *const table = (const int32_t *)(uintptr_t)kq_scalar(a.tables + (size_t)p.b * a.M);
         const kq_bytes base = (kq_bytes)(uintptr_t)kq_scalar(a.cache + (size_t)p.hk * KvqChunk<D>::bytes(1 << a.rbits));
-        const int mine = p.s0 + w, n_act = min(p.s1 - p.s0, kKqWaves);
+        const int mine = p.s0 + w;
         const bool active = mine < p.s1;
         // the first step's loads, before the queries
         KqK<D> k;
@@ -476,8 +528,8 @@ __global__ __launch_bounds__(kKqThreads, NC == 1 ? 4 : 2) void kvq_attn_kernel(K
             id = kq_ids(a, table, mine * 32, p.total);
             nid = kq_ids(a, table, min(mine + kKqWaves, p.s1 - 1) * 32, p.total);
             const KqBase at = kq_base<D>(a, base, id, mine * 32);
-            kq_load_k<D>(k, at);
-            kq_load_v<D>(v, a, at);
+            kq_load_k<D, FAR>(k, at);
+            kq_load_v<D, FAR>(v, a, at);
         }
         // this lane's columns: their queries' operands (d = D/4 * grp + 8 * c + 0..7) and ancestors
         const KqArgs aq = kq_args_query();
@@ -519,80 +571,95 @@ __global__ __launch_bounds__(kKqThreads, NC == 1 ? 4 : 2) void kvq_attn_kernel(K
         };
         if (active)
             for (int s = mine; s < p.s1; s += kKqWaves) {
+                // Two wavefronts share a SIMD, w and w + 4, which left alone lets the older one have its way: they are favoured in turn.
+                if (((s >> 3) ^ (w >> 2)) & 1) __builtin_amdgcn_s_setprio(1); else __builtin_amdgcn_s_setprio(0);
                 const int next = min(s + kKqWaves, p.s1 - 1);        // (the last step asks for rows that are there, in vain)
                 KqIds nnid;
-                kq_step<D, NC>(k, v, id, qop, [&] {
+                kq_step<D, NC, NC <= 2 ? NC * S::CH : FAR ? 2 : 4>(k, v, id, qop, [&] {
                     nnid = kq_ids(a, table, min(s + 2 * kKqWaves, p.s1 - 1) * 32, p.total);
-                    kq_load_k<D>(k, kq_base<D>(a, base, nid, next * 32));
+                    kq_load_k<D, FAR>(k, kq_base<D>(a, base, nid, next * 32));
                 }, oacc, negref, l_run, s_anc, a, s * 32, p.L, p.total);
-                kq_load_v<D>(v, a, kq_base<D>(a, base, nid, next * 32));
+                kq_load_v<D, FAR>(v, a, kq_base<D>(a, base, nid, next * 32));
                 id = nid;
                 nid = nnid;
             }
 
-        // the wavefronts' results, added up against their common reference, in NC passes over the outputs
+        __builtin_amdgcn_s_setprio(0);
+        // the wavefronts' results, added up against their common reference
         a = kq_args_end();
+        p = kq_recall<KqPiece>(state + sizeof(KqPlace) / 4);
         int tid = threadIdx.x;
         asm volatile("" : "+v"(tid));                                // (addresses are worked out here, and not kept from the start)
         const int r = tid & 15, grp = (tid >> 4) & 3;
-        __syncthreads();                                             // (the merge before, or nobody reads the queries any more)
-        if (w < n_act)
+        // A lane's outputs after the merge: of one column, IPT times four.  (Wavefronts that had no step add zeros.)
+        constexpr int Q4 = S::DP / 4, TPC = kKqThreads / S::COLS < Q4 ? kKqThreads / S::COLS : Q4, IPT = Q4 / TPC;      // fours of a pass; lanes of a column
 #pragma unroll
-            for (int n = 0; n < NC; ++n) {
-                const float l = kq_column_sum(l_run[n]);
-                if (grp == 0) { s_m[w * S::COLS + n * 16 + r] = -negref[n]; s_l[w * S::COLS + n * 16 + r] = l; }
-            }
+        for (int n = 0; n < NC; ++n) {
+            const float l = kq_column_sum(l_run[n]);
+            if (grp == 0) { s_m[w * S::COLS + n * 16 + r] = -negref[n]; s_l[w * S::COLS + n * 16 + r] = l; }
+        }
+        __syncthreads();
+        if (tid < S::COLS) {
+            float m[kKqWaves], M = -kKqNone, l = 0.f;
+#pragma unroll
+            for (int x = 0; x < kKqWaves; ++x) m[x] = s_m[x * S::COLS + tid];
+#pragma unroll
+            for (int x = 0; x < kKqWaves; ++x) M = fmaxf(M, m[x]);
+#pragma unroll
+            for (int x = 0; x < kKqWaves; ++x) l += s_l[x * S::COLS + tid] * __builtin_amdgcn_exp2f(m[x] - M);
+            s_M[tid] = M;
+            s_L[tid] = l;
+        }
         __syncthreads();
         float scl[NC];
 #pragma unroll
-        for (int n = 0; n < NC; ++n) {
-            float M = -kKqNone;
-            for (int x = 0; x < n_act; ++x) M = fmaxf(M, s_m[x * S::COLS + n * 16 + r]);
-            scl[n] = __builtin_amdgcn_exp2f(-negref[n] - M);
-        }
-        // a lane of the pass: four outputs of a column, d = D/4 * part + (4 / NC * pass + e) * NM + m
-        constexpr int Q4 = S::DP / 4, ITEMS = S::COLS * Q4;
+        for (int n = 0; n < NC; ++n) scl[n] = __builtin_amdgcn_exp2f(-negref[n] - s_M[n * 16 + r]);
 #pragma unroll
-        for (int pass = 0; pass < NC; ++pass) {
-            if (w < n_act)
+        for (int pass = 0; pass < S::PASSES; ++pass) {               // of a column: d = D/4 * part + (4 / PASSES * pass + e) * NM + m
+            if (pass > 0) __syncthreads();
 #pragma unroll
-                for (int n = 0; n < NC; ++n)
+            for (int n = 0; n < NC; ++n)
 #pragma unroll
-                    for (int e = 0; e < S::EP; ++e)
+                for (int e = 0; e < S::EP; ++e)
 #pragma unroll
-                        for (int m = 0; m < S::NM; m += 4) {
-                            floatx4 x;
+                    for (int m = 0; m < S::NM; m += 4) {
+                        floatx4 x;
 #pragma unroll
-                            for (int y = 0; y < 4; ++y) x[y] = oacc[m + y][n][pass * S::EP + e] * scl[n];
-                            *reinterpret_cast<floatx4 *>(s_o + (w * S::COLS + n * 16 + r) * S::ROW + (grp * S::EP + e) * S::NM + m) = x;
-                        }
+                        for (int y = 0; y < 4; ++y) x[y] = oacc[m + y][n][pass * S::EP + e] * scl[n];
+                        *reinterpret_cast<floatx4 *>(s_o + (w * S::COLS + n * 16 + r) * S::ROW + (grp * S::EP + e) * S::NM + m) = x;
+                    }
             __syncthreads();
-            for (int item = tid; item < ITEMS; item += kKqThreads) {
-                const int col = item / Q4, x = item % Q4 * 4, part = x / (S::EP * S::NM), in = x % (S::EP * S::NM);
-                floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-                float M = -kKqNone, l = 0.f;
-                for (int y = 0; y < n_act; ++y) {
-                    acc += *reinterpret_cast<const floatx4 *>(s_o + (y * S::COLS + col) * S::ROW + x);
-                    M = fmaxf(M, s_m[y * S::COLS + col]);
+            int lane2 = threadIdx.x;
+            asm volatile("" : "+v"(lane2));
+            const int mc = lane2 / TPC, mx = lane2 % TPC * 4, gc = p.cg * S::COLS + mc, mi = gc / a.G, mh = p.hk * a.G + gc - mi * a.G;
+            if (mc < S::COLS && (p.slot >= 0 || mi < p.nn)) {
+                const float M = s_M[mc], l = s_L[mc];
+                floatx4 o[IPT][kKqWaves];
+#pragma unroll
+                for (int z = 0; z < IPT; ++z)
+#pragma unroll
+                    for (int y = 0; y < kKqWaves; ++y) o[z][y] = *reinterpret_cast<const floatx4 *>(s_o + (y * S::COLS + mc) * S::ROW + z * TPC * 4 + mx);
+#pragma unroll
+                for (int z = 0; z < IPT; ++z) {
+                    const int x = z * TPC * 4 + mx, d = D / 4 * (x / (S::EP * S::NM)) + pass * S::EP * S::NM + x % (S::EP * S::NM);
+                    floatx4 acc = o[z][0];
+#pragma unroll
+                    for (int y = 1; y < kKqWaves; ++y) acc += o[z][y];
+                    if (p.slot >= 0) {
+                        float *const to = a.part + (size_t)p.slot * S::PART;
+                        *reinterpret_cast<floatx4 *>(to + mc * D + d) = acc;
+                        if (d == 0) { to[S::COLS * D + mc] = M; to[S::COLS * D + S::COLS + mc] = l; }
+                    } else {
+                        kq_write(a, p.b, mi, mh, d, acc, M, l);
+                    }
                 }
-                for (int y = 0; y < n_act; ++y) l += s_l[y * S::COLS + col] * __builtin_amdgcn_exp2f(s_m[y * S::COLS + col] - M);
-                const int d = D / 4 * part + pass * S::EP * S::NM + in;
-                if (!p.direct) {
-                    float *const to = a.part + (size_t)p.slot * S::PART;
-                    *reinterpret_cast<floatx4 *>(to + (size_t)col * D + d) = acc;
-                    if (d == 0) { to[S::COLS * D + col] = M; to[S::COLS * D + S::COLS + col] = l; }
-                    continue;
-                }
-                const int gc = p.cg * S::COLS + col, i = gc / a.G, h = p.hk * a.G + gc - i * a.G;
-                if (i >= p.nn) continue;
-                kq_write(a, p.b, i, h, d, acc, M, l);
             }
-            __syncthreads();
         }
+        __syncthreads();
     }
 
     // rows behind a tree's end, and of sequences that are not there: zeros (a lane looks at one row, the wavefront fills those that are found)
-    a = kq_args_end();
+    const KqArgs a = kq_args_end();
     const int rows = a.B * a.T, step = a.workgroups * kKqWaves;
     for (int x0 = (int)blockIdx.x + a.workgroups * w; x0 < rows; x0 += step * kWave) {
         const int x = (int)min((int64_t)x0 + (int64_t)step * lane, (int64_t)rows - 1);
@@ -654,8 +721,8 @@ static radar_status check_kvq_attn(const radar_kvq_attn_desc *d) {
 }
 
 struct KqPlan {
-    int nc, max_cgs, workgroups, least, shift;
-    bool merge;
+    int nc, max_cgs, workgroups, least, shift, unit_cost;
+    bool whole;                                            // no unit is divided: no merge
     size_t off_tab, off_part, bytes;
 };
 
@@ -665,12 +732,14 @@ static KqPlan plan_kvq(const radar_kvq_attn_desc *d) {
     p.nc = cols <= 16 ? 1 : cols <= 32 ? 2 : 4;
     p.max_cgs = (cols + 16 * p.nc - 1) / (16 * p.nc);
     p.workgroups = p.nc == 1 ? 512 : 256;                  // what the chip holds at once
-    p.least = d->rows_per_split ? d->rows_per_split / 32 : 8;
-    // positions on the line stay within 31 bits
     const int64_t units = (int64_t)d->B * d->cache.Hkv * p.max_cgs, steps = ((int64_t)d->S_max + 31) / 32;
+    p.least = d->rows_per_split ? d->rows_per_split / 32 : 8;
+    p.unit_cost = p.nc == 1 ? 16 : 24;
+    p.whole = d->rows_per_split == 0 && steps <= 24;
+    if (p.whole) p.least = 1;
+    // positions on the line stay within 31 bits
     p.shift = 0;
-    while (units * ((steps >> p.shift) + 1 + kKqUnitCost) >= (int64_t(1) << 31) && p.shift < 31) ++p.shift;
-    p.merge = steps > p.least;                             // else a share holds any unit... 
+    while (units * ((steps >> p.shift) + 1 + p.unit_cost) >= (int64_t(1) << 31) && p.shift < 31) ++p.shift;
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t o = off; off += (bytes + 255) & ~size_t(255); return o; };
     take(256);                                             // never empty: callers always pass a workspace
@@ -685,14 +754,15 @@ extern "C" size_t radar_tree_attention_kvq_workspace_bytes(const radar_kvq_attn_
     return plan_kvq(d).bytes;
 }
 
-template <int D, int NC>
+template <int D, int NC, bool FAR>
 static hipError_t launch_kvq(const KqArgs &a, const KqPlan &p, hipStream_t s) {
     constexpr int bytes = KqShape<D, NC>::lds_bytes();
-    static const hipError_t configured = hipFuncSetAttribute(reinterpret_cast<const void *>(&kvq_attn_kernel<D, NC>),
+    static const hipError_t configured = hipFuncSetAttribute(reinterpret_cast<const void *>(&kvq_attn_kernel<D, NC, FAR>),
                                                              hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (configured != hipSuccess) return configured;
-    const hipError_t e = launch("kvq_attention", kvq_attn_kernel<D, NC>, dim3((unsigned)p.workgroups), dim3(kKqThreads), bytes, s, a);
+    const hipError_t e = launch("kvq_attention", kvq_attn_kernel<D, NC, FAR>, dim3((unsigned)p.workgroups), dim3(kKqThreads), bytes, s, a);
     if (e != hipSuccess) return e;
+    if (p.whole) return e;
     return launch("kvq_merge", kvq_merge_kernel<D, NC>, dim3((unsigned)(a.B * a.Hkv * a.max_cgs), (unsigned)NC), dim3(256), 0, s, a);
 }
 
@@ -725,11 +795,18 @@ extern "C" radar_status radar_tree_attention_kvq(const void *q, const void *cach
     if ((int64_t)d->B * d->cache.Hkv * p.max_cgs > INT32_MAX || (int64_t)d->B * d->T_max > INT32_MAX) return RADAR_UNSUPPORTED_SHAPE;
     a.scale_log2 = (d->softmax_scale != 0.f ? d->softmax_scale : 1.0f / sqrtf((float)D)) * kqLog2e;
     a.workgroups = p.workgroups; a.least = p.least; a.shift = p.shift; a.max_cgs = p.max_cgs;
+    a.unit_cost = p.unit_cost; a.whole = p.whole;
     char *ws = static_cast<char *>(workspace);
     a.unit_tab = reinterpret_cast<uint32_t *>(ws + p.off_tab);
     a.part = reinterpret_cast<float *>(ws + p.off_part);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const hipError_t e = D == 128 ? (p.nc == 1 ? launch_kvq<128, 1>(a, p, s) : p.nc == 2 ? launch_kvq<128, 2>(a, p, s) : launch_kvq<128, 4>(a, p, s))
-                                  : (p.nc == 1 ? launch_kvq<64, 1>(a, p, s) : p.nc == 2 ? launch_kvq<64, 2>(a, p, s) : launch_kvq<64, 4>(a, p, s));
+    const bool far = (int64_t)a.n_blocks * a.block_bytes > UINT32_MAX;
+    auto go = [&](auto near_kernel, auto far_kernel) { return far ? far_kernel(a, p, s) : near_kernel(a, p, s); };
+    const hipError_t e = D == 128 ? (p.nc == 1   ? go(launch_kvq<128, 1, false>, launch_kvq<128, 1, true>)
+                                     : p.nc == 2 ? go(launch_kvq<128, 2, false>, launch_kvq<128, 2, true>)
+                                                 : go(launch_kvq<128, 4, false>, launch_kvq<128, 4, true>))
+                                  : (p.nc == 1   ? go(launch_kvq<64, 1, false>, launch_kvq<64, 1, true>)
+                                     : p.nc == 2 ? go(launch_kvq<64, 2, false>, launch_kvq<64, 2, true>)
+                                                 : go(launch_kvq<64, 4, false>, launch_kvq<64, 4, true>));
     return e == hipSuccess ? RADAR_OK : RADAR_HIP_ERROR;
 }
