@@ -9,6 +9,8 @@
 // products as they lie.  A lane of the V operand holds eight keys of one d, and the layout puts the codes of eight keys for the
 // same eight d side by side: 32 bytes are the operands of eight products.
 #include <algorithm>
+#include <cmath>
+#include <type_traits>
 
 #include "radar_host.h"
 #include "radar_kvq.h"
@@ -35,7 +37,7 @@ struct KqArgs {
     float scale_log2;
     int64_t block_bytes;                       // of a block, all heads
     int workgroups, least, shift, max_cgs;     // least share of the line; log2 steps per unit of it; column blocks of a KV head
-    int unit_cost, whole;                      // what a unit costs besides its steps; whole: units are not divided, and all alike
+    int unit_cost, whole;                      // what a unit costs besides its steps; whole: a workgroup for each unit, no line
     float *part;                               // [2 * workgroups] partial results: outputs, maxima (log2 units), sums, in fp32
     uint32_t *unit_tab;                        // first and last workgroup of a unit; alike: it is written already
 };
@@ -227,7 +229,7 @@ struct KqShape {
     static constexpr int ROW = DP + 4;                               // of the merge's buffer: rows 16 bytes apart from a multiple of the banks
     static constexpr int q_bytes() { return COLS * D * 2; }
     static constexpr int merge_bytes() { return kKqWaves * COLS * ROW * 4; }
-    static constexpr int lds_bytes() { return merge_bytes() + (kKqWaves + 2) * COLS * 8 + kKqWaves * 64 + (NC > 2 ? q_bytes() : 0); }
+    static constexpr int lds_bytes() { return merge_bytes() + (kKqWaves + 2) * COLS * 8 + kKqWaves * 64 + q_bytes(); }
     static constexpr int PART = COLS * D + 2 * COLS;                 // floats of a partial result: outputs, maxima, sums
 };
 
@@ -245,16 +247,22 @@ __device__ __forceinline__ void kq_step(const KqK<D> &k, KqV &v, KqIds id, QOp q
         for (int n = 0; n < NC; ++n) sacc[t][n] = floatx4{0.f, 0.f, 0.f, 0.f};
     const uint32_t pick = 0x0c0c0cu | (uint32_t)(r & 3) << 24;       // that byte on top, zeros under it
     const float f[2] = {__uint_as_float(__builtin_amdgcn_perm(0u, k.scale[0], pick) >> 1), __uint_as_float(__builtin_amdgcn_perm(0u, k.scale[1], pick) >> 1)};
-    // (the queries' operands come from LDS where there are many: asked for AHEAD of them ahead)
+    // (the queries' operands come from LDS where there are many: asked for AHEAD of them ahead; the next codes are turned into
+    // operands between the products of the ones before)
     constexpr int NQ = NC * S::CH;
     bf16x8 q[AHEAD];
 #pragma unroll
     for (int x = 0; x < AHEAD; ++x) q[x] = qop(x % NC, x / NC);
+    uint32_t w[2][2][4];
+    kvq_decode8(k.code[0][0], f[0], w[0][0]);
+    kvq_decode8(k.code[1][0], f[1], w[0][1]);
+    if (NC > 2) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int c = 0; c < S::CH; ++c) {
-        uint32_t w[2][4];
-        kvq_decode8(k.code[0][c], f[0], w[0]);
-        kvq_decode8(k.code[1][c], f[1], w[1]);
+        if (c + 1 < S::CH) {
+            kvq_decode8(k.code[0][c + 1], f[0], w[(c + 1) & 1][0]);
+            kvq_decode8(k.code[1][c + 1], f[1], w[(c + 1) & 1][1]);
+        }
 #pragma unroll
         for (int n = 0; n < NC; ++n) {
             const int x = c * NC + n;
@@ -262,12 +270,24 @@ __device__ __forceinline__ void kq_step(const KqK<D> &k, KqV &v, KqIds id, QOp q
             if (x + AHEAD < NQ) q[x % AHEAD] = qop((x + AHEAD) % NC, (x + AHEAD) / NC);
 #pragma unroll
             for (int t = 0; t < 2; ++t)
-                sacc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{w[t][0], w[t][1], w[t][2], w[t][3]}), cur, sacc[t][n], 0, 0, 0);
-            if (NC > 2) __builtin_amdgcn_sched_barrier(0);
+                sacc[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, u32x4{w[c & 1][t][0], w[c & 1][t][1], w[c & 1][t][2], w[c & 1][t][3]}), cur, sacc[t][n], 0, 0, 0);
+        }
+        if (NC > 2) {
+#pragma unroll
+            for (int n = 0; n < NC; ++n) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    if (c + 1 < S::CH) __builtin_amdgcn_sched_group_barrier(0x002, 1, 0);
+                }
+                if (c * NC + n + AHEAD < NQ) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
     __builtin_amdgcn_sched_barrier(0);         // (the phases stay apart: run into each other they need twice the registers)
     next_k();
+    __builtin_amdgcn_s_setprio(0);
     // this lane's eight keys: 8 * grp + e, e = 4 * tile + register
     uint32_t nan_keys = 0;
     const bool whole = key0 + 32 <= L && kq_there(a, id.a) && kq_there(a, id.b);      // all of it prefix: nothing to mask
@@ -320,6 +340,9 @@ __device__ __forceinline__ void kq_step(const KqK<D> &k, KqV &v, KqIds id, QOp q
         l_run[n] = sum;
         __builtin_amdgcn_sched_barrier(0);
     }
+    // Two wavefronts share a SIMD, and left alone do the same at the same time.  The one that has products goes first, the other one's softmax fills
+    // the gaps (four sequences of 16384 rows, 64 heads: 142 us without, 133 with; taking turns between barriers 146).
+    __builtin_amdgcn_s_setprio(1);
     // V^T operands: product m of lane (r, grp) is d = D/16 * r + m, keys 8 * grp + 0..7; a byte of the codes has two products' values
     float fv[8];
 #pragma unroll
@@ -328,29 +351,41 @@ __device__ __forceinline__ void kq_step(const KqK<D> &k, KqV &v, KqIds id, QOp q
 #pragma unroll
         for (int e = 0; e < 8; ++e) v.code[e] >>= 16 * (r & 1);
     }
-#pragma unroll
-    for (int j = 0; j < S::NM / 2; ++j) {
-        uint32_t lo[4], hi[4];
+    u32x4 vop[2][2];
+    auto decode = [&](auto byte, u32x4 (&to)[2]) {
+        constexpr int J = decltype(byte)::value;
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
-            uint32_t x, y;
-            if (j == 0) { x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v.code[e], fv[e], 0));
-                          y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v.code[e + 1], fv[e + 1], 0)); }
-            else if (j == 1) { x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v.code[e], fv[e], 1));
-                               y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v.code[e + 1], fv[e + 1], 1)); }
-            else if (j == 2) { x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v.code[e], fv[e], 2));
-                               y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v.code[e + 1], fv[e + 1], 2)); }
-            else { x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v.code[e], fv[e], 3));
-                   y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v.code[e + 1], fv[e + 1], 3)); }
-            lo[e >> 1] = __builtin_amdgcn_perm(y, x, 0x05040100u);
-            hi[e >> 1] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+            const uint32_t x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v.code[e], fv[e], J));
+            const uint32_t y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v.code[e + 1], fv[e + 1], J));
+            to[0][e >> 1] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+            to[1][e >> 1] = __builtin_amdgcn_perm(y, x, 0x07060302u);
         }
-        const bf16x8 v0 = __builtin_bit_cast(bf16x8, u32x4{lo[0], lo[1], lo[2], lo[3]}), v1 = __builtin_bit_cast(bf16x8, u32x4{hi[0], hi[1], hi[2], hi[3]});
+    };
+    decode(std::integral_constant<int, 0>{}, vop[0]);
+    if (NC > 2) __builtin_amdgcn_sched_barrier(0);
+    auto outputs = [&](auto byte) {
+        constexpr int J = decltype(byte)::value, LAST = S::NM / 2 - 1;
+        if constexpr (J < LAST) decode(std::integral_constant<int, J + 1>{}, vop[(J + 1) & 1]);
 #pragma unroll
-        for (int n = 0; n < NC; ++n) oacc[2 * j][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, p[n], oacc[2 * j][n], 0, 0, 0);
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int n = 0; n < NC; ++n) oacc[2 * j + 1][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, p[n], oacc[2 * j + 1][n], 0, 0, 0);
+            for (int n = 0; n < NC; ++n)
+                oacc[2 * J + x][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vop[J & 1][x]), p[n], oacc[2 * J + x][n], 0, 0, 0);
+        if (NC > 2) {
+#pragma unroll
+            for (int x = 0; x < 2 * NC; ++x) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                if (J < LAST) __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
+            }
+        }
         __builtin_amdgcn_sched_barrier(0);
+    };
+    outputs(std::integral_constant<int, 0>{});
+    outputs(std::integral_constant<int, 1>{});
+    if constexpr (S::NM > 4) {
+        outputs(std::integral_constant<int, 2>{});
+        outputs(std::integral_constant<int, 3>{});
     }
     if (!whole && __ballot(nan_keys != 0) != 0ull) {
         int lane2 = lane;
@@ -379,8 +414,11 @@ struct KqChunkPlan {                           // lane = sequence b0 + lane; the
     uint32_t len, start;                       // of a unit; where the sequence begins on the line
 };
 
-// workgroups: a multiple of eight
-__device__ __forceinline__ int kq_number(const KqArgs &a) { return (int)(blockIdx.x & 7) * (a.workgroups >> 3) + (int)(blockIdx.x >> 3); }
+// The share that a workgroup takes, of n; n: it takes none.  An XCD takes shares that follow each other, every XCD as many.
+__device__ __forceinline__ uint32_t kq_share_of(uint32_t n) {
+    const uint32_t each = (n + 7) >> 3, i = blockIdx.x >> 3;
+    return i < each ? min((blockIdx.x & 7) * each + i, n) : n;
+}
 
 template <int NC>
 __device__ __forceinline__ void kq_plan_chunk(KqChunkPlan &c, const KqArgs &a, int b0, uint32_t base) {
@@ -390,7 +428,7 @@ __device__ __forceinline__ void kq_plan_chunk(KqChunkPlan &c, const KqArgs &a, i
     c.L = s.L; c.nn = s.nn; c.total = s.total;
     c.cgs = (s.nn * a.G + 16 * NC - 1) / (16 * NC);
     const int steps = (s.total + 31) >> 5;
-    c.len = a.whole ? 1u : (uint32_t)((steps + (1 << a.shift) - 1) >> a.shift) + (uint32_t)a.unit_cost;
+    c.len = (uint32_t)((steps + (1 << a.shift) - 1) >> a.shift) + (uint32_t)a.unit_cost;
     const uint32_t mine = b0 + lane < a.B && s.nn > 0 ? c.len * (uint32_t)(a.Hkv * c.cgs) : 0u;
     if (mine == 0) c.len = 0;
     const uint32_t incl = wave_scan_u32(mine);
@@ -399,7 +437,7 @@ __device__ __forceinline__ void kq_plan_chunk(KqChunkPlan &c, const KqArgs &a, i
 }
 
 // A workgroup's place on the line and its piece, which wait in LDS (every wavefront has its own copy) while the loop needs the scalar registers.
-struct KqPlace { uint32_t pos, end, share; int b0; uint32_t base; };
+struct KqPlace { uint32_t pos, end, share; int b0; uint32_t base, number; };       // number: of its share
 struct KqPiece { int b, hk, cg, nn, slot, L, total, s0, s1; };       // slot: of its partial result, -1: it is all of its unit
 constexpr int kKqState = 16;                   // words of a wavefront's copy: the place, then the piece
 template <typename T>
@@ -462,8 +500,28 @@ __global__ __launch_bounds__(kKqThreads, NC == 1 ? 4 : 2) void kvq_attn_kernel(K
     const int lane = lane_id(), w = __builtin_amdgcn_readfirstlane(wave_id()), r = lane & 15, grp = lane >> 4;
     int *const state = s_state + w * kKqState;
 
+    // A workgroup for each unit: nothing to work out but which, and the only sequence's lengths.
+    auto whole_piece = [&]() -> bool {
+        const KqArgs a = kq_args_plan();
+        const uint32_t units = (uint32_t)(a.B * a.Hkv * a.max_cgs), u = kq_share_of(units);
+        if (u >= units) return false;
+        KqPiece p;
+        const uint32_t bh = u / (uint32_t)a.max_cgs;
+        p.cg = (int)__builtin_amdgcn_readfirstlane(u - bh * (uint32_t)a.max_cgs);
+        p.b = (int)__builtin_amdgcn_readfirstlane(bh / (uint32_t)a.Hkv);
+        p.hk = (int)__builtin_amdgcn_readfirstlane(bh) - p.b * a.Hkv;
+        p.L = min(uniform_word(a.ctx_lens, p.b), a.S);               // (kq_seq)
+        p.nn = a.n_nodes ? max(1, min(uniform_word(a.n_nodes, p.b), a.T)) : a.T;
+        if (p.L < 0) p.nn = 0;
+        p.total = p.L < 0 ? 0 : min(p.L + p.nn, a.S);
+        p.s0 = 0;
+        p.s1 = p.cg * S::COLS < p.nn * a.G ? (p.total + 31) >> 5 : 0;
+        p.slot = -1;
+        kq_remember(state + sizeof(KqPlace) / 4, p);
+        return true;
+    };
     // the line's length, and this workgroup's share of it
-    {
+    auto plan = [&] {
         const KqArgs a = kq_args_plan();
         KqChunkPlan c;
         uint32_t line = 0;
@@ -472,47 +530,51 @@ __global__ __launch_bounds__(kKqThreads, NC == 1 ? 4 : 2) void kvq_attn_kernel(K
             line = c.end;
         }
         const uint32_t share = max((line + a.workgroups - 1) / a.workgroups, (uint32_t)a.least);
-        const uint32_t pos = min((uint64_t)kq_number(a) * share, (uint64_t)line);
-        kq_remember(state, KqPlace{pos, (uint32_t)min((uint64_t)pos + share, (uint64_t)line), share, 0, 0});
-    }
+        const uint32_t pos = min((uint64_t)kq_share_of((line + share - 1) / share) * share, (uint64_t)line);
+        kq_remember(state, KqPlace{pos, (uint32_t)min((uint64_t)pos + share, (uint64_t)line), share, 0, 0, pos / share});
+    };
     auto next_piece = [&]() -> bool {                                // all values the same in every lane
-        const KqArgs a = kq_args_plan();
         KqPlace x = kq_recall<KqPlace>(state);
         if (x.pos >= x.end) return false;
+        const KqArgs a = kq_args_plan();
+        const uint32_t cost = (uint32_t)a.unit_cost;
         KqChunkPlan c;
         kq_plan_chunk<NC>(c, a, x.b0, x.base);
-        while (x.pos >= c.end) kq_plan_chunk<NC>(c, a, c.b0 + kWave, c.end);
-        x.b0 = c.b0; x.base = c.base;
-        const uint64_t before = __ballot(c.len > 0 && c.start <= x.pos);
-        const int q = 63 - __clzll((long long)before);
-        const uint32_t len = readlane_u32(c.len, q), first = readlane_u32(c.start, q);
-        const uint32_t u = __builtin_amdgcn_readfirstlane((x.pos - first) / len), at = first + u * len;      // (a quotient comes out of vector registers)
-        const int cgs = (int)readlane_u32((uint32_t)c.cgs, q), wg = kq_number(a);
-        KqPiece p;
-        p.b = c.b0 + q;
-        p.hk = __builtin_amdgcn_readfirstlane((int)u / cgs);
-        p.cg = (int)u - p.hk * cgs;
-        p.L = (int)readlane_u32((uint32_t)c.L, q);
-        p.nn = (int)readlane_u32((uint32_t)c.nn, q);
-        p.total = (int)readlane_u32((uint32_t)c.total, q);
-        const int steps = (p.total + 31) >> 5;
-        const uint32_t from = x.pos - at, to = min(x.end - at, len), cost = (uint32_t)a.unit_cost;
-        if (a.whole) {
-            p.s0 = 0; p.s1 = steps;
-        } else {
+        while (x.pos < x.end) {
+            while (x.pos >= c.end) kq_plan_chunk<NC>(c, a, c.b0 + kWave, c.end);
+            const uint64_t before = __ballot(c.len > 0 && c.start <= x.pos);
+            const int q = 63 - __clzll((long long)before);
+            const uint32_t len = readlane_u32(c.len, q), first = readlane_u32(c.start, q);
+            const uint32_t u = __builtin_amdgcn_readfirstlane((x.pos - first) / len), at = first + u * len;  // (a quotient comes out of vector registers)
+            const uint32_t from = x.pos - at, to = min(x.end - at, len);
+            x.pos = at + to;
+            if (to <= cost) continue;                                // (of the unit's own cost nobody has anything to do)
+            const int cgs = (int)readlane_u32((uint32_t)c.cgs, q);
+            KqPiece p;
+            p.b = c.b0 + q;
+            p.hk = __builtin_amdgcn_readfirstlane((int)u / cgs);
+            p.cg = (int)u - p.hk * cgs;
+            p.L = (int)readlane_u32((uint32_t)c.L, q);
+            p.nn = (int)readlane_u32((uint32_t)c.nn, q);
+            p.total = (int)readlane_u32((uint32_t)c.total, q);
+            const int steps = (p.total + 31) >> 5;
             p.s0 = min((int)(from > cost ? (from - cost) << a.shift : 0u), steps);
-            p.s1 = min((int)(to > cost ? (to - cost) << a.shift : 0u), steps);
+            p.s1 = min((int)((to - cost) << a.shift), steps);
+            p.slot = from <= cost && to == len ? -1 : 2 * (int)x.number + (to < len ? 1 : 0);
+            if (from <= cost && threadIdx.x == 0)       // for the merge: first and last workgroup
+                a.unit_tab[(p.b * a.Hkv + p.hk) * a.max_cgs + p.cg] = p.slot < 0 ? 0u : x.number << 16 | ((at + len - 1) / x.share);
+            x.b0 = c.b0; x.base = c.base;
+            kq_remember(state, x);
+            kq_remember(state + sizeof(KqPlace) / 4, p);
+            return true;
         }
-        p.slot = from == 0 && to == len ? -1 : 2 * wg + (to < len ? 1 : 0);
-        if (from == 0 && threadIdx.x == 0)                           // for the merge: first and last workgroup
-            a.unit_tab[(p.b * a.Hkv + p.hk) * a.max_cgs + p.cg] = p.slot < 0 ? 0u : (uint32_t)wg << 16 | ((at + len - 1) / x.share);
-        x.pos = at + to;
-        kq_remember(state, x);
-        kq_remember(state + sizeof(KqPlace) / 4, p);
-        return true;
+        return false;
     };
 
-    while (next_piece()) {
+    const bool whole = args_from_here<KqArgs>(0)->whole != 0;
+    if (!whole) plan();
+    for (bool more = true; more; more = !whole) {
+        if (!(whole ? whole_piece() : next_piece())) break;
         KqPiece p = kq_recall<KqPiece>(state + sizeof(KqPlace) / 4);
         KqArgs a = kq_args_loop();
         // (the same in every lane, which the compiler does not see behind the search for the piece)
@@ -520,16 +582,24 @@ __global__ __launch_bounds__(kKqThreads, NC == 1 ? 4 : 2) void kvq_attn_kernel(K
         const kq_bytes base = (kq_bytes)(uintptr_t)kq_scalar(a.cache + (size_t)p.hk * KvqChunk<D>::bytes(1 << a.rbits));
         const int mine = p.s0 + w;
         const bool active = mine < p.s1;
-        // the first step's loads, before the queries
-        KqK<D> k;
-        KqV v;
-        KqIds id{0, 0}, nid{0, 0};
+        // the first steps' loads, before the queries
+        constexpr int DEEP = NC > 2 || (NC == 1 && FAR) ? 1 : 2;                         // steps that the loads are ahead, two where the registers allow
+        KqK<D> k[DEEP];
+        KqV v[DEEP];
+        KqIds id[DEEP], nid{0, 0};
         if (active) {
-            id = kq_ids(a, table, mine * 32, p.total);
-            nid = kq_ids(a, table, min(mine + kKqWaves, p.s1 - 1) * 32, p.total);
-            const KqBase at = kq_base<D>(a, base, id, mine * 32);
-            kq_load_k<D, FAR>(k, at);
-            kq_load_v<D, FAR>(v, a, at);
+#pragma unroll
+            for (int x = 0; x < DEEP; ++x) {
+                const int s = min(mine + x * kKqWaves, p.s1 - 1);
+                id[x] = kq_ids(a, table, s * 32, p.total);
+            }
+            nid = kq_ids(a, table, min(mine + DEEP * kKqWaves, p.s1 - 1) * 32, p.total);
+#pragma unroll
+            for (int x = 0; x < DEEP; ++x) {
+                const KqBase at = kq_base<D>(a, base, id[x], min(mine + x * kKqWaves, p.s1 - 1) * 32);
+                kq_load_k<D, FAR>(k[x], at);
+                kq_load_v<D, FAR>(v[x], a, at);
+            }
         }
         // this lane's columns: their queries' operands (d = D/4 * grp + 8 * c + 0..7) and ancestors
         const KqArgs aq = kq_args_query();
@@ -540,15 +610,7 @@ __global__ __launch_bounds__(kKqThreads, NC == 1 ? 4 : 2) void kvq_attn_kernel(K
             if (i < p.nn) x = *reinterpret_cast<const u32x4 *>(a.q + (size_t)p.b * a.q_sb + (size_t)i * a.q_st + (size_t)(p.hk * a.G + col - i * a.G) * a.q_sh + (D / 4) * grp + 8 * ch);
             return x;
         };
-        bf16x8 q_regs[NC > 2 ? 1 : NC][S::CH];
-        if constexpr (NC > 2) {
-            for (int x = w; x < NC * S::CH; x += kKqWaves) s_q[x * kWave + lane] = query(x / S::CH, x % S::CH);
-        } else {
-#pragma unroll
-            for (int n = 0; n < NC; ++n)
-#pragma unroll
-                for (int ch = 0; ch < S::CH; ++ch) q_regs[n][ch] = __builtin_bit_cast(bf16x8, query(n, ch));
-        }
+        for (int x = w; x < NC * S::CH; x += kKqWaves) s_q[x * kWave + lane] = query(x / S::CH, x % S::CH);
         if (w < NC && p.s1 * 32 > p.L) {
             const uint64_t words = kq_ancestors(aq.parents ? aq.parents + (size_t)p.b * aq.T : nullptr, p.nn);
             const int i = ((p.cg * NC + w) * 16 + r) / aq.G, ii = min(i, RADAR_T_MAX - 1);
@@ -565,25 +627,29 @@ __global__ __launch_bounds__(kKqThreads, NC == 1 ? 4 : 2) void kvq_attn_kernel(K
             for (int m = 0; m < S::NM; ++m) oacc[m][n] = floatx4{0.f, 0.f, 0.f, 0.f};
         }
         __syncthreads();
-        auto qop = [&](int n, int ch) {
-            if constexpr (NC > 2) return __builtin_bit_cast(bf16x8, s_q[(n * S::CH + ch) * kWave + lane]);
-            else return q_regs[n][ch];
+        auto qop = [&](int n, int ch) { return __builtin_bit_cast(bf16x8, s_q[(n * S::CH + ch) * kWave + lane]); };
+        const int last = p.s1 - 1;                                   // (past it, rows that are there are asked for once more, in vain)
+        auto step = [&](int s, int set) __attribute__((always_inline)) {
+            const int next = min(s + DEEP * kKqWaves, last);
+            KqIds nnid;
+            kq_step<D, NC, FAR || NC == 1 ? 2 : 4>(k[set], v[set], id[set], qop, [&] {
+                nnid = kq_ids(a, table, min(s + (DEEP + 1) * kKqWaves, last) * 32, p.total);
+                kq_load_k<D, FAR>(k[set], kq_base<D>(a, base, nid, next * 32));
+            }, oacc, negref, l_run, s_anc, a, s * 32, p.L, p.total);
+            kq_load_v<D, FAR>(v[set], a, kq_base<D>(a, base, nid, next * 32));
+            id[set] = nid;
+            nid = nnid;
         };
-        if (active)
-            for (int s = mine; s < p.s1; s += kKqWaves) {
-                // Two wavefronts share a SIMD, w and w + 4, which left alone lets the older one have its way: they are favoured in turn.
-                if (((s >> 3) ^ (w >> 2)) & 1) __builtin_amdgcn_s_setprio(1); else __builtin_amdgcn_s_setprio(0);
-                const int next = min(s + kKqWaves, p.s1 - 1);        // (the last step asks for rows that are there, in vain)
-                KqIds nnid;
-                kq_step<D, NC, NC <= 2 ? NC * S::CH : FAR ? 2 : 4>(k, v, id, qop, [&] {
-                    nnid = kq_ids(a, table, min(s + 2 * kKqWaves, p.s1 - 1) * 32, p.total);
-                    kq_load_k<D, FAR>(k, kq_base<D>(a, base, nid, next * 32));
-                }, oacc, negref, l_run, s_anc, a, s * 32, p.L, p.total);
-                kq_load_v<D, FAR>(v, a, kq_base<D>(a, base, nid, next * 32));
-                id = nid;
-                nid = nnid;
+        if constexpr (DEEP == 2) {
+            int s = mine;
+            for (; s + kKqWaves < p.s1; s += 2 * kKqWaves) {
+                step(s, 0);
+                step(s + kKqWaves, 1);
             }
-
+            if (s < p.s1) step(s, 0);
+        } else {
+            for (int s = mine; s < p.s1; s += kKqWaves) step(s, 0);
+        }
         __builtin_amdgcn_s_setprio(0);
         // the wavefronts' results, added up against their common reference
         a = kq_args_end();
@@ -632,7 +698,14 @@ __global__ __launch_bounds__(kKqThreads, NC == 1 ? 4 : 2) void kvq_attn_kernel(K
             int lane2 = threadIdx.x;
             asm volatile("" : "+v"(lane2));
             const int mc = lane2 / TPC, mx = lane2 % TPC * 4, gc = p.cg * S::COLS + mc, mi = gc / a.G, mh = p.hk * a.G + gc - mi * a.G;
-            if (mc < S::COLS && (p.slot >= 0 || mi < p.nn)) {
+            if (whole && mc < S::COLS && mi >= p.nn && mi < a.T) {   // rows behind the tree's end: zeros
+#pragma unroll
+                for (int z = 0; z < IPT; ++z) {
+                    const int x = z * TPC * 4 + mx, d = D / 4 * (x / (S::EP * S::NM)) + pass * S::EP * S::NM + x % (S::EP * S::NM);
+                    *reinterpret_cast<u32x2 *>(a.out + (size_t)p.b * a.o_sb + (size_t)mi * a.o_st + (size_t)mh * a.o_sh + d) = u32x2{0, 0};
+                    if (a.lse && d == 0) a.lse[((size_t)p.b * a.T + mi) * a.Hq + mh] = 0.f;
+                }
+            } else if (mc < S::COLS && (p.slot >= 0 || mi < p.nn)) {
                 const float M = s_M[mc], l = s_L[mc];
                 floatx4 o[IPT][kKqWaves];
 #pragma unroll
@@ -658,6 +731,7 @@ __global__ __launch_bounds__(kKqThreads, NC == 1 ? 4 : 2) void kvq_attn_kernel(K
         __syncthreads();
     }
 
+    if (whole) return;
     // rows behind a tree's end, and of sequences that are not there: zeros (a lane looks at one row, the wavefront fills those that are found)
     const KqArgs a = kq_args_end();
     const int rows = a.B * a.T, step = a.workgroups * kKqWaves;
@@ -717,6 +791,8 @@ static radar_status check_kvq_attn(const radar_kvq_attn_desc *d) {
     if (d->rows_per_split < 0 || d->rows_per_split % 64 != 0) return RADAR_INVALID_ARG;
     if (!(d->softmax_scale >= 0.f)) return RADAR_INVALID_ARG;
     if (d->T_max > RADAR_T_MAX || d->B > 65535 || d->Hq > 65535 || d->S_max > INT32_MAX - 4096) return RADAR_UNSUPPORTED_SHAPE;
+    // units of 16 columns are counted in 32 bits
+    if ((int64_t)d->B * d->cache.Hkv * ((d->Hq / d->cache.Hkv * d->T_max + 15) / 16) > (1 << 30)) return RADAR_UNSUPPORTED_SHAPE;
     return RADAR_OK;
 }
 
@@ -729,22 +805,43 @@ struct KqPlan {
 static KqPlan plan_kvq(const radar_kvq_attn_desc *d) {
     KqPlan p;
     const int cols = d->Hq / d->cache.Hkv * d->T_max, D = d->cache.D;
-    p.nc = cols <= 16 ? 1 : cols <= 32 ? 2 : 4;
+    const int64_t steps = ((int64_t)d->S_max + 31) / 32;
+    // Columns a workgroup, and whole units or divided ones: whichever takes less, from what rounds of steps and the rest took (us, one MI355X, D = 128,
+    // beside the 6 of any call).  Divided units cost 13 more, a second launch and two pieces a workgroup, and pay for sequences that differ (the host
+    // knows the longest only; half of it is taken for the others).  60 tree rows, 32 heads on 8, us with 16 / 32 / 64 columns:
+    //                              whole             divided
+    //   3000 rows            18  21  30        23  21  24
+    //   12000 rows           49  56  83        38  34  37
+    //   4 of 2000 rows       23  19  25        33  23  33
+    //   16 of 250 .. 2048    73  63  49        68  63  58
+    //   16 of 500 .. 5000                     108  97  79
+    // The choice was the quickest or within 2% of it in 19 of 20 such shapes; the worst, two sequences of 9000 rows with 64 heads, 62 us for 50.
+    p.whole = false;
+    double best = 1e300;
+    const double rounds = (double)((steps + 7) / 8);
+    for (int i = 0; i < 6; ++i) {
+        const int x = i >> 1, nc = 1 << x;
+        const bool whole = i & 1;
+        if ((nc > 1 && cols <= 8 * nc) || (whole && d->rows_per_split != 0)) continue;
+        const double units = (double)d->B * d->cache.Hkv * ((cols + 16 * nc - 1) / (16 * nc));
+        const double alone[] = {0.91, 1.05, 1.7}, shared[] = {0.8, 1.27, 2.2}, end[] = {0.0, 2.3, 4.0}, divided[] = {13.2, 12.7, 16.0};
+        const double us = whole ? std::ceil(units / 256.0) * (rounds * alone[x] + end[x])
+                                : divided[x] + units / 256.0 * ((d->B > 1 ? 0.5 : 1.0) * rounds * shared[x] + 3.0 + end[x]);
+        if (us < best) { best = us; p.nc = nc; p.whole = whole; }
+    }
     p.max_cgs = (cols + 16 * p.nc - 1) / (16 * p.nc);
-    p.workgroups = p.nc == 1 ? 512 : 256;                  // what the chip holds at once
-    const int64_t units = (int64_t)d->B * d->cache.Hkv * p.max_cgs, steps = ((int64_t)d->S_max + 31) / 32;
+    const int64_t units = (int64_t)d->B * d->cache.Hkv * p.max_cgs;
+    p.workgroups = p.whole ? (int)((units + 7) / 8 * 8) : p.nc == 1 ? 512 : 256;             // or what the chip holds at once
     p.least = d->rows_per_split ? d->rows_per_split / 32 : 8;
     p.unit_cost = p.nc == 1 ? 16 : 24;
-    p.whole = d->rows_per_split == 0 && steps <= 24;
-    if (p.whole) p.least = 1;
     // positions on the line stay within 31 bits
     p.shift = 0;
     while (units * ((steps >> p.shift) + 1 + p.unit_cost) >= (int64_t(1) << 31) && p.shift < 31) ++p.shift;
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t o = off; off += (bytes + 255) & ~size_t(255); return o; };
     take(256);                                             // never empty: callers always pass a workspace
-    p.off_tab = take((size_t)units * sizeof(uint32_t));
-    p.off_part = take((size_t)2 * p.workgroups * (16 * p.nc * (D + 2)) * sizeof(float));
+    p.off_tab = take(p.whole ? 0 : (size_t)units * sizeof(uint32_t));
+    p.off_part = take(p.whole ? 0 : (size_t)2 * p.workgroups * (16 * p.nc * (D + 2)) * sizeof(float));
     p.bytes = off;
     return p;
 }
@@ -792,7 +889,6 @@ extern "C" radar_status radar_tree_attention_kvq(const void *q, const void *cach
     const uintptr_t al = (uintptr_t)q | (uintptr_t)cache | (uintptr_t)out;
     const int64_t strides = a.q_sh | a.q_st | a.q_sb | a.o_sh | a.o_st | a.o_sb;
     if ((al & 15) != 0 || (strides & 7) != 0 || strides < 0) return RADAR_INVALID_ARG;
-    if ((int64_t)d->B * d->cache.Hkv * p.max_cgs > INT32_MAX || (int64_t)d->B * d->T_max > INT32_MAX) return RADAR_UNSUPPORTED_SHAPE;
     a.scale_log2 = (d->softmax_scale != 0.f ? d->softmax_scale : 1.0f / sqrtf((float)D)) * kqLog2e;
     a.workgroups = p.workgroups; a.least = p.least; a.shift = p.shift; a.max_cgs = p.max_cgs;
     a.unit_cost = p.unit_cost; a.whole = p.whole;
