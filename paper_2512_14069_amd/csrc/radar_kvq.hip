@@ -145,11 +145,11 @@ __global__ __launch_bounds__(256) void kvq_slots_kernel(BlArgs a) {
 
 // ===================================================================== rows into the cache and out of it
 // Eight rows of the input and one head take 2 * D lanes: the first half of them K, the other V, a lane eight values (16
-// bytes of bf16, 4 of codes).  Lanes of K go along the rows, whose codes lie in one piece; lanes of V go down the eight
-// rows, whose codes of the same eight values lie side by side: where the rows follow each other in the cache
-// (prompts, trees) both store whole lines.  The largest magnitude of 32 values is that of four lanes, found on their bit
-// patterns (larger than 0x7f7f: not a number or infinite).
-constexpr int kRwThreads = 256;
+// bytes of bf16, 4 of codes).  All go along the rows where they touch values, and so do lanes of K at the codes, which lie in one piece; there lanes
+// of V go down the eight rows, whose codes of the same eight values lie side by side: where the rows follow each other in the cache (prompts, trees)
+// all store and load whole lines.  A word and a scale change lanes between the two orders.  The largest magnitude of 32 values is that of four lanes,
+// found on their bit patterns (larger than 0x7f7f: not a number or infinite).
+constexpr int kRwThreads = 256, kRwGroups = 2048, kRwLayers = 4;
 
 struct RwArgs {
     const __bf16 *k, *v;                       // append: rows in;
@@ -157,7 +157,7 @@ struct RwArgs {
     const int32_t *slots;
     unsigned char *cache;
     int64_t N, stride_n, stride_h, layer_stride, total;   // total: slots of the cache
-    int rbits, Hkv;
+    int rbits, Hkv, layers, per;               // read: layers, and those of a workgroup
 };
 
 template <int D>
@@ -166,84 +166,102 @@ struct RwLane {                                // which eight values a lane has
     int h, row8, piece;
     bool is_v;
 };
+// down: a wavefront's lanes of V go down the rows, as the codes lie; otherwise along them, as the values do.
 template <int D>
-__device__ __forceinline__ RwLane<D> rw_lane(int Hkv) {
+__device__ __forceinline__ RwLane<D> rw_lane(int Hkv, bool down) {
     constexpr int P = D / 8, HALF = 8 * P;     // lanes of K, of V
-    const int64_t unit = (int64_t)blockIdx.x * (kRwThreads / (2 * HALF)) + threadIdx.x / (2 * HALF);
+    const uint32_t unit = blockIdx.x * (kRwThreads / (2 * HALF)) + threadIdx.x / (2 * HALF), group = unit / (uint32_t)Hkv;      // (the grid is at most 2^31)
     const int l = threadIdx.x % (2 * HALF), l2 = l % HALF;
     RwLane<D> r;
     r.is_v = l >= HALF;
-    r.row8 = r.is_v ? l2 % 8 : l2 / P;
-    r.piece = r.is_v ? l2 / 8 : l2 % P;
-    r.h = (int)(unit % Hkv);
-    r.n = unit / Hkv * 8 + r.row8;
+    r.row8 = !r.is_v ? l2 / P : down ? l2 % 8 : l2 % 64 / 8;
+    r.piece = !r.is_v ? l2 % P : l2 / 64 * 8 + (down ? l2 % 64 / 8 : l2 % 8);
+    r.h = (int)(unit - group * (uint32_t)Hkv);
+    r.n = (int64_t)group * 8 + r.row8;
     return r;
+}
+// What the lane has that is this one's counterpart in the other order (K: itself).
+__device__ __forceinline__ uint32_t rw_turned(bool is_v, uint32_t x) {
+    const int l = lane_id();
+    return (uint32_t)__shfl((int)x, is_v ? l % 8 * 8 + l / 8 : l);
 }
 
 template <int D>
 __global__ __launch_bounds__(kRwThreads) void kvq_append_kernel(RwArgs a) {
     using C = KvqChunk<D>;
-    const RwLane<D> r = rw_lane<D>(a.Hkv);
-    const int64_t n = min(r.n, a.N - 1);       // (lanes past the end go along: the maximum is taken over whole wavefronts)
-    const int slot = a.slots[n];
-    const u32x4 x = *reinterpret_cast<const u32x4 *>((r.is_v ? a.v : a.k) + n * a.stride_n + r.h * a.stride_h + r.piece * 8);
+    const RwLane<D> in = rw_lane<D>(a.Hkv, false), r = rw_lane<D>(a.Hkv, true);
+    const int64_t n = min(in.n, a.N - 1);      // (lanes past the end go along: the maximum is taken over whole wavefronts)
+    const int slot = a.slots[min(r.n, a.N - 1)];
+    const u32x4 x = *reinterpret_cast<const u32x4 *>((in.is_v ? a.v : a.k) + n * a.stride_n + in.h * a.stride_h + in.piece * 8);
     uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) top = max(top, max(x[i] & 0x7fffu, (x[i] >> 16) & 0x7fffu));
-    const int near = r.is_v ? 8 : 1;           // lanes of the same 32 values: next to each other, or eight apart
-    top = max(top, (uint32_t)__shfl_xor((int)top, near));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 2 * near));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 1));             // four neighbours share a scale
+    top = max(top, (uint32_t)__shfl_xor((int)top, 2));
     // amax = (1 + m/128) 2^(E-127): the scale's exponent is E - 127 - 2, or one more from 1.75 on, where 6 would be too little by more than half a step
     const bool sound = top < 0x7f80u;
-    const int byte = min(max((int)(top >> 7) - 2 + ((top & 127u) >= 96u ? 1 : 0), 1), 252);
-    const float scale = kvq_scale((uint32_t)byte);
+    const uint32_t byte = (uint32_t)min(max((int)(top >> 7) - 2 + ((top & 127u) >= 96u ? 1 : 0), 1), 252);
+    const float scale = kvq_scale(byte);
     const uint32_t x0 = x[0], x1 = x[1], x2 = x[2], x3 = x[3];      // (a bit cast of a vector's element would take its first)
     uint32_t w = 0;
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, x0), scale, 0);
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, x1), scale, 1);
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, x2), scale, 2);
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, x3), scale, 3);
+    const uint32_t code = rw_turned(in.is_v, sound ? w : 0u), mark = rw_turned(in.is_v, sound ? byte : (uint32_t)kScaleNaN);
     if (r.n >= a.N || slot < 0 || slot >= a.total) return;
     const int R = 1 << a.rbits, row = slot & (R - 1);
     unsigned char *const chunk = a.cache + ((size_t)(slot >> a.rbits) * a.Hkv + r.h) * C::bytes(R);
-    *reinterpret_cast<uint32_t *>(chunk + (r.is_v ? C::v_piece(R, row, r.piece) : C::k_row(row) + r.piece * 4)) = sound ? w : 0u;
-    if ((r.piece & 3) == 0)
-        chunk[r.is_v ? C::v_scale(R, row, r.piece >> 2) : C::k_scale(R, row, r.piece >> 2)] = (unsigned char)(sound ? byte : kScaleNaN);
+    *reinterpret_cast<uint32_t *>(chunk + (r.is_v ? C::v_piece(R, row, r.piece) : C::k_row(row) + r.piece * 4)) = code;
+    if ((r.piece & 3) == 0) chunk[r.is_v ? C::v_scale(R, row, r.piece >> 2) : C::k_scale(R, row, r.piece >> 2)] = (unsigned char)mark;
 }
 
-template <int D>
+// A workgroup reads its rows in `per` layers, U at a time: where a row is in a layer is worked out once (80 layers of 576 rows of 8 heads, 188 MB of
+// outputs: 53 us with four layers, 66 with one; 8191 rows of one layer 9.2).  The outputs are stored past the caches: kept there they push out what the
+// next kernel needs (a commit after such a read 44 us, 61 with ordinary stores), and the 8191 rows take 10.3 us.
+template <int D, int U>
 __global__ __launch_bounds__(kRwThreads) void kvq_read_kernel(RwArgs a) {
     using C = KvqChunk<D>;
-    const RwLane<D> r = rw_lane<D>(a.Hkv);
-    if (r.n >= a.N) return;
-    const int slot = a.slots[r.n], layer = blockIdx.y;
-    u32x4 out = {0, 0, 0, 0};
-    if (slot >= 0 && slot < a.total) {
-        const int R = 1 << a.rbits, row = slot & (R - 1);
-        const unsigned char *const chunk = a.cache + (size_t)layer * a.layer_stride + ((size_t)(slot >> a.rbits) * a.Hkv + r.h) * C::bytes(R);
-        const uint32_t w = *reinterpret_cast<const uint32_t *>(chunk + (r.is_v ? C::v_piece(R, row, r.piece) : C::k_row(row) + r.piece * 4));
-        const uint32_t byte = chunk[r.is_v ? C::v_scale(R, row, r.piece >> 2) : C::k_scale(R, row, r.piece >> 2)];
-        uint32_t o[4];
-        kvq_decode8(w, kvq_scale(byte), o);
-        out = u32x4{o[0], o[1], o[2], o[3]};
+    const RwLane<D> r = rw_lane<D>(a.Hkv, true), out = rw_lane<D>(a.Hkv, false);
+    const int slot = a.slots[min(r.n, a.N - 1)], first = blockIdx.y * a.per, last = min(first + a.per, a.layers) - 1;
+    const bool there = slot >= 0 && slot < a.total;
+    const int R = 1 << a.rbits, row = there ? slot & (R - 1) : 0;
+    const unsigned char *const chunk = a.cache + ((size_t)(there ? slot >> a.rbits : 0) * a.Hkv + r.h) * C::bytes(R);
+    const unsigned char *const code = chunk + (r.is_v ? C::v_piece(R, row, r.piece) : C::k_row(row) + r.piece * 4);
+    const unsigned char *const scale = chunk + (r.is_v ? C::v_scale(R, row, r.piece >> 2) : C::k_scale(R, row, r.piece >> 2));
+    __bf16 *const to = (r.is_v ? a.v_out : a.k_out) + ((size_t)out.n * a.Hkv + r.h) * D + out.piece * 8;
+    const size_t out_stride = (size_t)a.N * a.Hkv * D;
+    for (int l0 = first; l0 <= last; l0 += U) {
+        uint32_t w[U], byte[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const size_t at = (size_t)min(l0 + u, last) * a.layer_stride;
+            w[u] = there ? *reinterpret_cast<const uint32_t *>(code + at) : 0u;
+            byte[u] = there ? scale[at] : 0u;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (l0 + u > last) break;
+            uint32_t o[4];
+            kvq_decode8(rw_turned(r.is_v, w[u]), kvq_scale(rw_turned(r.is_v, byte[u])), o);
+            if (out.n < a.N) __builtin_nontemporal_store(u32x4{o[0], o[1], o[2], o[3]}, reinterpret_cast<u32x4 *>(to + (size_t)(l0 + u) * out_stride));
+        }
     }
-    __bf16 *const to = (r.is_v ? a.v_out : a.k_out) + (((size_t)layer * a.N + r.n) * a.Hkv + r.h) * D + r.piece * 8;
-    *reinterpret_cast<u32x4 *>(to) = out;
 }
 
 // ===================================================================== the accepted path's rows into place
-// A wavefront takes one (sequence, layer, head) and moves its rows as they are: D/4 words of codes a row, a word a lane,
-// and the scales' bytes.  All of them are read before the first is written, so any path is right; a path of the
-// usual length (up to eight rows, of 60) is four loads deep.  What bounds it is the chain of round trips before the
-// rows themselves: length, path, table.
-constexpr int kCmThreads = 256;
+// Rows move as they are: D/4 words of codes, a word a lane, and the scales' bytes.  A wavefront finds out once where its lanes' words of one
+// sequence's rows come from and go to (length, path, table: a chain of round trips), and then moves them in `per` pairs of layer and head: four at a
+// time for the usual path of at most eight rows, one at a time for longer ones.  All of a pair's rows are read before its first is written, so any
+// path is right.  64 sequences in 80 layers of 8 heads: 44 us (a pair a wavefront, words dealt along the rows: 64); one sequence in 32 layers 4.3.
+constexpr int kCmThreads = 256, kCmWaves = 4096, kCmQuick = 8;
 
 struct CmArgs {
     unsigned char *cache;
     const int32_t *tables, *ctx_lens, *accept_len, *accept_path;
     int32_t *new_ctx;
     int64_t layer_stride;
-    int M, P, rbits, Hkv, units, n_blocks;      // units: layers * Hkv
+    int M, P, rbits, Hkv, units, n_blocks, per;        // units: layers * Hkv; per: of a wavefront
 };
 
 template <int D>
@@ -251,16 +269,19 @@ __global__ __launch_bounds__(kCmThreads) void kvq_commit_kernel(CmArgs a) {
     using C = KvqChunk<D>;
     constexpr int W = D / 4, PER = kWave / W;   // words of codes of a row, K and V; rows that a wavefront's load covers
     constexpr int S = 2 * (D / 32);             // scale bytes of a row
-    const int b = blockIdx.y, unit = blockIdx.x * (kCmThreads / kWave) + wave_id(), lane = lane_id();
+    const int b = blockIdx.y, first = (blockIdx.x * (kCmThreads / kWave) + wave_id()) * a.per, last = min(first + a.per, a.units) - 1, lane = lane_id();
     const int ctx = a.ctx_lens[b];
     const int n = ctx < 0 ? 0 : min(max(a.accept_len[b], 0), a.P - 1);
     if (blockIdx.x == 0 && threadIdx.x == 0 && a.new_ctx) a.new_ctx[b] = ctx < 0 ? ctx : (int)min((int64_t)ctx + n + 1, (int64_t)INT32_MAX);
-    if (n == 0 || unit >= a.units) return;
-    const int R = 1 << a.rbits, layer = unit / a.Hkv, h = unit - layer * a.Hkv;
-    unsigned char *const base = a.cache + (size_t)layer * a.layer_stride + (size_t)h * C::bytes(R);
+    if (n == 0 || first > last) return;
+    const int R = 1 << a.rbits;
     const int64_t rows = (int64_t)a.M << a.rbits;
+    auto base_of = [&](int unit) {
+        const int layer = unit / a.Hkv, h = unit - layer * a.Hkv;
+        return a.cache + (size_t)layer * a.layer_stride + (size_t)h * C::bytes(R);
+    };
 
-    // Lane s knows where row s goes from and to: bytes of the chunk from `base`, and the row in it; from < 0: it stays.
+    // Lane s knows where row s goes from and to: its block's bytes from a layer's first, and the row in it; from < 0: it stays.
     int64_t from = -1, to = -1;
     int from_row = 0, to_row = 0;
     if (lane >= 1 && lane <= n) {
@@ -277,50 +298,100 @@ __global__ __launch_bounds__(kCmThreads) void kvq_commit_kernel(CmArgs a) {
     auto at64 = [](int64_t v, int s) {
         return (int64_t)((uint64_t)(uint32_t)__shfl((int)(uint32_t)v, s) | (uint64_t)(uint32_t)__shfl((int)(uint32_t)((uint64_t)v >> 32), s) << 32);
     };
-    constexpr int ITEMS = RADAR_T_MAX / PER, BYTES = RADAR_T_MAX * S / kWave;
-    uint32_t word[ITEMS];
-    unsigned char scale[BYTES];
     const int wi = lane % W;                    // this lane's word of a row: K's first, then V's eights
     auto code_at = [&](int row) { return wi < W / 2 ? C::k_row(row) + wi * 4 : C::v_piece(R, row, wi - W / 2); };
     const int si = lane % S;
     auto scale_at = [&](int row) { return si < S / 2 ? C::k_scale(R, row, si) : C::v_scale(R, row, si - S / 2); };
+
+    if (n <= kCmQuick) {
+        // Words and rows a load: K's along its rows, V's and the scales down the rows, whose words of the same values are neighbours in the cache.
+        constexpr int KL = D / 64, ITEMS = 2 * KL, U = 4;
+        static_assert(kCmQuick * D / 8 == KL * kWave && kCmQuick * S <= kWave);
+        int64_t src[ITEMS + 1], dst[ITEMS + 1];                      // of this lane's words and its scale, < 0: there is none
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-        word[i] = 0;
-        if (1 + i * PER <= n) {                 // the same in every lane
-            const int s = min(1 + i * PER + lane / W, kWave - 1);
-            const int64_t f = at64(from, s);
-            const int row = __shfl(from_row, s);
-            if (f >= 0) word[i] = *reinterpret_cast<const uint32_t *>(base + f + code_at(row));
+        for (int i = 0; i <= ITEMS; ++i) {
+            const int row = i < KL ? (i * kWave + lane) / (D / 8) : lane % 8;
+            const bool mine = i < ITEMS || lane / 8 < S;
+            src[i] = at64(from, 1 + row); dst[i] = at64(to, 1 + row);              // (lanes behind the path know of no row)
+            const int fr = __shfl(from_row, 1 + row), tr = __shfl(to_row, 1 + row);
+            auto in_chunk = [&](int r) {
+                if (i < KL) return C::k_row(r) + lane % (D / 8) * 4;
+                if (i < ITEMS) return C::v_piece(R, r, (i - KL) * 8 + lane / 8);
+                return lane / 8 < S / 2 ? C::k_scale(R, r, lane / 8) : C::v_scale(R, r, lane / 8 - S / 2);
+            };
+            if (!mine) src[i] = -1;
+            if (src[i] >= 0) { src[i] += in_chunk(fr); dst[i] += in_chunk(tr); }
         }
-    }
+        for (int u0 = first; u0 <= last; u0 += U) {
+            uint32_t word[U][ITEMS];
+            unsigned char scale[U];
 #pragma unroll
-    for (int i = 0; i < BYTES; ++i) {
-        scale[i] = 0;
-        if (1 + i * (kWave / S) <= n) {
-            const int s = min(1 + i * (kWave / S) + lane / S, kWave - 1);
-            const int64_t f = at64(from, s);
-            const int row = __shfl(from_row, s);
-            if (f >= 0) scale[i] = base[f + scale_at(row)];
+            for (int u = 0; u < U; ++u) {
+                const unsigned char *const base = base_of(min(u0 + u, last));
+#pragma unroll
+                for (int i = 0; i < ITEMS; ++i) word[u][i] = src[i] >= 0 ? *reinterpret_cast<const uint32_t *>(base + src[i]) : 0u;
+                scale[u] = src[ITEMS] >= 0 ? base[src[ITEMS]] : (unsigned char)0;
+            }
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // every row has been read
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (u0 + u > last) break;
+                unsigned char *const base = base_of(u0 + u);
+#pragma unroll
+                for (int i = 0; i < ITEMS; ++i)
+                    if (src[i] >= 0) *reinterpret_cast<uint32_t *>(base + dst[i]) = word[u][i];
+                if (src[ITEMS] >= 0) base[dst[ITEMS]] = scale[u];
+            }
         }
+        return;
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");               // every row has been read
+
+    constexpr int ITEMS = RADAR_T_MAX / PER, BYTES = RADAR_T_MAX * S / kWave;
+    for (int unit = first; unit <= last; ++unit) {
+        unsigned char *const base = base_of(unit);
+        int m = n;
+        asm volatile("" : "+v"(m));            // (in each pass anew: what comes of comparing it would be kept for the loop, in more scalars than there are)
+        m = __builtin_amdgcn_readfirstlane(m);
+        uint32_t word[ITEMS];
+        unsigned char scale[BYTES];
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-        if (1 + i * PER <= n) {
-            const int s = 1 + i * PER + lane / W;
-            const int64_t t = at64(to, min(s, kWave - 1));
-            const int row = __shfl(to_row, min(s, kWave - 1));
-            if (s <= n && t >= 0) *reinterpret_cast<uint32_t *>(base + t + code_at(row)) = word[i];
+        for (int i = 0; i < ITEMS; ++i) {
+            word[i] = 0;
+            if (1 + i * PER <= m) {             // the same in every lane
+                const int s = min(1 + i * PER + lane / W, kWave - 1);
+                const int64_t f = at64(from, s);
+                const int row = __shfl(from_row, s);
+                if (f >= 0) word[i] = *reinterpret_cast<const uint32_t *>(base + f + code_at(row));
+            }
         }
-    }
 #pragma unroll
-    for (int i = 0; i < BYTES; ++i) {
-        if (1 + i * (kWave / S) <= n) {
-            const int s = 1 + i * (kWave / S) + lane / S;
-            const int64_t t = at64(to, min(s, kWave - 1));
-            const int row = __shfl(to_row, min(s, kWave - 1));
-            if (s <= n && t >= 0) base[t + scale_at(row)] = scale[i];
+        for (int i = 0; i < BYTES; ++i) {
+            scale[i] = 0;
+            if (1 + i * (kWave / S) <= m) {
+                const int s = min(1 + i * (kWave / S) + lane / S, kWave - 1);
+                const int64_t f = at64(from, s);
+                const int row = __shfl(from_row, s);
+                if (f >= 0) scale[i] = base[f + scale_at(row)];
+            }
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");           // every row has been read
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            if (1 + i * PER <= m) {
+                const int s = 1 + i * PER + lane / W;
+                const int64_t t = at64(to, min(s, kWave - 1));
+                const int row = __shfl(to_row, min(s, kWave - 1));
+                if (s <= m && t >= 0) *reinterpret_cast<uint32_t *>(base + t + code_at(row)) = word[i];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < BYTES; ++i) {
+            if (1 + i * (kWave / S) <= m) {
+                const int s = 1 + i * (kWave / S) + lane / S;
+                const int64_t t = at64(to, min(s, kWave - 1));
+                const int row = __shfl(to_row, min(s, kWave - 1));
+                if (s <= m && t >= 0) base[t + scale_at(row)] = scale[i];
+            }
         }
     }
 }
@@ -408,7 +479,11 @@ extern "C" radar_status radar_kvq_read(const void *cache, const int32_t *slots, 
     if (a.layer_stride < 0) return RADAR_INVALID_ARG;
     if (d->layers > 65535) return RADAR_UNSUPPORTED_SHAPE;
     if (N == 0) return RADAR_OK;
-    const hipError_t e = launch("kvq_read", d->D == 128 ? kvq_read_kernel<128> : kvq_read_kernel<64>, dim3((unsigned)groups, (unsigned)d->layers),
+    // layers a workgroup: up to four, as long as eight workgroups a CU are left
+    a.layers = d->layers;
+    a.per = (int)std::min<int64_t>({std::max<int64_t>(groups * d->layers / kRwGroups, 1), kRwLayers, d->layers});
+    const auto kernel = d->D == 128 ? (a.per > 1 ? kvq_read_kernel<128, 4> : kvq_read_kernel<128, 1>) : a.per > 1 ? kvq_read_kernel<64, 4> : kvq_read_kernel<64, 1>;
+    const hipError_t e = launch("kvq_read", kernel, dim3((unsigned)groups, (unsigned)((d->layers + a.per - 1) / a.per)),
                                 dim3(kRwThreads), 0, static_cast<hipStream_t>(stream), a);
     return e == hipSuccess ? RADAR_OK : RADAR_HIP_ERROR;
 }
@@ -422,11 +497,14 @@ extern "C" radar_status radar_kvq_commit(void *cache, const int32_t *block_table
     if (st != RADAR_OK) return st;
     if (path_len > RADAR_T_MAX || B > 65535) return RADAR_UNSUPPORTED_SHAPE;
     CmArgs a{static_cast<unsigned char *>(cache), block_tables, ctx_lens, accept_len, accept_path, new_ctx_lens, layer_bytes(d),
-             max_blocks, path_len, kvq_log2(d->block_rows), d->Hkv, 0, d->n_blocks};
+             max_blocks, path_len, kvq_log2(d->block_rows), d->Hkv, 0, d->n_blocks, 0};
     if (a.layer_stride < 0) return RADAR_INVALID_ARG;
-    if ((int64_t)d->layers * d->Hkv > INT32_MAX - 4) return RADAR_UNSUPPORTED_SHAPE;
+    if ((int64_t)d->layers * d->Hkv > INT32_MAX - 64) return RADAR_UNSUPPORTED_SHAPE;
     a.units = d->layers * d->Hkv;
-    const dim3 grid((unsigned)((a.units + kCmThreads / kWave - 1) / (kCmThreads / kWave)), (unsigned)B);
+    // pairs a wavefront: as many as leave 16 wavefronts a CU
+    a.per = (int)std::min<int64_t>(std::max<int64_t>((int64_t)a.units * B / kCmWaves, 1), 16);
+    const int per_group = kCmThreads / kWave * a.per;
+    const dim3 grid((unsigned)((a.units + per_group - 1) / per_group), (unsigned)B);
     const hipError_t e = launch("kvq_commit", d->D == 128 ? kvq_commit_kernel<128> : kvq_commit_kernel<64>, grid, dim3(kCmThreads), 0,
                                 static_cast<hipStream_t>(stream), a);
     return e == hipSuccess ? RADAR_OK : RADAR_HIP_ERROR;
