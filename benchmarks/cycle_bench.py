@@ -7,11 +7,15 @@ by call (argument marshalling done beforehand) or as one captured HIP graph, and
 scripted to stop after 2, 4 or all 8 draft calls.  Inputs rotate through several sets (one graph
 per set).  Prints one JSON line per (mode, stop) with the microseconds per cycle.
 
-    python -m benchmarks.cycle_bench [--cycles 300] [--sets 4] [--batch B]
+    python -m benchmarks.cycle_bench [--cycles 300] [--sets 4] [--batch B] [--kv4]
 
 --batch B > 1 runs the cycles of B sequences together: batched draft calls (radar_draft_expand_batch with
 every sequence's own state and decision), one batched rerank, attention and the verify walk over the B
 sequences; a scripted stop then applies to every second sequence only, so that the batch is ragged.
+
+--kv4 keeps the attention's rows in the paged 4-bit cache: before the attention the tree gets its blocks and slots and its keys and values go
+into the cache, and after the walk the accepted path's rows are moved into place (radar_kvq_blocks, radar_kvq_append, radar_tree_attention_kvq,
+radar_kvq_commit).  The prefix stays what it is, cycle after cycle.
 """
 import argparse
 import json
@@ -24,6 +28,7 @@ def main():
     ap.add_argument("--cycles", type=int, default=300)
     ap.add_argument("--sets", type=int, default=4)
     ap.add_argument("--batch", type=int, default=1)
+    ap.add_argument("--kv4", action="store_true")
     args = ap.parse_args()
     import numpy as np
     import torch
@@ -46,6 +51,32 @@ def main():
     attn_parents = torch.from_numpy(par_np[None].copy()).to(dev)
     ctx = torch.tensor(A.ctx_lens, dtype=torch.int32, device=dev)
     nn_ = torch.tensor(A.n_nodes, dtype=torch.int32, device=dev)
+
+    class Cache4:
+        """One layer's paged 4-bit cache of B sequences, their prefixes written, and the calls of a cycle that use it."""
+
+        def __init__(self, q, ctx, nn, parents, out):
+            B, T_ = q.shape[:2]
+            L, R = int(ctx.max()), 16
+            per = -(-(L + T_) // R)
+            self.q, self.ctx, self.nn, self.parents, self.out, self.S = q, ctx, nn, parents, out, L + T_
+            self.cache, self.tables = b.KvqCache(B * per, R, A.Hkv, A.D), b.KvqTables(B, per, B * per, R)
+            rows = lambda n: torch.randn((B, n, A.Hkv, A.D), generator=gen, device=dev).to(torch.bfloat16)       # noqa: E731
+            slots, _ = b.radar_kvq_blocks(torch.zeros_like(ctx), self.tables, L, n_new=ctx)
+            b.radar_kvq_append(self.cache, rows(L), rows(L), slots)
+            self.k, self.v = rows(T_), rows(T_)
+            self.slots, self.granted = torch.empty((B, T_), dtype=torch.int32, device=dev), torch.empty_like(ctx)
+            self.new_ctx = torch.empty_like(ctx)
+            self.ws = b.new_workspace(b.radar_tree_attention_kvq_workspace_bytes(b.kvq_attn_desc(q, self.cache, per, self.S)))
+
+        def attention(self):
+            return [b.radar_kvq_blocks(self.ctx, self.tables, self.q.shape[1], n_new=self.nn, slots=self.slots, granted=self.granted, prepared=True),
+                    b.radar_kvq_append(self.cache, self.k, self.v, self.slots, prepared=True),
+                    b.radar_tree_attention_kvq(self.q, self.cache, self.tables.block_tables, self.ctx, self.parents, self.nn, S_max=self.S,
+                                               out=self.out, workspace=self.ws, prepared=True)]
+
+        def commit(self, accepted):
+            return [b.radar_kvq_commit(self.cache, self.tables.block_tables, self.ctx, accepted[0], accepted[1], new_ctx_lens=self.new_ctx, prepared=True)]
 
     class Cycle:
         def __init__(self):
@@ -73,6 +104,7 @@ def main():
             adesc = b.attn_desc(self.q, self.kc)
             self.attn_ws = b.new_workspace(b.radar_tree_attention_workspace_bytes(adesc))
             self.adesc = adesc
+            self.kv4 = Cache4(self.q, ctx, nn_, attn_parents, self.attn_out) if args.kv4 else None
             self.calls = self.prepare()
 
         def prepare(self):
@@ -88,12 +120,13 @@ def main():
                 count_max += (1 if s == 0 else k) * k
                 ps, pi = self.eouts[s].frontier_scores, self.eouts[s].frontier_pool_idx
             calls.append(b.radar_draft_rerank_cycle(self.pool, self.state, cap, N, 1, out=self.tree, prepared=True))
-            calls.append(b.radar_tree_attention(self.q, self.kc, self.vc, attn_parents, ctx, nn_, out=self.attn_out,
-                                                desc=self.adesc, workspace=self.attn_ws, prepared=True))
+            calls += self.kv4.attention() if args.kv4 else [
+                b.radar_tree_attention(self.q, self.kc, self.vc, attn_parents, ctx, nn_, out=self.attn_out,
+                                       desc=self.adesc, workspace=self.attn_ws, prepared=True)]
             calls.append(b.radar_verify_accept(self.target, self.tree.tokens.view(1, -1), self.tree.parents.view(1, -1),
                                                self.tree.n_nodes, self.acc_uni, mode=b.RADAR_ACCEPT_SAMPLE, D_max=T - 1,
                                                out=self.acc_out, workspace=self.acc_ws, prepared=True))
-            return calls
+            return calls + (self.kv4.commit(self.acc_out) if args.kv4 else [])
 
         def enqueue(self, calls=None):
             for c in (calls or self.calls):
@@ -137,6 +170,7 @@ def main():
                             torch.empty(B, dtype=torch.int32, device=dev))
             self.adesc = b.attn_desc(self.q, self.kc)
             self.attn_ws = b.new_workspace(b.radar_tree_attention_workspace_bytes(self.adesc))
+            self.kv4 = Cache4(self.q, self.ctx, self.nn, self.attn_parents, self.attn_out) if args.kv4 else None
             self.calls = self.prepare()
 
         def prepare(self):
@@ -153,12 +187,13 @@ def main():
                 ps, pi = self.eouts[s].frontier_scores, self.eouts[s].frontier_pool_idx
             calls.append(b.radar_draft_rerank_batch(self.pool, N, self.roots, states=self.state, pool_count_max=cap,
                                                     out=self.tree, prepared=True))
-            calls.append(b.radar_tree_attention(self.q, self.kc, self.vc, self.attn_parents, self.ctx, self.nn,
-                                                out=self.attn_out, desc=self.adesc, workspace=self.attn_ws, prepared=True))
+            calls += self.kv4.attention() if args.kv4 else [
+                b.radar_tree_attention(self.q, self.kc, self.vc, self.attn_parents, self.ctx, self.nn,
+                                       out=self.attn_out, desc=self.adesc, workspace=self.attn_ws, prepared=True)]
             calls.append(b.radar_verify_accept(self.target, self.tree.tokens, self.tree.parents, self.tree.n_nodes, self.acc_uni,
                                                mode=b.RADAR_ACCEPT_SAMPLE, D_max=T - 1, out=self.acc_out, workspace=self.acc_ws,
                                                prepared=True))
-            return calls
+            return calls + (self.kv4.commit(self.acc_out) if args.kv4 else [])
 
         def enqueue(self, calls=None):
             for c in (calls or self.calls):
@@ -187,6 +222,12 @@ def main():
             cy.enqueue(held)
         graphs.append((g, held))
 
+    attn_launches = 2
+    if args.kv4:
+        b.radar_profile_begin(64)
+        cycles[0].enqueue()
+        attn_launches = sum(v["calls"] for name, v in b.radar_profile_end().items() if name.startswith("kvq_"))
+
     n = args.cycles
     for stop_after in (t_max, 4, 2):
         for cy in cycles:
@@ -202,14 +243,14 @@ def main():
             torch.cuda.synchronize()
             us = (time.perf_counter() - t0) / n * 1e6
             st = cycles[0].state.cpu().tolist()
-            extra = {}
+            extra = {"cache": "paged, 4 bits"} if args.kv4 else {}
             if B > 1:                                      # report the batch: sequence 0 stops, sequence 1 does not
-                extra = {"batch": B, "us_per_cycle_and_sequence": round(us / B, 2),
+                extra |= {"batch": B, "us_per_cycle_and_sequence": round(us / B, 2),
                          "draft_calls_run_per_sequence": [r[2] for r in st][:8]}
                 st = st[0]
             print(json.dumps({"mode": mode, **extra, "draft_calls_allowed": t_max, "stop_after": stop_after,
                               "draft_calls_run": st[2], "pool_count": st[1], "us_per_cycle": round(us, 2),
-                              "launches_per_cycle": (2 * t_max - 1 if B > 1 else t_max) + 1 + 2 + 1, "cycles": n,
+                              "launches_per_cycle": (2 * t_max - 1 if B > 1 else t_max) + 1 + attn_launches + 1, "cycles": n,
                               "workload": "c3 expand chain (V=%d, k=%d, fused prediction model) + rerank N=%d + one c2 attention layer + sampled accept" % (V, k, N)}),
                   flush=True)
 

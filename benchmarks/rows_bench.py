@@ -1,6 +1,6 @@
 """Times the entry points that widen the hot path, at the 8B shape (V = 128256, k = 10, 61 tree rows):
 acceptance-length distribution, prediction-model step (alone and fused into the expansion), the
-expansion of 4, 16 and 64 sequences in one launch, and verification with draft distributions.  One JSON line per entry point with the per-kernel device
+expansion of 4, 16 and 64 sequences in one launch, verification with draft distributions, and the paged 4-bit cache.  One JSON line per entry point with the per-kernel device
 durations the library records (radar_profile_begin / radar_profile_end) and the algorithmic bytes.
 
     python -m benchmarks.rows_bench [--reps 100]
@@ -127,6 +127,35 @@ def main():
                                        d["uniforms"], d["q_rows"], workspace=qws, prepared=True, walk_spin_limit=limit)
         used = len(set(x["q_rows"][0, 1:T].tolist()))
         timed("radar_verify_accept_q", [call], (T + used) * V * 4, label + "; bytes: %d target rows and %d draft rows, of which the shared walk reads those it visits" % (T, used))
+
+    # the paged 4-bit cache of one layer: 32 heads on 8, D = 128; 2048 to 8192 rows of prefix
+    Hq, H, D, R = 32, 8, 128, 16
+    for B, Tq, lo, hi in ((1, 1, 2048, 2048), (64, 1, 2048, 8192), (1, 60, 2048, 2048), (16, 60, 2048, 8192)):
+        L = rng.integers(lo, hi + 1, B)
+        per = -(-(int(L.max()) + Tq) // R)
+        n_blocks = sum(-(-(int(x) + Tq) // R) for x in L)
+        cache, tables = b.KvqCache(n_blocks, R, H, D), b.KvqTables(B, per, n_blocks, R)
+        cache.data.random_(0, 256, generator=gen)
+        cache.data[..., R * D:].fill_(126)
+        ctx = to(L.astype(np.int32))
+        b.radar_kvq_blocks(torch.zeros_like(ctx), tables, int(L.max()), n_new=ctx)
+        kv = torch.randn((2, B, Tq, H, D), generator=gen, device=dev).to(torch.bfloat16)
+        q = torch.randn((B, Tq, Hq, D), generator=gen, device=dev).to(torch.bfloat16)
+        parents = to(np.tile(synth.make_tree(rng, Tq, 8, k, V)[0], (B, 1)).astype(np.int32)) if Tq > 1 else None
+        room = b.radar_kvq_blocks(ctx, tables, Tq, prepared=True)
+        room()
+        write = b.radar_kvq_append(cache, kv[0], kv[1], room.out[0], prepared=True)
+        what = "B=%d T=%d, %d rows of prefix" % (B, Tq, int(L.sum()))
+        row = H * (D + D // 16)
+        attend = b.radar_tree_attention_kvq(q, cache, tables.block_tables, ctx, parents, S_max=int(L.max()) + Tq, prepared=True)
+        timed("radar_tree_attention_kvq " + what, [attend], (int(L.sum()) + B * Tq) * row + q.numel() * 4, "bytes: the sequences' rows once, queries and outputs")
+        if Tq > 1:
+            length, path = torch.full((B,), 6, dtype=torch.int32, device=dev), to(np.tile([0, 3, 9, 17, 30, 41, 55], (B, 1)).astype(np.int32))
+            move = b.radar_kvq_commit(cache, tables.block_tables, ctx, length, path, prepared=True)
+            timed("radar_kvq_blocks + append + commit " + what, [room, write, move], B * Tq * (4 * H * D + row) + B * 6 * 2 * row,
+                  "a verification pass's other calls; bytes: the trees' rows in and the paths' rows")
+        del cache
+        torch.cuda.empty_cache()
 
 
 if __name__ == "__main__":

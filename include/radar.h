@@ -548,7 +548,7 @@ radar_status radar_draft_rerank_batch(const int32_t *pool_tokens, const float *p
 typedef struct radar_kvq_desc {
     int32_t n_blocks, block_rows, Hkv, D;
     int32_t layers;          /* radar_kvq_commit and radar_kvq_read: how many layers the call covers */
-    int64_t layer_stride;    /* bytes from one layer's cache to the next; 0 => dense */
+    int64_t layer_stride;    /* bytes from one layer's cache to the next, a layer's at least; 0 => dense */
 } radar_kvq_desc;
 
 /* Bytes of one KV head's rows of one block; 0 where the limits are not met. */

@@ -706,6 +706,8 @@ class KvqCache:
             data = torch.zeros((layers, n_blocks, Hkv, chunk), dtype=torch.uint8, device=device)
         if data.dim() != 4 or data.dtype != torch.uint8 or data.shape[3] != chunk or not data[0].is_contiguous():
             raise ValueError(f"data: expected uint8 [layers, n_blocks, Hkv, {chunk}], each layer contiguous")
+        if data.shape[0] > 1 and (data.stride(0) < data[0].numel() or data.stride(0) % 16 != 0):
+            raise ValueError(f"data: layers {data.stride(0)} bytes apart; expected a multiple of 16 of at least {data[0].numel()}")
         self.data, self.block_rows, self.D = data, int(block_rows), int(D)
         self.layers, self.n_blocks, self.Hkv = (int(n) for n in data.shape[:3])
 

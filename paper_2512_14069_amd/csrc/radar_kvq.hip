@@ -466,6 +466,7 @@ extern "C" radar_status radar_kvq_append(const void *k, const void *v, const int
 static int64_t layer_bytes(const radar_kvq_desc *d) {
     const int64_t dense = (int64_t)d->n_blocks * d->Hkv * d->block_rows * (d->D + d->D / 16);
     if (d->layers < 1 || d->layer_stride < 0 || (d->layer_stride & 15) != 0) return -1;
+    if (d->layer_stride != 0 && d->layers > 1 && d->layer_stride < dense) return -1;       // layers would share memory
     return d->layer_stride ? d->layer_stride : dense;
 }
 

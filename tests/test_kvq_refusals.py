@@ -67,6 +67,21 @@ def test_rows(lib):
     assert read(N=0) == 0
 
 
+def test_layers_do_not_share_memory(lib):
+    from paper_2512_14069_amd import binding as b
+    layer = 8 * 2 * 16 * 136
+    for stride, layers, want in ((layer - 16, 2, -1), (16, 3, -1), (layer, 2, 0), (16, 1, 0)):
+        assert lib.radar_kvq_read(ONE, ONE, ONE, ONE, 0, ctypes.byref(desc(layers=layers, layer_stride=stride)), None) == want
+    assert lib.radar_kvq_commit(ONE, ONE, 4, ONE, ONE, ONE, 9, 1, None, ctypes.byref(desc(layer_stride=layer - 16)), None) == -1
+    one = torch.zeros((1, 8, 2, 16 * 136), dtype=torch.uint8)
+    with pytest.raises(ValueError, match="layers 0 bytes apart"):
+        b.KvqCache(data=one.expand(3, -1, -1, -1))
+    wide = torch.zeros((3, layer + 8), dtype=torch.uint8)[:, :layer].view(3, 8, 2, 16 * 136)
+    with pytest.raises(ValueError, match="multiple of 16"):
+        b.KvqCache(data=wide)
+    assert b.KvqCache(data=torch.zeros((3, layer + 32), dtype=torch.uint8)[:, :layer].view(3, 8, 2, 16 * 136)).desc().layer_stride == layer + 32
+
+
 def test_commit(lib):
     d, two = ctypes.byref(desc()), ctypes.c_void_p(512)
     commit = lambda c=ONE, t=ONE, M=4, ctx=ONE, n=ONE, p=ONE, P=9, B=1, out=two, dd=d: lib.radar_kvq_commit(c, t, M, ctx, n, p, P, B, out, dd, None)  # noqa: E731
