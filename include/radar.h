@@ -542,8 +542,9 @@ radar_status radar_draft_rerank_batch(const int32_t *pool_tokens, const float *p
  * Row j of sequence b is row j % R of block block_tables[b][j / R].
  *
  * Limits for all of them: D in {64, 128}; block_rows in {16, 32, 64, 128};
- * n_blocks * block_rows < 2^31; Hkv <= 65535; cache and layer_stride multiples
- * of 16 bytes.  Block numbers and slots that are out of range are not
+ * n_blocks * block_rows < 2^31; Hkv <= 65535; layers <= 65535 and layers * Hkv
+ * < 2^24; rows of a call times Hkv < 2^27; cache and layer_stride multiples of 16
+ * bytes.  Block numbers and slots that are out of range are not
  * dereferenced: such a row is not there. */
 typedef struct radar_kvq_desc {
     int32_t n_blocks, block_rows, Hkv, D;
@@ -622,7 +623,8 @@ radar_status radar_kvq_commit(void *cache, const int32_t *block_tables, int32_t 
  * cache: the layer's first block; block_tables i32 [B,max_blocks]; S_max: the rows
  * that the call is planned for, at most max_blocks * block_rows (the longest
  * ctx_lens[b] + T_max where it is known).  Other arguments and limits as for
- * radar_tree_attention; q and out 16-byte aligned rows. */
+ * radar_tree_attention; B * Hkv * ceil(Hq / Hkv * T_max / 16) < 2^23 - 7; q and out
+ * 16-byte aligned rows.  One kernel, or two where units of work are divided. */
 typedef struct radar_kvq_attn_desc {
     radar_kvq_desc cache;    /* layers and layer_stride are ignored */
     int32_t B, T_max, Hq, max_blocks, S_max;

@@ -861,9 +861,12 @@ def kvq_attn_desc(q, cache, max_blocks, S_max=None, out=None, rows_per_split=0, 
     d.max_blocks = int(max_blocks)
     d.S_max = d.max_blocks * cache.block_rows if S_max is None else int(S_max)
     d.rows_per_split, d.softmax_scale = int(rows_per_split), float(softmax_scale)
-    d.q_stride_b, d.q_stride_t, d.q_stride_h = q.stride()[:3]
-    if out is not None:
-        d.out_stride_b, d.out_stride_t, d.out_stride_h = out.stride()[:3]
+    for t, name in ((q, "q"), (out, "out")):
+        for axis, of in enumerate("bth"):
+            if t is not None and t.shape[axis] > 1:
+                if t.stride(axis) == 0:
+                    raise ValueError(f"{name}: broadcast along axis {axis}; make it contiguous")
+                setattr(d, f"{name}_stride_{of}", t.stride(axis))
     return d
 
 

@@ -170,7 +170,7 @@ struct RwLane {                                // which eight values a lane has
 template <int D>
 __device__ __forceinline__ RwLane<D> rw_lane(int Hkv, bool down) {
     constexpr int P = D / 8, HALF = 8 * P;     // lanes of K, of V
-    const uint32_t unit = blockIdx.x * (kRwThreads / (2 * HALF)) + threadIdx.x / (2 * HALF), group = unit / (uint32_t)Hkv;      // (the grid is at most 2^31)
+    const uint32_t unit = blockIdx.x * (kRwThreads / (2 * HALF)) + threadIdx.x / (2 * HALF), group = unit / (uint32_t)Hkv;      // (of a grid of less than 2^24)
     const int l = threadIdx.x % (2 * HALF), l2 = l % HALF;
     RwLane<D> r;
     r.is_v = l >= HALF;
@@ -443,7 +443,7 @@ static radar_status rw_args(const void *k, const void *v, const int32_t *slots, 
     const int units = kRwThreads / (2 * d->D);
     if (N > (int64_t)INT32_MAX) return RADAR_UNSUPPORTED_SHAPE;
     *groups = ((N + 7) / 8 * d->Hkv + units - 1) / units;
-    return *groups <= INT32_MAX ? RADAR_OK : RADAR_UNSUPPORTED_SHAPE;
+    return *groups < (1 << 24) ? RADAR_OK : RADAR_UNSUPPORTED_SHAPE;               // (a launch has less than 2^32 lanes)
 }
 
 extern "C" radar_status radar_kvq_append(const void *k, const void *v, const int32_t *slots, void *cache, int64_t N, int64_t stride_n, int64_t stride_h,
@@ -500,7 +500,7 @@ extern "C" radar_status radar_kvq_commit(void *cache, const int32_t *block_table
     CmArgs a{static_cast<unsigned char *>(cache), block_tables, ctx_lens, accept_len, accept_path, new_ctx_lens, layer_bytes(d),
              max_blocks, path_len, kvq_log2(d->block_rows), d->Hkv, 0, d->n_blocks, 0};
     if (a.layer_stride < 0) return RADAR_INVALID_ARG;
-    if ((int64_t)d->layers * d->Hkv > INT32_MAX - 64) return RADAR_UNSUPPORTED_SHAPE;
+    if ((int64_t)d->layers * d->Hkv >= (1 << 24)) return RADAR_UNSUPPORTED_SHAPE;
     a.units = d->layers * d->Hkv;
     // pairs a wavefront: as many as leave 16 wavefronts a CU
     a.per = (int)std::min<int64_t>(std::max<int64_t>((int64_t)a.units * B / kCmWaves, 1), 16);

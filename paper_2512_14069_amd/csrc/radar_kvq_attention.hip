@@ -9,6 +9,7 @@
 // products as they lie.  A lane of the V operand holds eight keys of one d, and the layout puts the codes of eight keys for the
 // same eight d side by side: 32 bytes are the operands of eight products.
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <type_traits>
 
@@ -791,8 +792,8 @@ static radar_status check_kvq_attn(const radar_kvq_attn_desc *d) {
     if (d->rows_per_split < 0 || d->rows_per_split % 64 != 0) return RADAR_INVALID_ARG;
     if (!(d->softmax_scale >= 0.f)) return RADAR_INVALID_ARG;
     if (d->T_max > RADAR_T_MAX || d->B > 65535 || d->Hq > 65535 || d->S_max > INT32_MAX - 4096) return RADAR_UNSUPPORTED_SHAPE;
-    // units of 16 columns are counted in 32 bits
-    if ((int64_t)d->B * d->cache.Hkv * ((d->Hq / d->cache.Hkv * d->T_max + 15) / 16) > (1 << 30)) return RADAR_UNSUPPORTED_SHAPE;
+    // a launch has less than 2^32 lanes, a unit of 16 columns up to 512 of them
+    if ((int64_t)d->B * d->cache.Hkv * ((d->Hq / d->cache.Hkv * d->T_max + 15) / 16) > (1 << 23) - 8) return RADAR_UNSUPPORTED_SHAPE;
     return RADAR_OK;
 }
 
@@ -854,10 +855,17 @@ extern "C" size_t radar_tree_attention_kvq_workspace_bytes(const radar_kvq_attn_
 template <int D, int NC, bool FAR>
 static hipError_t launch_kvq(const KqArgs &a, const KqPlan &p, hipStream_t s) {
     constexpr int bytes = KqShape<D, NC>::lds_bytes();
-    static const hipError_t configured = hipFuncSetAttribute(reinterpret_cast<const void *>(&kvq_attn_kernel<D, NC, FAR>),
-                                                             hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (configured != hipSuccess) return configured;
-    const hipError_t e = launch("kvq_attention", kvq_attn_kernel<D, NC, FAR>, dim3((unsigned)p.workgroups), dim3(kKqThreads), bytes, s, a);
+    static std::atomic<uint64_t> configured{0};            // devices on which the kernel may have so much LDS (two threads may both say so)
+    int device = 0;
+    hipError_t e = hipGetDevice(&device);
+    if (e != hipSuccess) return e;
+    const uint64_t bit = 1ull << (device & 63);
+    if (device > 63 || !(configured.load(std::memory_order_relaxed) & bit)) {
+        e = hipFuncSetAttribute(reinterpret_cast<const void *>(&kvq_attn_kernel<D, NC, FAR>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e != hipSuccess) return e;
+        configured.fetch_or(bit, std::memory_order_relaxed);
+    }
+    e = launch("kvq_attention", kvq_attn_kernel<D, NC, FAR>, dim3((unsigned)p.workgroups), dim3(kKqThreads), bytes, s, a);
     if (e != hipSuccess) return e;
     if (p.whole) return e;
     return launch("kvq_merge", kvq_merge_kernel<D, NC>, dim3((unsigned)(a.B * a.Hkv * a.max_cgs), (unsigned)NC), dim3(256), 0, s, a);

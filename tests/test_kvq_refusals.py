@@ -58,7 +58,7 @@ def test_rows(lib):
     append = lambda k=ONE, v=ONE, s=ONE, c=ONE, N=1, sn=0, sh=0, dd=d: lib.radar_kvq_append(k, v, s, c, N, sn, sh, dd, None)   # noqa: E731
     assert append(k=None) == append(v=None) == append(s=None) == append(c=None) == append(dd=None) == -1
     assert append(k=odd) == append(v=odd) == append(c=odd) == append(N=-1) == append(sn=12) == append(sh=-8) == append(sn=-128) == -1
-    assert append(N=1 << 31) == -2
+    assert append(N=1 << 31) == append(N=1 << 26) == -2              # more lanes than a launch has
     assert append(N=0) == 0                                          # nothing to do, nothing launched
     read = lambda c=ONE, s=ONE, k=ONE, v=ONE, N=1, dd=d: lib.radar_kvq_read(c, s, k, v, N, dd, None)                             # noqa: E731
     assert read(c=None) == read(s=None) == read(k=None) == read(v=None) == read(dd=None) == read(k=odd) == read(N=-2) == -1
@@ -132,7 +132,7 @@ def test_attention(lib):
     assert call(B=0) == call(T_max=0) == call(Hq=0) == call(Hq=3) == call(max_blocks=0) == call(S_max=0) == -1
     assert call(S_max=65) == call(rows_per_split=32) == call(rows_per_split=-64) == call(softmax_scale=-1.0) == call(softmax_scale=float("nan")) == -1
     assert call(q_stride_t=12) == call(out_stride_h=4) == call(q_stride_b=-8) == -1
-    assert call(T_max=65) == call(B=65536) == call(Hq=65538) == -2
+    assert call(T_max=65) == call(B=65536) == call(Hq=65538) == call(B=65535, T_max=64, Hq=64) == -2
 
 
 def test_the_binding_raises():
@@ -159,6 +159,9 @@ def test_the_binding_raises():
                 lambda: b.radar_tree_attention_kvq(torch.zeros((1, 2, 4, 128), dtype=torch.bfloat16), cache, i32(2, 2), i32(1)),
                 lambda: b.radar_tree_attention_kvq(torch.zeros((1, 2, 4, 128), dtype=torch.bfloat16), cache, i32(1, 2), i32(2)),
                 lambda: b.radar_tree_attention_kvq(torch.zeros((1, 2, 4, 128), dtype=torch.bfloat16), cache, i32(1, 2), i32(1), parents=i32(2, 1)),
+                lambda: b.radar_tree_attention_kvq(torch.zeros((1, 1, 4, 128), dtype=torch.bfloat16).expand(3, 2, 4, 128), cache, i32(3, 2), i32(3)),
+                lambda: b.radar_tree_attention_kvq(torch.zeros((1, 2, 4, 128), dtype=torch.bfloat16), cache, i32(1, 2), i32(1),
+                                                   out=torch.zeros((1, 2, 1, 128), dtype=torch.bfloat16).expand(1, 2, 4, 128)),
                 lambda: b.radar_kvq_blocks(i32(3), b.KvqTables(2, 4, 9, device="cpu"), 8),
                 lambda: b.radar_kvq_blocks(i32(2), b.KvqTables(2, 4, 9, device="cpu"), 8, slots=i32(2, 7)),
                 lambda: b.radar_kvq_blocks(i32(2), b.KvqTables(2, 4, 9, device="cpu"), 8, n_new=i32(1))):
