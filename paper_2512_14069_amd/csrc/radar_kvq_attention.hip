@@ -749,34 +749,84 @@ __global__ __launch_bounds__(kKqThreads, NC == 1 ? 4 : 2) void kvq_attn_kernel(K
     }
 }
 
-// The units that several workgroups had parts of.  A workgroup takes one block of 16 columns of a unit, a lane 4 (D = 64) or 8 outputs of one.
-template <int D, int NC>
-__global__ __launch_bounds__(256) void kvq_merge_kernel(KqArgs a) {
+// The units that several workgroups had parts of.  A lane takes 4 (D = 64) or 8 outputs of a column.  GROUPS = 1: a workgroup has 16 columns, a lane
+// goes over the parts.  GROUPS = 16, for units in many parts (a long context of one sequence): a workgroup has 4 columns and a wavefront
+// every 16th part, four at a time; they meet in LDS (64 parts of a unit: 4.6 us, 25 by one lane).
+template <int D, int NC, int GROUPS>
+__global__ __launch_bounds__(GROUPS == 1 ? 256 : 1024) void kvq_merge_kernel(KqArgs a) {
     using S = KqShape<D, NC>;
-    constexpr int PER = D / 16;
+    constexpr int PER = D / 16, CW = GROUPS == 1 ? 16 : 4, U = GROUPS == 1 ? 1 : 4, Q = PER / 4;
     const int unit = blockIdx.x, b = unit / (a.Hkv * a.max_cgs), hk = unit / a.max_cgs % a.Hkv, cg = unit % a.max_cgs, n = blockIdx.y;
     const KqSeq s = kq_seq(a, b);
-    if ((cg * NC + n) * 16 >= s.nn * a.G) return;
+    if ((cg * S::COLS + n * CW) >= s.nn * a.G) return;
     const uint32_t tab = a.unit_tab[unit];
     const int w0 = tab >> 16, w1 = tab & 0xffff;
     if (w0 == w1) return;
-    const int col = n * 16 + threadIdx.x / 16, d = threadIdx.x % 16 * PER;
+    const int group = GROUPS == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave_id()), mine = GROUPS == 1 ? threadIdx.x / 16 : lane_id() / 16;
+    const int col = n * CW + mine, d = threadIdx.x % 16 * PER;
+    float M = -kKqNone, l = 0.f;
+    floatx4 acc[Q];
+#pragma unroll
+    for (int x = 0; x < Q; ++x) acc[x] = floatx4{0.f, 0.f, 0.f, 0.f};
+    auto add = [&](const float (&m)[U], const float (&ls)[U], const floatx4 (&o)[U][Q]) {
+        float Mn = M;
+#pragma unroll
+        for (int u = 0; u < U; ++u) Mn = fmaxf(Mn, m[u]);
+        const float f0 = __builtin_amdgcn_exp2f(M - Mn);
+        M = Mn;
+        l *= f0;
+#pragma unroll
+        for (int x = 0; x < Q; ++x) acc[x] *= f0;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const float f = __builtin_amdgcn_exp2f(m[u] - Mn);
+            l += ls[u] * f;
+#pragma unroll
+            for (int x = 0; x < Q; ++x) acc[x] += o[u][x] * f;
+        }
+    };
+    for (int w = w0 + group; w <= w1; w += U * GROUPS) {
+        float m[U], ls[U];
+        floatx4 o[U][Q];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const bool there = w + u * GROUPS <= w1;                 // (the same in every lane; otherwise the last part once more, as nothing)
+            const int part = min(w + u * GROUPS, w1);
+            const float *const from = a.part + (size_t)(2 * part + (part < w1 ? 1 : 0)) * S::PART;
+            m[u] = there ? from[S::COLS * D + col] : -kKqNone;
+            ls[u] = there ? from[S::COLS * D + S::COLS + col] : 0.f;
+#pragma unroll
+            for (int x = 0; x < Q; ++x) o[u][x] = there ? *reinterpret_cast<const floatx4 *>(from + (size_t)col * D + d + 4 * x) : floatx4{0.f, 0.f, 0.f, 0.f};
+        }
+        add(m, ls, o);
+    }
+    if constexpr (GROUPS > 1) {
+        __shared__ float s_m[GROUPS][CW], s_l[GROUPS][CW];
+        __shared__ __attribute__((aligned(16))) float s_o[GROUPS][CW][D];
+        if (d == 0) { s_m[group][mine] = M; s_l[group][mine] = l; }
+#pragma unroll
+        for (int x = 0; x < Q; ++x) *reinterpret_cast<floatx4 *>(&s_o[group][mine][d + 4 * x]) = acc[x];
+        __syncthreads();
+        if (group != 0) return;
+        for (int g = 1; g < GROUPS; g += U) {                        // (the last of the 15 is counted once: beyond it nothing)
+            float m[U], ls[U];
+            floatx4 o[U][Q];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const bool there = g + u < GROUPS;
+                const int y = min(g + u, GROUPS - 1);
+                m[u] = there ? s_m[y][mine] : -kKqNone;
+                ls[u] = there ? s_l[y][mine] : 0.f;
+#pragma unroll
+                for (int x = 0; x < Q; ++x) o[u][x] = there ? *reinterpret_cast<const floatx4 *>(&s_o[y][mine][d + 4 * x]) : floatx4{0.f, 0.f, 0.f, 0.f};
+            }
+            add(m, ls, o);
+        }
+    }
     const int gc = cg * S::COLS + col, i = gc / a.G, h = hk * a.G + gc - i * a.G;
     if (i >= s.nn) return;
-    float M = -kKqNone, l = 0.f;
-    floatx4 acc[PER / 4];
 #pragma unroll
-    for (int x = 0; x < PER / 4; ++x) acc[x] = floatx4{0.f, 0.f, 0.f, 0.f};
-    for (int w = w0; w <= w1; ++w) {
-        const float *const from = a.part + (size_t)(2 * w + (w < w1 ? 1 : 0)) * S::PART;
-        const float m = from[S::COLS * D + col], Mn = fmaxf(M, m), f0 = __builtin_amdgcn_exp2f(M - Mn), f1 = __builtin_amdgcn_exp2f(m - Mn);
-        M = Mn;
-        l = l * f0 + from[S::COLS * D + S::COLS + col] * f1;
-#pragma unroll
-        for (int x = 0; x < PER / 4; ++x) acc[x] = acc[x] * f0 + *reinterpret_cast<const floatx4 *>(from + (size_t)col * D + d + 4 * x) * f1;
-    }
-#pragma unroll
-    for (int x = 0; x < PER / 4; ++x) kq_write(a, b, i, h, d + 4 * x, acc[x], M, l);
+    for (int x = 0; x < Q; ++x) kq_write(a, b, i, h, d + 4 * x, acc[x], M, l);
 }
 
 }  // namespace radar
@@ -868,7 +918,10 @@ static hipError_t launch_kvq(const KqArgs &a, const KqPlan &p, hipStream_t s) {
     e = launch("kvq_attention", kvq_attn_kernel<D, NC, FAR>, dim3((unsigned)p.workgroups), dim3(kKqThreads), bytes, s, a);
     if (e != hipSuccess) return e;
     if (p.whole) return e;
-    return launch("kvq_merge", kvq_merge_kernel<D, NC>, dim3((unsigned)(a.B * a.Hkv * a.max_cgs), (unsigned)NC), dim3(256), 0, s, a);
+    const unsigned units = (unsigned)(a.B * a.Hkv * a.max_cgs);
+    // units in more than four parts or so
+    if (4 * units <= (unsigned)p.workgroups) return launch("kvq_merge", kvq_merge_kernel<D, NC, 16>, dim3(units, 4 * NC), dim3(1024), 0, s, a);
+    return launch("kvq_merge", kvq_merge_kernel<D, NC, 1>, dim3(units, NC), dim3(256), 0, s, a);
 }
 
 extern "C" radar_status radar_tree_attention_kvq(const void *q, const void *cache, const int32_t *block_tables, const int32_t *parents,

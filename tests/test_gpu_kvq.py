@@ -267,15 +267,17 @@ def test_attention_against_the_oracle(ctx, T, nodes, Hq, H, D, R):
         check_attention(q, cache, R, D, 1, tables, ctx, par, nodes, got, lse)
 
 
-@pytest.mark.parametrize("ctx,T,Hq,H,D,R", [([2048], 60, 32, 8, 128, 32), ([700, 2900, 1], 1, 32, 8, 128, 16), ([4099], 3, 16, 2, 64, 16), ([1500, 9], 40, 64, 8, 128, 64)])
-def test_attention_over_long_contexts(ctx, T, Hq, H, D, R):
-    """Rows split over workgroups and joined.  The trees are chains (parents left out), all nodes used (n_nodes left out)."""
+@pytest.mark.parametrize("ctx,T,Hq,H,D,R,split", [
+    ([2048], 60, 32, 8, 128, 32, 0), ([700, 2900, 1], 1, 32, 8, 128, 16, 0), ([4099], 3, 16, 2, 64, 16, 0), ([1500, 9], 40, 64, 8, 128, 64, 0),
+    ([9001], 1, 4, 1, 128, 16, 64), ([9001], 20, 4, 1, 64, 16, 64), ([6000, 300], 40, 2, 1, 128, 32, 64)])
+def test_attention_over_long_contexts(ctx, T, Hq, H, D, R, split):
+    """Rows split over workgroups and joined, up to 140 parts.  The trees are chains (parents left out), all nodes used (n_nodes left out)."""
     b, rng = binding(), seed(70 + T)
     ctx = np.array(ctx, np.int32)
     tables, cache, q, qb, _ = make_attention(rng, ctx, T, np.full(len(ctx), T), Hq, H, D, R)
     c = gpu_cache(cache, R, D)
     lse = torch.empty(q.shape[:3], dtype=torch.float32, device="cuda")
-    got = b.radar_tree_attention_kvq(bf16_dev(qb), c, dev(tables), dev(ctx), lse_out=lse, S_max=int(ctx.max()) + T)
+    got = b.radar_tree_attention_kvq(bf16_dev(qb), c, dev(tables), dev(ctx), lse_out=lse, S_max=int(ctx.max()) + T, rows_per_split=split)
     pick = sorted({0, T // 2, T - 1})                                # of the rows; the oracle is slow
     par = np.tile(np.arange(-1, T - 1, dtype=np.int32), (len(ctx), 1))
     some = q.copy()
