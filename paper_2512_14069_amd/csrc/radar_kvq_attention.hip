@@ -583,24 +583,16 @@ __global__ __launch_bounds__(kKqThreads, NC == 1 ? 4 : 2) void kvq_attn_kernel(K
         const kq_bytes base = (kq_bytes)(uintptr_t)kq_scalar(a.cache + (size_t)p.hk * KvqChunk<D>::bytes(1 << a.rbits));
         const int mine = p.s0 + w;
         const bool active = mine < p.s1;
-        // the first steps' loads, before the queries
-        constexpr int DEEP = NC > 2 || (NC == 1 && FAR) ? 1 : 2;                         // steps that the loads are ahead, two where the registers allow
-        KqK<D> k[DEEP];
-        KqV v[DEEP];
-        KqIds id[DEEP], nid{0, 0};
+        // the first step's loads, before the queries (two steps ahead took as long or longer: 64 single tokens 71 us, 69 with one)
+        KqK<D> k;
+        KqV v;
+        KqIds id{0, 0}, nid{0, 0};
         if (active) {
-#pragma unroll
-            for (int x = 0; x < DEEP; ++x) {
-                const int s = min(mine + x * kKqWaves, p.s1 - 1);
-                id[x] = kq_ids(a, table, s * 32, p.total);
-            }
-            nid = kq_ids(a, table, min(mine + DEEP * kKqWaves, p.s1 - 1) * 32, p.total);
-#pragma unroll
-            for (int x = 0; x < DEEP; ++x) {
-                const KqBase at = kq_base<D>(a, base, id[x], min(mine + x * kKqWaves, p.s1 - 1) * 32);
-                kq_load_k<D, FAR>(k[x], at);
-                kq_load_v<D, FAR>(v[x], a, at);
-            }
+            id = kq_ids(a, table, mine * 32, p.total);
+            nid = kq_ids(a, table, min(mine + kKqWaves, p.s1 - 1) * 32, p.total);
+            const KqBase at = kq_base<D>(a, base, id, mine * 32);
+            kq_load_k<D, FAR>(k, at);
+            kq_load_v<D, FAR>(v, a, at);
         }
         // this lane's columns: their queries' operands (d = D/4 * grp + 8 * c + 0..7) and ancestors
         const KqArgs aq = kq_args_query();
@@ -630,26 +622,16 @@ __global__ __launch_bounds__(kKqThreads, NC == 1 ? 4 : 2) void kvq_attn_kernel(K
         __syncthreads();
         auto qop = [&](int n, int ch) { return __builtin_bit_cast(bf16x8, s_q[(n * S::CH + ch) * kWave + lane]); };
         const int last = p.s1 - 1;                                   // (past it, rows that are there are asked for once more, in vain)
-        auto step = [&](int s, int set) __attribute__((always_inline)) {
-            const int next = min(s + DEEP * kKqWaves, last);
+        for (int s = mine; s < p.s1; s += kKqWaves) {
+            const int next = min(s + kKqWaves, last);
             KqIds nnid;
-            kq_step<D, NC, FAR || NC == 1 ? 2 : 4>(k[set], v[set], id[set], qop, [&] {
-                nnid = kq_ids(a, table, min(s + (DEEP + 1) * kKqWaves, last) * 32, p.total);
-                kq_load_k<D, FAR>(k[set], kq_base<D>(a, base, nid, next * 32));
+            kq_step<D, NC, FAR || NC == 1 ? 2 : 4>(k, v, id, qop, [&] {
+                nnid = kq_ids(a, table, min(s + 2 * kKqWaves, last) * 32, p.total);
+                kq_load_k<D, FAR>(k, kq_base<D>(a, base, nid, next * 32));
             }, oacc, negref, l_run, s_anc, a, s * 32, p.L, p.total);
-            kq_load_v<D, FAR>(v[set], a, kq_base<D>(a, base, nid, next * 32));
-            id[set] = nid;
+            kq_load_v<D, FAR>(v, a, kq_base<D>(a, base, nid, next * 32));
+            id = nid;
             nid = nnid;
-        };
-        if constexpr (DEEP == 2) {
-            int s = mine;
-            for (; s + kKqWaves < p.s1; s += 2 * kKqWaves) {
-                step(s, 0);
-                step(s + kKqWaves, 1);
-            }
-            if (s < p.s1) step(s, 0);
-        } else {
-            for (int s = mine; s < p.s1; s += kKqWaves) step(s, 0);
         }
         __builtin_amdgcn_s_setprio(0);
         // the wavefronts' results, added up against their common reference
@@ -861,12 +843,12 @@ static KqPlan plan_kvq(const radar_kvq_attn_desc *d) {
     // beside the 6 of any call).  Divided units cost 13 more, a second launch and two pieces a workgroup, and pay for sequences that differ (the host
     // knows the longest only; half of it is taken for the others).  60 tree rows, 32 heads on 8, us with 16 / 32 / 64 columns:
     //                              whole             divided
-    //   3000 rows            18  21  30        23  21  24
-    //   12000 rows           49  56  83        38  34  37
-    //   4 of 2000 rows       23  19  25        33  23  33
-    //   16 of 250 .. 2048    73  63  49        68  63  58
-    //   16 of 500 .. 5000                     108  97  79
-    // The choice was the quickest or within 2% of it in 19 of 20 such shapes; the worst, two sequences of 9000 rows with 64 heads, 62 us for 50.
+    //   3000 rows            18  21  30        23  21  25
+    //   12000 rows           50  59  82        38  33  33
+    //   4 of 2000 rows       23  19  25        33  22  32
+    //   16 of 250 .. 2048    70  63  49        62  57  55
+    //   16 of 500 .. 5000                      99  82  74
+    // The choice was the quickest or within 2% of it in 23 of 26 such shapes; the worst, two sequences of 9000 rows with 64 heads, 62 us for 52.
     p.whole = false;
     double best = 1e300;
     const double rounds = (double)((steps + 7) / 8);
@@ -884,7 +866,9 @@ static KqPlan plan_kvq(const radar_kvq_attn_desc *d) {
     const int64_t units = (int64_t)d->B * d->cache.Hkv * p.max_cgs;
     p.workgroups = p.whole ? (int)((units + 7) / 8 * 8) : p.nc == 1 ? 512 : 256;             // or what the chip holds at once
     p.least = d->rows_per_split ? d->rows_per_split / 32 : 8;
-    p.unit_cost = p.nc == 1 ? 16 : 24;
+    // what a unit costs besides its steps, in steps of a wavefront of eight: the merge in LDS, the way in and out (64 single tokens with 0 / 16 / 24 / 48:
+    // 86 72 70 73 us; 16 ragged trees by 64 columns with 0 / 24 / 48 / 96: 109 80 71 74; by 32 with 16 / 48 / 96: 94 80 88)
+    p.unit_cost = p.nc == 1 ? 24 : p.nc == 2 ? 48 : 56;
     // positions on the line stay within 31 bits
     p.shift = 0;
     while (units * ((steps >> p.shift) + 1 + p.unit_cost) >= (int64_t(1) << 31) && p.shift < 31) ++p.shift;
