@@ -753,6 +753,10 @@ def radar_kvq_blocks(ctx_lens, tables, T, n_new=None, slots=None, granted=None, 
     """Room for T (n_new i32 [B]: so many) new rows of every sequence behind its ctx_lens i32 [B] rows (negative: it has ended) in
     `tables` (KvqTables, updated; owned and n_free too unless owned_out and n_free_out are given).
     Returns (slots i32 [B,T], granted i32 [B])."""
+    if slots is not None and granted is not None and (native := _direct(prepared)) and native.kvq_blocks(
+            ctx_lens, n_new, tables.block_tables, tables.owned, tables.free_blocks, tables.n_free, tables.owned if owned_out is None else owned_out,
+            tables.n_free if n_free_out is None else n_free_out, slots, granted, T, tables.block_rows):
+        return slots, granted
     B, M = tables.block_tables.shape
     dev = ctx_lens.device
     for t, shape, name in ((ctx_lens, (B,), "ctx_lens"), (n_new, (B,), "n_new"), (tables.owned, (B,), "owned"), (owned_out, (B,), "owned_out"),
@@ -799,6 +803,8 @@ def _layer(cache, layer):
 def radar_kvq_append(cache, k, v, slots, layer=0, prepared=False):
     """k, v bf16 [..., Hkv, D] (one row axis of any number of dimensions, evenly spaced: a slice of a projection's output will do; the same
     strides for both, D contiguous); slots i32, as many as rows.  Writes the rows into `layer` of the KvqCache; returns it."""
+    if (native := _direct(prepared)) and native.kvq_append(cache.data, cache.block_rows, cache.D, k, v, slots, layer):
+        return cache
     if tuple(k.shape) != tuple(v.shape) or tuple(k.shape[-2:]) != (cache.Hkv, cache.D) or k.dim() < 3:
         raise ValueError(f"k, v: expected [..., {cache.Hkv}, {cache.D}], got {tuple(k.shape)} and {tuple(v.shape)}")
     N = k.numel() // (cache.Hkv * cache.D)
@@ -840,6 +846,9 @@ def radar_kvq_read(cache, slots, k=None, v=None, layer=None, prepared=False):
 def radar_kvq_commit(cache, block_tables, ctx_lens, accept_len, accept_path, new_ctx_lens=None, prepared=False):
     """The accepted path's rows of every layer into place: accept_len i32 [B], accept_path i32 [B, D_max+1] as radar_verify_accept
     gives them; block_tables i32 [B,M], ctx_lens i32 [B].  Returns new_ctx_lens i32 [B] (not ctx_lens itself)."""
+    if new_ctx_lens is not None and (native := _direct(prepared)) and native.kvq_commit(
+            cache.data, cache.block_rows, cache.D, block_tables, ctx_lens, accept_len, accept_path, new_ctx_lens):
+        return new_ctx_lens
     B, M = block_tables.shape
     _sized(ctx_lens, (B,), "ctx_lens"), _sized(accept_len, (B,), "accept_len"), _sized(new_ctx_lens, (B,), "new_ctx_lens")
     if accept_path.dim() != 2 or accept_path.shape[0] != B:
@@ -879,6 +888,11 @@ def radar_tree_attention_kvq(q, cache, block_tables, ctx_lens, parents=None, n_n
     """radar_tree_attention over `layer` of a KvqCache: q bf16 [B,T,Hq,D]; block_tables i32 [B,M]; ctx_lens i32 [B]; parents i32 [B,T]
     or None (a chain); n_nodes i32 [B] or None; S_max: the rows in use (the longest ctx_lens + T), default all that the tables
     hold.  Returns out bf16 [B,T,Hq,D]."""
+    if workspace is not None and S_max != 0 and (native := _direct(prepared)):
+        done = native.tree_attention_kvq(q, cache.data, cache.block_rows, cache.D, block_tables, ctx_lens, parents, n_nodes, layer, S_max or 0, out, lse_out,
+                                         workspace, rows_per_split, softmax_scale)
+        if done is not None:
+            return done
     if q.dim() != 4 or q.shape[3] != cache.D or q.stride(3) != 1:
         raise ValueError(f"q: expected [B, T, Hq, {cache.D}], the innermost axis contiguous")
     B, T, Hq, _ = q.shape

@@ -38,6 +38,10 @@ struct Library {
     decltype(&radar_verify_accept_q) verify_accept_q;
     decltype(&radar_accept_length_distribution) accept_length_distribution;
     decltype(&radar_policy_step) policy_step;
+    decltype(&radar_kvq_blocks) kvq_blocks;
+    decltype(&radar_kvq_append) kvq_append;
+    decltype(&radar_kvq_commit) kvq_commit;
+    decltype(&radar_tree_attention_kvq) tree_attention_kvq;
 } lib;
 
 // Reads a call's arguments in order; `ok` turns false at the first one that does not fit.
@@ -357,6 +361,127 @@ PyObject *policy_step(PyObject *, PyObject *const *args, Py_ssize_t n) {
                                 Reader::pointer<float>(u), ho, co, lg, pr, act, (int32_t)B, stream()));
 }
 
+// What the paged cache's calls check beside types: every tensor on the current device, and of these sizes.
+bool here(std::initializer_list<const at::Tensor *> all) {
+    const auto device = c10::hip::getCurrentHIPStream().device_index();
+    for (const at::Tensor *t : all)
+        if (t && t->get_device() != device) return false;
+    return true;
+}
+bool sized(const at::Tensor *t, std::initializer_list<int64_t> sizes) { return t == nullptr || t->sizes() == at::IntArrayRef(sizes.begin(), sizes.size()); }
+
+// A KvqCache: its tensor (whose layers it has found to lie apart), block_rows, D
+const at::Tensor *read_cache(Reader &r, radar_kvq_desc *d) {
+    const at::Tensor *data = r.tensor(at::kByte, false);
+    d->block_rows = r.integer(); d->D = r.integer();
+    if (!r.ok || data->dim() != 4 || data->size(3) != (int64_t)d->block_rows * (d->D + d->D / 16) || data->stride(3) != 1 ||
+        data->stride(2) != data->size(3) || data->stride(1) != data->size(2) * data->size(3) || data->size(0) > INT32_MAX || data->size(1) > INT32_MAX)
+        return r.fail();
+    d->layers = (int32_t)data->size(0); d->n_blocks = (int32_t)data->size(1); d->Hkv = (int32_t)data->size(2);
+    d->layer_stride = d->layers > 1 ? data->stride(0) : 0;
+    return data;
+}
+char *layer_of(const at::Tensor *data, int32_t layer) { return static_cast<char *>(data->data_ptr()) + layer * data->stride(0); }
+
+// ctx_lens, n_new, block_tables, owned, free_blocks, n_free, owned_out, n_free_out, slots, granted, T, block_rows
+PyObject *kvq_blocks(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    Reader r(args, n);
+    const at::Tensor *ctx = r.i32(), *fresh = r.i32(true), *tables = r.i32(), *owned = r.i32(), *free_blocks = r.i32(), *n_free = r.i32();
+    const at::Tensor *owned_out = r.i32(), *n_free_out = r.i32(), *slots = r.i32(), *granted = r.i32();
+    radar_kvq_blocks_desc d{};
+    d.T_max = r.integer(); d.block_rows = r.integer();
+    if (!r.ok || tables->dim() != 2 || free_blocks->dim() != 1 || free_blocks->numel() > INT32_MAX) Py_RETURN_NONE;
+    const int64_t B = tables->size(0);
+    d.B = (int32_t)B; d.max_blocks = (int32_t)tables->size(1); d.n_blocks = (int32_t)free_blocks->numel();
+    for (const at::Tensor *t : {ctx, fresh, owned, owned_out, granted})
+        if (!sized(t, {B})) Py_RETURN_NONE;
+    if (!sized(n_free, {1}) || !sized(n_free_out, {1}) || !sized(slots, {B, d.T_max}) ||
+        !here({ctx, fresh, tables, owned, free_blocks, n_free, owned_out, n_free_out, slots, granted})) Py_RETURN_NONE;
+    auto p = [](const at::Tensor *t) { return Reader::pointer<int32_t>(t); };
+    return done(call(lib.kvq_blocks, p(ctx), p(fresh), p(tables), p(owned), p(free_blocks), p(n_free), p(owned_out), p(n_free_out), p(slots), p(granted),
+                     &d, stream()));
+}
+
+// cache, k, v, slots, layer
+PyObject *kvq_append(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    Reader r(args, n);
+    radar_kvq_desc d{};
+    const at::Tensor *data = read_cache(r, &d), *k = r.tensor(at::kBFloat16, false), *v = r.tensor(at::kBFloat16, false), *slots = r.i32();
+    const int32_t layer = r.integer();
+    if (!r.ok || layer < 0 || layer >= d.layers || k->dim() < 3 || k->sizes() != v->sizes() || k->strides() != v->strides() || !here({data, k, v, slots}))
+        Py_RETURN_NONE;
+    const int64_t dims = k->dim();
+    if (k->size(dims - 2) != d.Hkv || k->size(dims - 1) != d.D || k->stride(dims - 1) != 1 || k->numel() == 0 || slots->numel() * d.Hkv * d.D != k->numel())
+        Py_RETURN_NONE;
+    int64_t first = 0, step = 0;                                     // the leading dimensions as one evenly spaced axis
+    for (int64_t i = dims - 3; i >= 0; --i) {
+        if (k->size(i) == 1) continue;
+        if (k->stride(i) == 0 || (step != 0 && k->stride(i) != step)) Py_RETURN_NONE;
+        if (step == 0) first = k->stride(i);
+        step = k->stride(i) * k->size(i);
+    }
+    const int64_t head = d.Hkv > 1 ? k->stride(dims - 2) : 0;
+    if (d.Hkv > 1 && head == 0) Py_RETURN_NONE;
+    return done(call(lib.kvq_append, k->data_ptr(), v->data_ptr(), Reader::pointer<int32_t>(slots), layer_of(data, layer), slots->numel(), first, head, &d,
+                     stream()));
+}
+
+// cache, block_tables, ctx_lens, accept_len, accept_path, new_ctx_lens
+PyObject *kvq_commit(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    Reader r(args, n);
+    radar_kvq_desc d{};
+    const at::Tensor *data = read_cache(r, &d), *tables = r.i32(), *ctx = r.i32(), *len = r.i32(), *path = r.i32(), *out = r.i32();
+    if (!r.ok || tables->dim() != 2 || path->dim() != 2) Py_RETURN_NONE;
+    const int64_t B = tables->size(0);
+    if (!sized(ctx, {B}) || !sized(len, {B}) || !sized(out, {B}) || path->size(0) != B || path->size(1) > INT32_MAX || B > INT32_MAX ||
+        !here({data, tables, ctx, len, path, out})) Py_RETURN_NONE;
+    auto p = [](const at::Tensor *t) { return Reader::pointer<int32_t>(t); };
+    return done(call(lib.kvq_commit, data->data_ptr(), p(tables), (int32_t)tables->size(1), p(ctx), p(len), p(path), (int32_t)path->size(1), (int32_t)B,
+                     p(out), &d, stream()));
+}
+
+// q, cache, block_tables, ctx_lens, parents, n_nodes, layer, S_max (0: all that the tables hold), out (None: allocated here), lse_out, workspace,
+// rows_per_split, softmax_scale -> out
+PyObject *tree_attention_kvq(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    Reader r(args, n);
+    const at::Tensor *q = r.tensor(at::kBFloat16, false);
+    radar_kvq_attn_desc d{};
+    const at::Tensor *data = read_cache(r, &d.cache), *tables = r.i32(), *ctx = r.i32(), *parents = r.i32(true), *nodes = r.i32(true);
+    const int32_t layer = r.integer();
+    d.S_max = r.integer();
+    PyObject *out_obj = r.peek();
+    const at::Tensor *out = r.tensor(at::kBFloat16, false, true);
+    const at::Tensor *lse = r.f32(true);
+    void *ws; size_t ws_bytes;
+    const at::Tensor *room = nullptr;
+    if (PyObject *o = r.peek(); o != nullptr && THPVariable_Check(o)) room = &THPVariable_Unpack(o);
+    r.workspace(&ws, &ws_bytes);
+    d.rows_per_split = r.integer();
+    d.softmax_scale = r.real();
+    if (!r.ok || q->dim() != 4 || q->size(3) != d.cache.D || q->stride(3) != 1 || layer < 0 || layer >= d.cache.layers || tables->dim() != 2) Py_RETURN_NONE;
+    const int64_t B = q->size(0), T = q->size(1), H = q->size(2), M = tables->size(1);
+    if (tables->size(0) != B || !sized(ctx, {B}) || !sized(nodes, {B}) || !sized(parents, {B, T}) || !sized(lse, {B, T, H}) ||
+        (out && (out->sizes() != q->sizes() || out->stride(3) != 1)) || !here({q, data, tables, ctx, parents, nodes, out, lse, room})) Py_RETURN_NONE;
+    if (d.S_max == 0) {
+        if (M * d.cache.block_rows > INT32_MAX) Py_RETURN_NONE;
+        d.S_max = (int32_t)(M * d.cache.block_rows);
+    }
+    d.B = (int32_t)B; d.T_max = (int32_t)T; d.Hq = (int32_t)H; d.max_blocks = (int32_t)M;
+    at::Tensor fresh;
+    if (out == nullptr) { fresh = at::empty(q->sizes(), q->options().memory_format(c10::nullopt)); out = &fresh; }
+    int64_t *const qs[] = {&d.q_stride_b, &d.q_stride_t, &d.q_stride_h}, *const os[] = {&d.out_stride_b, &d.out_stride_t, &d.out_stride_h};
+    for (int i = 0; i < 3; ++i) {
+        if (q->size(i) == 1) continue;
+        if (q->stride(i) == 0 || out->stride(i) == 0) Py_RETURN_NONE;
+        *qs[i] = q->stride(i); *os[i] = out->stride(i);
+    }
+    const radar_status rc = call(lib.tree_attention_kvq, q->data_ptr(), layer_of(data, layer), Reader::pointer<int32_t>(tables), Reader::pointer<int32_t>(parents),
+                                 Reader::pointer<int32_t>(ctx), Reader::pointer<int32_t>(nodes), out->data_ptr(), Reader::pointer<float>(lse), &d, ws, ws_bytes,
+                                 stream());
+    if (rc != RADAR_OK) Py_RETURN_NONE;
+    return fresh.defined() ? THPVariable_Wrap(std::move(fresh)) : done(rc, out_obj);
+}
+
 // the library's path: looks its entry points up (it is the copy that ctypes has loaded already)
 PyObject *bind(PyObject *, PyObject *path) {
     const char *p = PyUnicode_AsUTF8(path);
@@ -380,6 +505,10 @@ PyObject *bind(PyObject *, PyObject *path) {
     find(lib.verify_accept_q, "radar_verify_accept_q");
     find(lib.accept_length_distribution, "radar_accept_length_distribution");
     find(lib.policy_step, "radar_policy_step");
+    find(lib.kvq_blocks, "radar_kvq_blocks");
+    find(lib.kvq_append, "radar_kvq_append");
+    find(lib.kvq_commit, "radar_kvq_commit");
+    find(lib.tree_attention_kvq, "radar_tree_attention_kvq");
     if (!all) { PyErr_Format(PyExc_RuntimeError, "%s lacks an entry point", p); return nullptr; }
     Py_RETURN_NONE;
 }
@@ -387,7 +516,7 @@ PyObject *bind(PyObject *, PyObject *path) {
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<name>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     FAST(tree_attention), FAST(draft_expand), FAST(draft_rerank), FAST(verify_accept), FAST(verify_accept_q),
-    FAST(accept_length_distribution), FAST(policy_step),
+    FAST(accept_length_distribution), FAST(policy_step), FAST(kvq_blocks), FAST(kvq_append), FAST(kvq_commit), FAST(tree_attention_kvq),
     {"bind", bind, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "argument marshalling of the hot calls", -1, methods, nullptr, nullptr, nullptr, nullptr};

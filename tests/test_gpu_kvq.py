@@ -647,3 +647,71 @@ def test_prepared_calls_are_the_same_calls():
     for _ in range(3):
         call.out.zero_()
         assert call() is call.out and torch.equal(call.out, want)
+
+
+def test_direct_calls_by_the_native_half(monkeypatch):
+    """Direct calls whose buffers are all given are marshalled natively; they do what ctypes makes them do.  What the native half does not take
+    reaches the other's checks."""
+    from test_gpu_support import _Both
+    b, rng = binding(), seed(96)
+    both = _Both(b, monkeypatch)
+    ctx, T, nodes, Hq, H, D, R = np.array([77, 31], np.int32), 8, np.array([8, 5], np.int32), 8, 2, 128, 16
+    tables, cache, q, qb, par = make_attention(rng, ctx, T, nodes, Hq, H, D, R, layers=3)
+    M, n_blocks = tables.shape[1], cache.shape[1]
+    fused = torch.randn((2, T, Hq + 2 * H, D), device="cuda").bfloat16()
+    fused[:, :, :Hq] = bf16_dev(qb)
+    dq, dk, dv, dt, dc, dp, dn = fused[:, :, :Hq], fused[:, :, Hq:Hq + H], fused[:, :, Hq + H:], dev(tables), dev(ctx), dev(par), dev(nodes)
+    slots = dev(np.stack([[kvq.row_slot(tables[bb], R, n_blocks, int(ctx[bb]) + i) for i in range(T)] for bb in range(2)]).astype(np.int32))
+    wide = torch.zeros((3, cache[0].size + 64), dtype=torch.uint8, device="cuda")
+
+    def fresh(spread=False):
+        if not spread:
+            return gpu_cache(cache, R, D)
+        wide[:, :cache[0].size] = dev(cache.reshape(3, -1))
+        return b.KvqCache(data=wide[:, :cache[0].size].view(cache.shape), block_rows=R, D=D)
+
+    for spread in (False, True):
+        for k, v in ((dk, dv), (dk.contiguous(), dv.contiguous()), (dk[:1, 3:4], dv[:1, 3:4])):
+            def append():
+                c = fresh(spread)
+                assert b.radar_kvq_append(c, k, v, slots.view(-1)[:k.shape[0] * k.shape[1]], layer=1) is c
+                return [c.data.clone()]
+            both("append", append)
+
+        def commit():
+            c, new = fresh(spread), torch.full((2,), 9, dtype=torch.int32, device="cuda")
+            path = dev(np.array([[0, 2, 5], [0, 3, 4]], np.int32))
+            assert b.radar_kvq_commit(c, dt, dc, dev(np.array([2, 1], np.int32)), path, new_ctx_lens=new) is new
+            return [c.data.clone(), new]
+        both("commit", commit)
+        c = fresh(spread)
+        ws = b.new_workspace(b.radar_tree_attention_kvq_workspace_bytes(b.kvq_attn_desc(dq, c, M, rows_per_split=64)))
+        room = torch.zeros((2, Hq, T, D), dtype=torch.bfloat16, device="cuda")
+        for parents, n, S, out, split, scale in ((dp, dn, None, None, 0, 0.0), (dp, dn, 90, "own", 64, 0.2), (None, None, 90, None, 64, 0.0)):
+            def attend():
+                lse = torch.full((2, T, Hq), 7.0, device="cuda")
+                o = room.zero_().transpose(1, 2) if out else None
+                got = b.radar_tree_attention_kvq(dq, c, dt, dc, parents, n, layer=2, S_max=S, out=o, lse_out=lse, workspace=ws, rows_per_split=split,
+                                                 softmax_scale=scale)
+                assert o is None or got is o
+                return [got.clone(), lse]
+            both("attention", attend)
+
+    def blocks():
+        t = b.KvqTables(2, M, n_blocks, R)
+        s, g = torch.full((2, T), 5, dtype=torch.int32, device="cuda"), torch.full((2,), 5, dtype=torch.int32, device="cuda")
+        got = b.radar_kvq_blocks(dc, t, T, n_new=dn, slots=s, granted=g)
+        assert got[0] is s and got[1] is g
+        return [s, g, t.block_tables, t.owned, t.free_blocks, t.n_free]
+    both("blocks", blocks)
+    both.native = True
+    c = fresh()
+    for bad in (lambda: b.radar_kvq_append(c, dk.float(), dv.float(), slots), lambda: b.radar_kvq_append(c, dk, dv, slots[:1]),
+                lambda: b.radar_kvq_append(c, dk, dv, slots, layer=3), lambda: b.radar_kvq_append(c, dk[:1].expand(2, T, H, D), dv[:1].expand(2, T, H, D), slots),
+                lambda: b.radar_kvq_commit(c, dt, dc[:1], dc, slots, new_ctx_lens=dn), lambda: b.radar_tree_attention_kvq(dq, c, dt, dc, dp[:, :3], dn, workspace=ws),
+                lambda: b.radar_tree_attention_kvq(dq[:1].expand(2, T, Hq, D), c, dt, dc, dp, dn, workspace=ws),
+                lambda: b.radar_kvq_blocks(dc, b.KvqTables(3, M, n_blocks, R), T, slots=slots, granted=dn)):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(b.RadarError):
+        b.radar_tree_attention_kvq(dq, c, dt, dc, dp, dn, S_max=M * R + 1, workspace=ws)

@@ -175,6 +175,21 @@ def test_the_binding_raises():
     assert t.free_blocks.tolist() == list(range(8, -1, -1)) and t.n_free.tolist() == [9] and (t.block_tables == -1).all()
 
 
+def test_the_native_half_returns_none(lib):
+    """Whatever it cannot take: tensors that are not on a GPU, other objects, too few of them, sizes that are none."""
+    from paper_2512_14069_amd import binding as b
+    n, i32 = b._native, torch.zeros((2, 2), dtype=torch.int32)
+    cache, x = torch.zeros((1, 4, 2, 16 * 136), dtype=torch.uint8), torch.zeros((3, 2, 128), dtype=torch.bfloat16)
+    calls = ((n.kvq_blocks, [i32] * 10 + [8, 16]), (n.kvq_append, [cache, 16, 128, x, x, i32, 0]), (n.kvq_commit, [cache, 16, 128] + [i32] * 5),
+             (n.tree_attention_kvq, [x, cache, 16, 128, i32, i32, None, None, 0, 0, None, None, i32, 0, 0.0]))
+    for f, args in calls:
+        assert f(*args) is None and f() is None
+        for i in range(len(args)):
+            assert f(*args[:i]) is None
+            for other in (None, "no", 1 << 70, -1, object(), x, i32):
+                assert f(*args[:i], other, *args[i + 1:]) is None
+
+
 def test_under_sanitizers():
     if os.environ.get("RADAR_LIB_SANITIZE") == "1":
         pytest.skip("this is the sanitized run")
