@@ -43,9 +43,10 @@ struct KqArgs {
     float scale_log2;
     int64_t block_bytes;                       // of a block, all heads
     int workgroups, least, shift, max_cgs;     // least share of the line; log2 steps per unit of it; column blocks of a KV head
-    int unit_cost, whole;                      // what a unit costs besides its steps; whole: a workgroup for each unit, no line
+    int unit_cost, whole;                      // what a unit costs besides its steps; whole: no line, 2^(whole - 1) workgroups for each unit
     float *part;                               // [2 * workgroups] partial results: outputs, maxima (log2 units), sums, in fp32
     uint32_t *unit_tab;                        // first and last workgroup of a unit; alike: it is written already
+    unsigned int *arrived;                     // of a unit's workgroups, kKqArrived words apart
 };
 
 // A sequence: rows of its prefix, nodes of its tree, rows that may be attended to.  There is none: nn = 0.
@@ -225,6 +226,8 @@ __device__ __forceinline__ uint32_t kq_allowed(uint64_t anc, int first) {
 // take 128 registers, and the queries' operands stay in LDS.
 constexpr int kKqWaves = 8, kKqThreads = kKqWaves * kWave;
 constexpr float kKqMost = 2048.0f;             // what a lane's eight weights may add up to before the reference is moved
+constexpr int kKqArrived = 16;                 // counters are 64 bytes apart: atomics on one line wait for each other
+constexpr int kKqJoined = 256;                 // most workgroups of units that several take
 constexpr float kKqNone = 3.0e38f;             // negated reference of a column that has seen no key yet
 
 template <int D, int NC>
@@ -236,7 +239,7 @@ struct KqShape {
     static constexpr int q_bytes() { return COLS * D * 2; }
     static constexpr int merge_bytes() { return kKqWaves * COLS * ROW * 4; }
     static constexpr int lds_bytes() { return merge_bytes() + (kKqWaves + 2) * COLS * 8 + kKqWaves * 64 + q_bytes(); }
-    static constexpr int PART = COLS * D + 2 * COLS;                 // floats of a partial result: outputs, maxima, sums
+    static constexpr int PART = COLS * D + 2 * COLS;                 // floats of a partial result: outputs, maxima and sums in pairs
 };
 
 // One wavefront, one step: scores of 32 keys, softmax against the running reference, outputs.  The loads of the wavefront's next step are
@@ -444,7 +447,7 @@ __device__ __forceinline__ void kq_plan_chunk(KqChunkPlan &c, const KqArgs &a, i
 
 // A workgroup's place on the line and its piece, which wait in LDS (every wavefront has its own copy) while the loop needs the scalar registers.
 struct KqPlace { uint32_t pos, end, share; int b0; uint32_t base, number; };       // number: of its share
-struct KqPiece { int b, hk, cg, nn, slot, L, total, s0, s1; };       // slot: of its partial result, -1: it is all of its unit
+struct KqPiece { int b, hk, cg, nn, slot, L, total, s0, s1, parts; };        // slot: of its partial result, -1: it is all of its unit
 constexpr int kKqState = 16;                   // words of a wavefront's copy: the place, then the piece
 template <typename T>
 __device__ __forceinline__ T kq_recall(const int *from) {            // the same in every lane
@@ -490,6 +493,7 @@ __device__ __forceinline__ KqArgs kq_args_end() {
     KqArgs a;
     a.out = g->out; a.o_sb = g->o_sb; a.o_st = g->o_st; a.o_sh = g->o_sh; a.lse = g->lse; a.G = g->G; a.T = g->T; a.Hq = g->Hq; a.part = g->part;
     a.ctx_lens = g->ctx_lens; a.n_nodes = g->n_nodes; a.S = g->S; a.B = g->B; a.workgroups = g->workgroups;
+    a.whole = g->whole; a.arrived = g->arrived;
     return a;
 }
 
@@ -506,23 +510,27 @@ __global__ __launch_bounds__(kKqThreads, NC == 1 ? 4 : 2) void kvq_attn_kernel(K
     const int lane = lane_id(), w = __builtin_amdgcn_readfirstlane(wave_id()), r = lane & 15, grp = lane >> 4;
     int *const state = s_state + w * kKqState;
 
-    // A workgroup for each unit: nothing to work out but which, and the only sequence's lengths.
+    // A workgroup, or as many as `parts`, for each unit: nothing to work out but which, and the only sequence's lengths.
     auto whole_piece = [&]() -> bool {
         const KqArgs a = kq_args_plan();
-        const uint32_t units = (uint32_t)(a.B * a.Hkv * a.max_cgs), u = kq_share_of(units);
-        if (u >= units) return false;
+        const int bits = a.whole - 1;
+        const uint32_t n = (uint32_t)(a.B * a.Hkv * a.max_cgs) << bits, u = kq_share_of(n), unit = u >> bits;
+        if (u >= n) return false;
         KqPiece p;
-        const uint32_t bh = u / (uint32_t)a.max_cgs;
-        p.cg = (int)__builtin_amdgcn_readfirstlane(u - bh * (uint32_t)a.max_cgs);
+        const uint32_t bh = unit / (uint32_t)a.max_cgs;
+        p.cg = (int)__builtin_amdgcn_readfirstlane(unit - bh * (uint32_t)a.max_cgs);
         p.b = (int)__builtin_amdgcn_readfirstlane(bh / (uint32_t)a.Hkv);
         p.hk = (int)__builtin_amdgcn_readfirstlane(bh) - p.b * a.Hkv;
         p.L = min(uniform_word(a.ctx_lens, p.b), a.S);               // (kq_seq)
         p.nn = a.n_nodes ? max(1, min(uniform_word(a.n_nodes, p.b), a.T)) : a.T;
         if (p.L < 0) p.nn = 0;
         p.total = p.L < 0 ? 0 : min(p.L + p.nn, a.S);
-        p.s0 = 0;
-        p.s1 = p.cg * S::COLS < p.nn * a.G ? (p.total + 31) >> 5 : 0;
-        p.slot = -1;
+        const int steps = p.cg * S::COLS < p.nn * a.G ? (p.total + 31) >> 5 : 0, per = (steps + (1 << bits) - 1) >> bits;
+        p.s0 = (int)(u & ((1u << bits) - 1)) * max(per, 1);
+        p.s1 = min(p.s0 + per, steps);
+        if (p.s0 > 0 && p.s0 >= steps) return false;                 // (a unit without steps has its first workgroup, for the zeros)
+        p.parts = per > 0 ? (int)__builtin_amdgcn_readfirstlane((uint32_t)(steps + per - 1) / (uint32_t)per) : 1;
+        p.slot = p.parts > 1 ? (int)u : -1;
         kq_remember(state + sizeof(KqPlace) / 4, p);
         return true;
     };
@@ -566,6 +574,7 @@ __global__ __launch_bounds__(kKqThreads, NC == 1 ? 4 : 2) void kvq_attn_kernel(K
             const int steps = (p.total + 31) >> 5;
             p.s0 = min((int)(from > cost ? (from - cost) << a.shift : 0u), steps);
             p.s1 = min((int)((to - cost) << a.shift), steps);
+            p.parts = 1;
             p.slot = from <= cost && to == len ? -1 : 2 * (int)x.number + (to < len ? 1 : 0);
             if (from <= cost && threadIdx.x == 0)       // for the merge: first and last workgroup
                 a.unit_tab[(p.b * a.Hkv + p.hk) * a.max_cgs + p.cg] = p.slot < 0 ? 0u : x.number << 16 | ((at + len - 1) / x.share);
@@ -686,12 +695,14 @@ __global__ __launch_bounds__(kKqThreads, NC == 1 ? 4 : 2) void kvq_attn_kernel(K
             int lane2 = threadIdx.x;
             asm volatile("" : "+v"(lane2));
             const int mc = lane2 / TPC, mx = lane2 % TPC * 4, gc = p.cg * S::COLS + mc, mi = gc / a.G, mh = p.hk * a.G + gc - mi * a.G;
-            if (whole && mc < S::COLS && mi >= p.nn && mi < a.T) {   // rows behind the tree's end: zeros
+            if (whole && mc < S::COLS && mi >= p.nn) {               // rows behind the tree's end: zeros
 #pragma unroll
                 for (int z = 0; z < IPT; ++z) {
                     const int x = z * TPC * 4 + mx, d = D / 4 * (x / (S::EP * S::NM)) + pass * S::EP * S::NM + x % (S::EP * S::NM);
-                    *reinterpret_cast<u32x2 *>(a.out + (size_t)p.b * a.o_sb + (size_t)mi * a.o_st + (size_t)mh * a.o_sh + d) = u32x2{0, 0};
-                    if (a.lse && d == 0) a.lse[((size_t)p.b * a.T + mi) * a.Hq + mh] = 0.f;
+                    if (mi < a.T && p.s0 == 0) {
+                        *reinterpret_cast<u32x2 *>(a.out + (size_t)p.b * a.o_sb + (size_t)mi * a.o_st + (size_t)mh * a.o_sh + d) = u32x2{0, 0};
+                        if (a.lse && d == 0) a.lse[((size_t)p.b * a.T + mi) * a.Hq + mh] = 0.f;
+                    }
                 }
             } else if (mc < S::COLS && (p.slot >= 0 || mi < p.nn)) {
                 const float M = s_M[mc], l = s_L[mc];
@@ -706,10 +717,15 @@ __global__ __launch_bounds__(kKqThreads, NC == 1 ? 4 : 2) void kvq_attn_kernel(K
                     floatx4 acc = o[z][0];
 #pragma unroll
                     for (int y = 1; y < kKqWaves; ++y) acc += o[z][y];
-                    if (p.slot >= 0) {
-                        float *const to = a.part + (size_t)p.slot * S::PART;
+                    float *const to = a.part + (size_t)p.slot * S::PART;
+                    if (p.parts > 1) {
+                        const float a0 = acc[0], a1 = acc[1], a2 = acc[2], a3 = acc[3];
+                        store_shared_result(reinterpret_cast<uint64_t *>(to + mc * D + d), (uint64_t)__float_as_uint(a1) << 32 | __float_as_uint(a0));
+                        store_shared_result(reinterpret_cast<uint64_t *>(to + mc * D + d + 2), (uint64_t)__float_as_uint(a3) << 32 | __float_as_uint(a2));
+                        if (d == 0) store_shared_result(reinterpret_cast<uint64_t *>(to + S::COLS * D + 2 * mc), (uint64_t)__float_as_uint(l) << 32 | __float_as_uint(M));
+                    } else if (p.slot >= 0) {
                         *reinterpret_cast<floatx4 *>(to + mc * D + d) = acc;
-                        if (d == 0) { to[S::COLS * D + mc] = M; to[S::COLS * D + S::COLS + mc] = l; }
+                        if (d == 0) { to[S::COLS * D + 2 * mc] = M; to[S::COLS * D + 2 * mc + 1] = l; }
                     } else {
                         kq_write(a, p.b, mi, mh, d, acc, M, l);
                     }
@@ -717,6 +733,47 @@ __global__ __launch_bounds__(kKqThreads, NC == 1 ? 4 : 2) void kvq_attn_kernel(K
             }
         }
         __syncthreads();
+        if (p.parts > 1) {
+            // The unit's workgroup that arrives last has all the parts, its own among them, join.
+            const int bits = a.whole - 1, unit = p.slot >> bits;
+            unsigned int *const counter = a.arrived + unit * kKqArrived;
+            if ((int)publish_then_ticket(counter, reinterpret_cast<unsigned int *>(s_m)) != p.parts - 1) return;
+            if (threadIdx.x == 0) store_shared_result(counter, 0u);
+            const float *const from = a.part + (size_t)(unit << bits) * S::PART;
+            for (int x = threadIdx.x; x < S::COLS * D / 4; x += kKqThreads) {
+                const int mc = x / (D / 4), d = x % (D / 4) * 4, gc = p.cg * S::COLS + mc, mi = gc / a.G, mh = p.hk * a.G + gc - mi * a.G;
+                if (mi >= p.nn) continue;
+                float M = -kKqNone, l = 0.f;
+                floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+                constexpr int U = 4;
+                for (int y0 = 0; y0 < p.parts; y0 += U) {
+                    uint64_t ml[U], lo[U], hi[U];
+#pragma unroll
+                    for (int y = 0; y < U; ++y) {
+                        const float *const part = from + (size_t)min(y0 + y, p.parts - 1) * S::PART;
+                        ml[y] = load_shared_result(reinterpret_cast<const uint64_t *>(part + S::COLS * D + 2 * mc));
+                        lo[y] = load_shared_result(reinterpret_cast<const uint64_t *>(part + mc * D + d));
+                        hi[y] = load_shared_result(reinterpret_cast<const uint64_t *>(part + mc * D + d + 2));
+                    }
+                    float Mn = M;
+#pragma unroll
+                    for (int y = 0; y < U; ++y) Mn = fmaxf(Mn, __uint_as_float((uint32_t)ml[y]));
+                    const float f0 = __builtin_amdgcn_exp2f(M - Mn);
+                    M = Mn;
+                    l *= f0;
+                    acc *= f0;
+#pragma unroll
+                    for (int y = 0; y < U; ++y) {
+                        if (y0 + y >= p.parts) break;                // (the last part once more)
+                        const float f = __builtin_amdgcn_exp2f(__uint_as_float((uint32_t)ml[y]) - Mn);
+                        l += __uint_as_float((uint32_t)(ml[y] >> 32)) * f;
+                        acc += floatx4{__uint_as_float((uint32_t)lo[y]), __uint_as_float((uint32_t)(lo[y] >> 32)), __uint_as_float((uint32_t)hi[y]),
+                                       __uint_as_float((uint32_t)(hi[y] >> 32))} * f;
+                    }
+                }
+                kq_write(a, p.b, mi, mh, d, acc, M, l);
+            }
+        }
     }
 
     if (whole) return;
@@ -780,8 +837,8 @@ __global__ __launch_bounds__(GROUPS == 1 ? 256 : 1024) void kvq_merge_kernel(KqA
             const bool there = w + u * GROUPS <= w1;                 // (the same in every lane; otherwise the last part once more, as nothing)
             const int part = min(w + u * GROUPS, w1);
             const float *const from = a.part + (size_t)(2 * part + (part < w1 ? 1 : 0)) * S::PART;
-            m[u] = there ? from[S::COLS * D + col] : -kKqNone;
-            ls[u] = there ? from[S::COLS * D + S::COLS + col] : 0.f;
+            m[u] = there ? from[S::COLS * D + 2 * col] : -kKqNone;
+            ls[u] = there ? from[S::COLS * D + 2 * col + 1] : 0.f;
 #pragma unroll
             for (int x = 0; x < Q; ++x) o[u][x] = there ? *reinterpret_cast<const floatx4 *>(from + (size_t)col * D + d + 4 * x) : floatx4{0.f, 0.f, 0.f, 0.f};
         }
@@ -836,40 +893,47 @@ static radar_status check_kvq_attn(const radar_kvq_attn_desc *d) {
 
 struct KqPlan {
     int nc, max_cgs, workgroups, least, shift, unit_cost;
-    bool whole;                                            // no unit is divided: no merge
-    size_t off_tab, off_part, bytes;
+    int whole;                                             // as in KqArgs: no line, no second launch
+    size_t off_arrived, off_tab, off_part, bytes;
 };
 
 static KqPlan plan_kvq(const radar_kvq_attn_desc *d) {
     KqPlan p;
     const int cols = d->Hq / d->cache.Hkv * d->T_max, D = d->cache.D;
     const int64_t steps = ((int64_t)d->S_max + 31) / 32;
-    // Columns a workgroup, and whole units or divided ones: whichever takes less, from what rounds of steps and the rest took (us, one MI355X, D = 128,
-    // beside the 6 of any call).  Divided units cost 13 more, a second launch and two pieces a workgroup, and pay for sequences that differ (the host
-    // knows the longest only; half of it is taken for the others).  60 tree rows, 32 heads on 8, us with 16 / 32 / 64 columns:
-    //                              whole             divided
-    //   3000 rows            18  21  30        23  21  25
-    //   12000 rows           50  59  82        38  33  33
-    //   4 of 2000 rows       23  19  25        33  22  32
-    //   16 of 250 .. 2048    70  63  49        62  57  55
-    //   16 of 500 .. 5000                      99  82  74
-    // The choice was the quickest or within 2% of it in 23 of 26 such shapes; the worst, two sequences of 9000 rows with 64 heads, 62 us for 52.
-    p.whole = false;
+    // Columns a workgroup, and how units are given out: whole; to 2, 4, ... 64 workgroups each, the last of which joins their parts; or all of them in a
+    // line, in equal shares.  Whichever takes least, from what rounds of steps and the rest took (us, one MI355X, D = 128, beside the 6 of any call).
+    // The line costs 13 more, a second launch and two pieces a workgroup, and pays where units differ or would leave many workgroups without one (the
+    // host knows the longest only; half of it is taken for the others).  us with 16 / 32 / 64 columns, "-" where there are too many units to join:
+    //                                         whole       joined, by 2 ... 32                   line
+    //   1 token, 32 heads on 8, 2048 rows       13          10.8  9.3  8.9 10.2 11.4              12.5
+    //   16000 rows                              60          34  21  15.5  13.3  15.5              17
+    //   60 tree rows, 2048 rows                 14 17 24    12.5 15.9 22.9, by 4 - 14.0 20.2      21 21 25
+    //   12000 rows                              50 57 84    32 37 53, by 4 - 26 36, by 8 - - 31   38 33 34
+    //   4 sequences of 2000 rows                23 18 26    - - 25                                33 22 32
+    //   4 of 9000                               69 54 69    - - 51                                78 55 56
+    //   16 of 250 .. 2048                       70 63 49    - - -                                 62 57 55
+    //   16 of 500 .. 5000                                   - - -                                 99 82 74
+    p.whole = 0;
     double best = 1e300;
     const double rounds = (double)((steps + 7) / 8);
-    for (int i = 0; i < 6; ++i) {
-        const int x = i >> 1, nc = 1 << x;
-        const bool whole = i & 1;
-        if ((nc > 1 && cols <= 8 * nc) || (whole && d->rows_per_split != 0)) continue;
+    for (int x = 0; x < 3; ++x) {
+        const int nc = 1 << x;
+        if (nc > 1 && cols <= 8 * nc) continue;
         const double units = (double)d->B * d->cache.Hkv * ((cols + 16 * nc - 1) / (16 * nc));
         const double alone[] = {0.91, 1.05, 1.7}, shared[] = {0.8, 1.27, 2.2}, end[] = {0.0, 2.3, 4.0}, divided[] = {13.2, 12.7, 16.0};
-        const double us = whole ? std::ceil(units / 256.0) * (rounds * alone[x] + end[x])
-                                : divided[x] + units / 256.0 * ((d->B > 1 ? 0.5 : 1.0) * rounds * shared[x] + 3.0 + end[x]);
-        if (us < best) { best = us; p.nc = nc; p.whole = whole; }
+        const double few[] = {0.83, 1.0, 1.65}, many[] = {0.95, 1.27, 2.05}, join[] = {0.2, 0.35, 0.5};        // (many: more workgroups than half the CUs)
+        auto take = [&](double us, int whole) { if (us < best) { best = us; p.nc = nc; p.whole = whole; } };
+        take(divided[x] + units / 256.0 * ((d->B > 1 ? 0.5 : 1.0) * rounds * shared[x] + 3.0 + end[x]), 0);
+        if (d->rows_per_split != 0) continue;
+        take(std::ceil(units / 256.0) * (rounds * alone[x] + end[x]), 1);
+        for (int bits = 1; bits <= 6 && units * (1 << bits) <= kKqJoined; ++bits)
+            take((d->B > 1 ? 0.88 : 1.0) * (std::ceil(rounds / (1 << bits)) * (units * (1 << bits) > 128 ? many[x] : few[x]) + end[x] + 1.4 + join[x] * (1 << bits)), 1 + bits);
     }
     p.max_cgs = (cols + 16 * p.nc - 1) / (16 * p.nc);
     const int64_t units = (int64_t)d->B * d->cache.Hkv * p.max_cgs;
-    p.workgroups = p.whole ? (int)((units + 7) / 8 * 8) : p.nc == 1 ? 512 : 256;             // or what the chip holds at once
+    const int64_t parts = p.whole ? units << (p.whole - 1) : 0;
+    p.workgroups = p.whole ? (int)((parts + 7) / 8 * 8) : p.nc == 1 ? 512 : 256;             // or what the chip holds at once
     p.least = d->rows_per_split ? d->rows_per_split / 32 : 8;
     // what a unit costs besides its steps, in steps of a wavefront of eight: the merge in LDS, the way in and out (64 single tokens with 0 / 16 / 24 / 48:
     // 86 72 70 73 us; 16 ragged trees by 64 columns with 0 / 24 / 48 / 96: 109 80 71 74; by 32 with 16 / 48 / 96: 94 80 88)
@@ -879,9 +943,10 @@ static KqPlan plan_kvq(const radar_kvq_attn_desc *d) {
     while (units * ((steps >> p.shift) + 1 + p.unit_cost) >= (int64_t(1) << 31) && p.shift < 31) ++p.shift;
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t o = off; off += (bytes + 255) & ~size_t(255); return o; };
-    take(256);                                             // never empty: callers always pass a workspace
+    p.off_arrived = take(kKqJoined * kKqArrived * sizeof(unsigned int));      // first, whatever the shape: all calls leave them at zero
     p.off_tab = take(p.whole ? 0 : (size_t)units * sizeof(uint32_t));
-    p.off_part = take(p.whole ? 0 : (size_t)2 * p.workgroups * (16 * p.nc * (D + 2)) * sizeof(float));
+    const size_t slots = p.whole > 1 ? (size_t)parts : p.whole ? 0 : (size_t)2 * p.workgroups;
+    p.off_part = take(slots * (16 * p.nc * (D + 2)) * sizeof(float));
     p.bytes = off;
     return p;
 }
@@ -943,6 +1008,7 @@ extern "C" radar_status radar_tree_attention_kvq(const void *q, const void *cach
     a.workgroups = p.workgroups; a.least = p.least; a.shift = p.shift; a.max_cgs = p.max_cgs;
     a.unit_cost = p.unit_cost; a.whole = p.whole;
     char *ws = static_cast<char *>(workspace);
+    a.arrived = reinterpret_cast<unsigned int *>(ws + p.off_arrived);
     a.unit_tab = reinterpret_cast<uint32_t *>(ws + p.off_tab);
     a.part = reinterpret_cast<float *>(ws + p.off_part);
     hipStream_t s = static_cast<hipStream_t>(stream);

@@ -342,6 +342,39 @@ def test_attention_of_a_batch_in_every_shape(T, S, D, far):
     torch.cuda.empty_cache()
 
 
+@pytest.mark.parametrize("far", [False, True])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("B,T,Hq,H,S", [(3, 4, 8, 2, 4096), (2, 1, 4, 1, 60000), (1, 60, 32, 8, 7000), (4, 60, 32, 8, 9000)])
+def test_units_that_several_workgroups_join(B, T, Hq, H, S, D, far):
+    """Few units and room for long sequences: parts of a unit in several workgroups, 16, 32 and 64 columns each.  One workspace for calls whose lengths
+    leave parts without a step, units with one part, and none; its counters are zero again after every call."""
+    b, rng, R = binding(), seed(300 + T + D + B), 16
+    tables, cache, _, _, _ = make_attention(rng, np.full(B, 900), T, np.full(B, T), Hq, H, D, R)
+    n_small = cache.shape[1]
+    if far:
+        n_blocks = (5 << 30) // (H * kvq.chunk_bytes(R, D))
+        c = b.KvqCache(n_blocks, R, H, D)
+        ids = np.sort(rng.choice(n_blocks, n_small, replace=False)).astype(np.int32)
+        c.data[0, torch.from_numpy(ids).long().cuda()] = dev(cache[0])
+    else:
+        c, ids = gpu_cache(cache, R, D), np.arange(n_small, dtype=np.int32)
+    wide = np.full((B, -(-S // R)), -1, np.int32)
+    wide[:, :tables.shape[1]] = ids[tables]
+    dt, ws = dev(wide), None
+    for ctx in ([900, 700, 37, 500], [0, -1, 300, 31], [65, 900, -1, 600]):
+        ctx, nodes = np.array(ctx[:B], np.int32), rng.integers(1, T + 1, B).astype(np.int32)
+        q, qb = bf16(rng.normal(size=(B, T, Hq, D)))
+        par = random_parents(rng, B, T, nodes)
+        ws = b.new_workspace(b.radar_tree_attention_kvq_workspace_bytes(b.kvq_attn_desc(bf16_dev(qb), c, wide.shape[1], S))) if ws is None else ws
+        out = torch.full(q.shape, 7.0, dtype=torch.bfloat16, device="cuda")
+        lse = torch.full(q.shape[:3], 7.0, dtype=torch.float32, device="cuda")
+        b.radar_tree_attention_kvq(bf16_dev(qb), c, dt, dev(ctx), dev(par), dev(nodes), out=out, lse_out=lse, S_max=S, workspace=ws)
+        check_attention(q, cache, R, D, 0, tables, ctx, par, nodes, out, lse)
+        assert (ws[:16384] == 0).all()
+    del c
+    torch.cuda.empty_cache()
+
+
 def test_attention_at_the_longest_lengths_allowed():
     """S_max up to the limit, where the work is counted in more than one step: short sequences under it, and a long one."""
     b, rng = binding(), seed(99)
