@@ -624,7 +624,9 @@ radar_status radar_kvq_commit(void *cache, const int32_t *block_tables, int32_t 
  * that the call is planned for, at most max_blocks * block_rows (the longest
  * ctx_lens[b] + T_max where it is known).  Other arguments and limits as for
  * radar_tree_attention; B * Hkv * ceil(Hq / Hkv * T_max / 16) < 2^23 - 7; q and out
- * 16-byte aligned rows.  One kernel, or two where units of work are divided. */
+ * 16-byte aligned rows.  One kernel, or two where units of work are divided.  The
+ * workspace's counters are at its head for all shapes: one that is large enough
+ * serves calls of any shape that follow each other, initialised once. */
 typedef struct radar_kvq_attn_desc {
     radar_kvq_desc cache;    /* layers and layer_stride are ignored */
     int32_t B, T_max, Hq, max_blocks, S_max;

@@ -11,8 +11,8 @@
 //
 // What bounds it (one MI355X, D = 128, blocks of 16 rows): 64 single tokens over 512 to 8192 rows, 283 MB, the rows' bytes (69 us; 55 at a copy's
 // rate); four sequences of 16384 rows with 64 heads, 129 GFLOP, vector instructions (72% of the SIMDs' cycles) beside the matrix pipe (51%): 121 us,
-// 1.07 PFLOP/s; 16 ragged trees over 512 to 8192 rows 64 us, a third of it the ends of pieces and the second launch; one tree over 2048 rows 13 us,
-// 120 workgroups of nine rounds; one token over 256 rows 5.8 us, a launch.
+// 1.07 PFLOP/s; 16 ragged trees over 512 to 8192 rows 64 us, a third of it the ends of pieces and the second launch; one tree over 2048 rows 12.1
+// us, 240 workgroups of five rounds that join in pairs; one token over 256 rows 5.8 us, a launch.
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -903,11 +903,12 @@ static KqPlan plan_kvq(const radar_kvq_attn_desc *d) {
     const int64_t steps = ((int64_t)d->S_max + 31) / 32;
     // Columns a workgroup, and how units are given out: whole; to 2, 4, ... 64 workgroups each, the last of which joins their parts; or all of them in a
     // line, in equal shares.  Whichever takes least, from what rounds of steps and the rest took (us, one MI355X, D = 128, beside the 6 of any call).
-    // The line costs 13 more, a second launch and two pieces a workgroup, and pays where units differ or would leave many workgroups without one (the
-    // host knows the longest only; half of it is taken for the others).  us with 16 / 32 / 64 columns, "-" where there are too many units to join:
+    // The line costs 13 more (9 with few units), a second launch and two pieces a workgroup, and pays where units differ or are more than the joined
+    // ones may be (the host knows the longest only; half of it is taken for the others).  us with 16 / 32 / 64 columns, "-" where there are too many units to join:
     //                                         whole       joined, by 2 ... 32                   line
     //   1 token, 32 heads on 8, 2048 rows       13          10.8  9.3  8.9 10.2 11.4              12.5
     //   16000 rows                              60          34  21  15.5  13.3  15.5              17
+    //   128000 rows                                         by 32 34                              33
     //   60 tree rows, 2048 rows                 14 17 24    12.5 15.9 22.9, by 4 - 14.0 20.2      21 21 25
     //   12000 rows                              50 57 84    32 37 53, by 4 - 26 36, by 8 - - 31   38 33 34
     //   4 sequences of 2000 rows                23 18 26    - - 25                                33 22 32
@@ -924,7 +925,7 @@ static KqPlan plan_kvq(const radar_kvq_attn_desc *d) {
         const double alone[] = {0.91, 1.05, 1.7}, shared[] = {0.8, 1.27, 2.2}, end[] = {0.0, 2.3, 4.0}, divided[] = {13.2, 12.7, 16.0};
         const double few[] = {0.83, 1.0, 1.65}, many[] = {0.95, 1.27, 2.05}, join[] = {0.2, 0.35, 0.5};        // (many: more workgroups than half the CUs)
         auto take = [&](double us, int whole) { if (us < best) { best = us; p.nc = nc; p.whole = whole; } };
-        take(divided[x] + units / 256.0 * ((d->B > 1 ? 0.5 : 1.0) * rounds * shared[x] + 3.0 + end[x]), 0);
+        take((units <= 32 ? 9.0 : divided[x]) + units / 256.0 * ((d->B > 1 ? 0.5 : 1.0) * rounds * shared[x] + 3.0 + end[x]), 0);
         if (d->rows_per_split != 0) continue;
         take(std::ceil(units / 256.0) * (rounds * alone[x] + end[x]), 1);
         for (int bits = 1; bits <= 6 && units * (1 << bits) <= kKqJoined; ++bits)

@@ -375,6 +375,23 @@ def test_units_that_several_workgroups_join(B, T, Hq, H, S, D, far):
     torch.cuda.empty_cache()
 
 
+def test_one_workspace_for_calls_of_any_shape():
+    """Units joined by different numbers of workgroups and units in a line, one call after the other in a workspace initialised once."""
+    b, rng = binding(), seed(97)
+    T, Hq, H, D, R, S = 16, 8, 2, 128, 16, 1 << 18
+    ctx, nodes = rng.integers(200, 700, 12).astype(np.int32), rng.integers(1, T + 1, 12).astype(np.int32)
+    tables, cache, q, qb, par = make_attention(rng, ctx, T, nodes, Hq, H, D, R)
+    wide = np.full((12, S // R), -1, np.int32)
+    wide[:, :tables.shape[1]] = tables
+    c, dq, dt, dc, dp, dn = gpu_cache(cache, R, D), bf16_dev(qb), dev(wide), dev(ctx), dev(par), dev(nodes)
+    shapes = [(12, S), (1, 8192), (12, 800), (1, S), (3, 4096), (12, 8192)]
+    ws = b.new_workspace(max(b.radar_tree_attention_kvq_workspace_bytes(b.kvq_attn_desc(dq[:B], c, S // R, S_max=n)) for B, n in shapes))
+    for B, n in 2 * shapes:
+        lse = torch.full((B, T, Hq), 7.0, device="cuda")
+        got = b.radar_tree_attention_kvq(dq[:B], c, dt[:B], dc[:B], dp[:B], dn[:B], lse_out=lse, S_max=n, workspace=ws)
+        check_attention(q[:B], cache, R, D, 0, tables[:B], ctx[:B], par[:B], nodes[:B], got, lse)
+
+
 def test_attention_at_the_longest_lengths_allowed():
     """S_max up to the limit, where the work is counted in more than one step: short sequences under it, and a long one."""
     b, rng = binding(), seed(99)
