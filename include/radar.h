@@ -523,6 +523,10 @@ radar_status radar_draft_rerank_batch(const int32_t *pool_tokens, const float *p
  *   radar_tree_attention_kvq      per layer: every node over its prefix and ancestors
  *   radar_kvq_commit              after the walk: the accepted path's rows into place
  * and radar_kvq_read gives rows back as bf16, e.g. to hand a prefix on.
+ * A sequence that radar_kvq_blocks refuses has no part in the pass: its rows are
+ * not written, and the later calls reach no block that is not its own.  What they
+ * give for it (outputs, an accepted path, new_ctx_lens) stands for nothing: keep its
+ * ctx_lens, or pass a negative length in its place.
  *
  * Format.  32 consecutive values x of a row of a head share a scale 2^e and are
  * 4-bit codes (sign; 0, 0.5, 1, 1.5, 2, 3, 4, 6).  With amax the largest |x|, e is
@@ -569,8 +573,11 @@ size_t radar_kvq_block_bytes(int32_t block_rows, int32_t D);
  * [0, T_max]), -1 for other i and for sequences that were not granted.
  * block_tables i32 [B,max_blocks] and free_blocks i32 [n_blocks] are updated in
  * place; entries behind the owned ones and the stack's height are left as they
- * were.  owned_out and n_free_out may be owned and n_free, or other arrays: as
- * long as they are, the call may be repeated with the same result.
+ * were, but for a sequence that is not granted, whose entries [owned[b], max_blocks)
+ * become -1 (later calls, which take rows behind ctx_lens[b] from the table, would
+ * find what it gave back and others hold).  owned_out and n_free_out may be owned
+ * and n_free, or other arrays: as long as they are, the call may be repeated with
+ * the same result.
  * ctx_lens, owned, granted, owned_out i32 [B]; n_new i32 [B] or NULL (= T_max);
  * n_free, n_free_out i32 [1]; slots i32 [B,T_max].  No workspace; one kernel, or
  * two where B * T_max is large. */

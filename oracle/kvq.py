@@ -110,6 +110,7 @@ def blocks(ctx, new, tables, owned, free, n_free, R, T):
             n_free -= 1
             tables[b, i] = free[n_free]
         owned[b] = want[b]
+    tables[(granted == 0)[:, None] & (np.arange(M) >= np.minimum(owned, M)[:, None])] = -1
     slots = np.full((B, T), -1, np.int32)
     for b in range(B):
         if granted[b] and ctx[b] >= 0:

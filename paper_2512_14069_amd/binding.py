@@ -752,7 +752,8 @@ def _i32p(t, name):
 def radar_kvq_blocks(ctx_lens, tables, T, n_new=None, slots=None, granted=None, owned_out=None, n_free_out=None, prepared=False):
     """Room for T (n_new i32 [B]: so many) new rows of every sequence behind its ctx_lens i32 [B] rows (negative: it has ended) in
     `tables` (KvqTables, updated; owned and n_free too unless owned_out and n_free_out are given).
-    Returns (slots i32 [B,T], granted i32 [B])."""
+    Returns (slots i32 [B,T], granted i32 [B]).  A sequence with granted 0 has no part in the pass: its slots are -1, so are its table's entries
+    behind the owned ones, and the caller keeps its ctx_lens whatever radar_kvq_commit returns."""
     if slots is not None and granted is not None and (native := _direct(prepared)) and native.kvq_blocks(
             ctx_lens, n_new, tables.block_tables, tables.owned, tables.free_blocks, tables.n_free, tables.owned if owned_out is None else owned_out,
             tables.n_free if n_free_out is None else n_free_out, slots, granted, T, tables.block_rows):
