@@ -633,7 +633,9 @@ radar_status radar_kvq_commit(void *cache, const int32_t *block_tables, int32_t 
  * radar_tree_attention; B * Hkv * ceil(Hq / Hkv * T_max / 16) < 2^23 - 7; q and out
  * 16-byte aligned rows.  One kernel, or two where units of work are divided.  The
  * workspace's counters are at its head for all shapes: one that is large enough
- * serves calls of any shape that follow each other, initialised once. */
+ * serves calls of any shape that follow each other, initialised once.  The size
+ * asked for goes by B, T_max and the heads: what a program's largest B and T_max
+ * ask for serves all smaller ones and any S_max. */
 typedef struct radar_kvq_attn_desc {
     radar_kvq_desc cache;    /* layers and layer_stride are ignored */
     int32_t B, T_max, Hq, max_blocks, S_max;

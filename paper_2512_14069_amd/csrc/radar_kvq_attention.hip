@@ -228,6 +228,7 @@ constexpr int kKqWaves = 8, kKqThreads = kKqWaves * kWave;
 constexpr float kKqMost = 2048.0f;             // what a lane's eight weights may add up to before the reference is moved
 constexpr int kKqArrived = 16;                 // counters are 64 bytes apart: atomics on one line wait for each other
 constexpr int kKqJoined = 256;                 // most workgroups of units that several take
+constexpr int kq_line_workgroups(int nc) { return nc == 1 ? 512 : 256; }       // what the chip holds at once
 constexpr float kKqNone = 3.0e38f;             // negated reference of a column that has seen no key yet
 
 template <int D, int NC>
@@ -934,7 +935,7 @@ static KqPlan plan_kvq(const radar_kvq_attn_desc *d) {
     p.max_cgs = (cols + 16 * p.nc - 1) / (16 * p.nc);
     const int64_t units = (int64_t)d->B * d->cache.Hkv * p.max_cgs;
     const int64_t parts = p.whole ? units << (p.whole - 1) : 0;
-    p.workgroups = p.whole ? (int)((parts + 7) / 8 * 8) : p.nc == 1 ? 512 : 256;             // or what the chip holds at once
+    p.workgroups = p.whole ? (int)((parts + 7) / 8 * 8) : kq_line_workgroups(p.nc);
     p.least = d->rows_per_split ? d->rows_per_split / 32 : 8;
     // what a unit costs besides its steps, in steps of a wavefront of eight: the merge in LDS, the way in and out (64 single tokens with 0 / 16 / 24 / 48:
     // 86 72 70 73 us; 16 ragged trees by 64 columns with 0 / 24 / 48 / 96: 109 80 71 74; by 32 with 16 / 48 / 96: 94 80 88)
@@ -942,12 +943,17 @@ static KqPlan plan_kvq(const radar_kvq_attn_desc *d) {
     // positions on the line stay within 31 bits
     p.shift = 0;
     while (units * ((steps >> p.shift) + 1 + p.unit_cost) >= (int64_t(1) << 31) && p.shift < 31) ++p.shift;
+    // The workspace has room for any plan of these heads with as many sequences and nodes or fewer, since a program that has one for its largest
+    // shape makes calls of all smaller ones, and these may be given out in another way and need more: units of 16 columns in the table, and as many
+    // columns of partial results as a line leaves, two pieces a workgroup (joined units leave less).
+    static_assert(kKqJoined <= 2 * kq_line_workgroups(4));
+    const int widest = cols > 32 ? 4 : cols > 16 ? 2 : 1;
+    const size_t units16 = (size_t)d->B * d->cache.Hkv * ((cols + 15) / 16), left = std::max(2 * kq_line_workgroups(1), 2 * kq_line_workgroups(widest) * widest) * 16;
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t o = off; off += (bytes + 255) & ~size_t(255); return o; };
     p.off_arrived = take(kKqJoined * kKqArrived * sizeof(unsigned int));      // first, whatever the shape: all calls leave them at zero
-    p.off_tab = take(p.whole ? 0 : (size_t)units * sizeof(uint32_t));
-    const size_t slots = p.whole > 1 ? (size_t)parts : p.whole ? 0 : (size_t)2 * p.workgroups;
-    p.off_part = take(slots * (16 * p.nc * (D + 2)) * sizeof(float));
+    p.off_tab = take(units16 * sizeof(uint32_t));
+    p.off_part = take(left * (D + 2) * sizeof(float));
     p.bytes = off;
     return p;
 }
