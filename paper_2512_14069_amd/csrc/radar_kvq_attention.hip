@@ -152,9 +152,9 @@ __device__ __forceinline__ T kq_read(kq_bytes base, uint64_t up, bool is_up, uin
 }
 
 template <int D, bool FAR>
-__device__ __forceinline__ void kq_load_k(KqK<D> &k, KqBase s) {
+__device__ __forceinline__ void kq_load_k(KqK<D> &k, KqBase s, int lane) {
     using C = KvqChunk<D>;
-    const int lane = lane_id(), r = lane & 15, grp = lane >> 4, group = (r >> 2) & 1, blk = D == 128 ? grp : grp >> 1;
+    const int r = lane & 15, grp = lane >> 4, group = (r >> 2) & 1, blk = D == 128 ? grp : grp >> 1;
     const bool is_up = (r >= 8) == s.second_up;
     const uint32_t at = (uint32_t)(C::k_row(8 * group + (r & 3)) + (D / 8) * grp);
 #pragma unroll
@@ -171,9 +171,9 @@ __device__ __forceinline__ void kq_load_k(KqK<D> &k, KqBase s) {
     k.scale = kq_read<u32x2, FAR>(s.scale, s.scale_up, is_up, (uint32_t)((group * C::kScales + blk) * 8));
 }
 template <int D, bool FAR>
-__device__ __forceinline__ void kq_load_v(KqV &v, const KqArgs &a, KqBase s) {
+__device__ __forceinline__ void kq_load_v(KqV &v, const KqArgs &a, KqBase s, int lane) {
     using C = KvqChunk<D>;
-    const int lane = lane_id(), r = lane & 15, grp = lane >> 4, piece = D == 128 ? r : r >> 1, blk = D == 128 ? r >> 2 : r >> 3;
+    const int r = lane & 15, grp = lane >> 4, piece = D == 128 ? r : r >> 1, blk = D == 128 ? r >> 2 : r >> 3;
     const bool is_up = (grp >= 2) == s.second_up;
     const kq_bytes code = s.code + ((D / 2) << a.rbits);
     const uint32_t at = (uint32_t)(((grp & 1) * C::kPieces + piece) * 32);
@@ -229,7 +229,12 @@ constexpr float kKqMost = 2048.0f;             // what a lane's eight weights ma
 constexpr int kKqArrived = 16;                 // counters are 64 bytes apart: atomics on one line wait for each other
 constexpr int kKqJoined = 256;                 // most workgroups of units that several take
 constexpr int kq_line_workgroups(int nc) { return nc == 1 ? 512 : 256; }       // what the chip holds at once
-constexpr float kKqNone = 3.0e38f;             // negated reference of a column that has seen no key yet
+// Scores from 2^25 on (in log2 units) are far.  An exponent is fma(score, scale, -reference) with the reference rounded, and what was rounded off is
+// up to half a step of 32 bits: 1 below 2^25, which is harmless as all of a column's weights have it alike, but 128 from 2^31 on, where all of them would
+// be zero or infinite.  So the reference of a far column, and of one that has seen no key yet, waits in LDS as a score, and its weights are
+// 2^((score - reference) scale); its register holds kKqNone, which sends every step there.
+constexpr float kKqNone = 3.0e38f;
+__device__ __forceinline__ bool kq_is_far(float negref) { return __builtin_amdgcn_ubfe(__float_as_uint(negref), 26, 5) >= 19; }      // exponent of 25 or more
 
 template <int D, int NC>
 struct KqShape {
@@ -247,7 +252,7 @@ struct KqShape {
 // asked for as soon as the registers of this one's are free: K's after the scores, V's at the end.
 template <int D, int NC, int AHEAD, typename QOp, typename NextK>
 __device__ __forceinline__ void kq_step(const KqK<D> &k, KqV &v, KqIds id, QOp qop, NextK next_k, floatx4 (&oacc)[D / 16][NC], float (&negref)[NC],
-                                        float (&l_run)[NC], const uint64_t *s_anc, const KqArgs &a, int key0, int L, int total) {
+                                        float (&l_run)[NC], const uint64_t *s_anc, float *s_ref, const KqArgs &a, int key0, int L, int total) {
     using S = KqShape<D, NC>;
     const int lane = lane_id(), r = lane & 15;
     floatx4 sacc[2][NC];
@@ -320,17 +325,17 @@ __device__ __forceinline__ void kq_step(const KqK<D> &k, KqV &v, KqIds id, QOp q
 #pragma unroll
     for (int n = 0; n < NC; ++n) {
         // The eight scores' exponentials against the running reference; p is the matrix cores' operand, the sum is of the unrounded ones, in fp32.
-        auto weigh = [&] {
+        auto weigh = [&](auto base, float shift) {
             float sum = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[e >> 2][n][e & 3], a.scale_log2, negref[n]));
+                const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(sacc[e >> 2][n][e & 3] - base, a.scale_log2, shift));
                 sum = e == 0 ? w : sum + w;
                 p[n][e] = (__bf16)w;
             }
             return sum;
         };
-        float sum = weigh();
+        float sum = weigh(std::integral_constant<int, 0>{}, negref[n]);
         // The reference is the columns' maximum at the time when some lane's sum last went past 2^11 (for a column without a key: at once).  Only then
         // do the four lanes of a column compare their maxima, and outputs and sums get rescaled: no step but a wavefront's first does it as a rule.
         // Weights of up to 2^11 instead of 1 lose nothing: they keep bf16's eight bits, and sums and outputs are fp32.
@@ -338,12 +343,21 @@ __device__ __forceinline__ void kq_step(const KqK<D> &k, KqV &v, KqIds id, QOp q
             float mx = sacc[0][n][0];
 #pragma unroll
             for (int e = 1; e < 8; ++e) mx = fmaxf(mx, sacc[e >> 2][n][e & 3]);
-            const float neg = fminf(negref[n], -(kq_column_max(mx) * a.scale_log2)), alpha = __builtin_amdgcn_exp2f(neg - negref[n]);
-            negref[n] = neg;
+            mx = kq_column_max(mx);
+            int tid = threadIdx.x;
+            asm volatile("" : "+v"(tid));                            // (the address is worked out here, and not kept in registers)
+            float *const ref = s_ref + (tid >> 6) * S::COLS + n * 16 + (tid & 15);                  // (a column's four lanes agree)
+            // a weight is 2^((score - base) scale + shift): shift 0 for a far column, base 0 for others
+            const float old = *ref, old_neg = negref[n], old_base = kq_is_far(old_neg) ? old : 0.f, old_shift = kq_is_far(old_neg) ? 0.f : old_neg;
+            mx = kq_is_far(old_neg) ? fmaxf(old, mx) : mx;
+            const float neg = fminf(old_neg, -(mx * a.scale_log2)), base = kq_is_far(neg) ? mx : 0.f, shift = kq_is_far(neg) ? 0.f : neg;
+            *ref = mx;
+            negref[n] = kq_is_far(neg) ? kKqNone : neg;
+            const float alpha = __builtin_amdgcn_exp2f(__builtin_fmaf(old_base - base, a.scale_log2, shift - old_shift));
             l_run[n] *= alpha;
 #pragma unroll
             for (int m = 0; m < S::NM; ++m) oacc[m][n] *= alpha;
-            sum = weigh();
+            sum = weigh(base, shift);
         }
         sum += l_run[n];
         asm volatile("" : "+v"(sum));                                // (added up here: left to the end of the step all of them stay in registers)
@@ -494,7 +508,7 @@ __device__ __forceinline__ KqArgs kq_args_end() {
     KqArgs a;
     a.out = g->out; a.o_sb = g->o_sb; a.o_st = g->o_st; a.o_sh = g->o_sh; a.lse = g->lse; a.G = g->G; a.T = g->T; a.Hq = g->Hq; a.part = g->part;
     a.ctx_lens = g->ctx_lens; a.n_nodes = g->n_nodes; a.S = g->S; a.B = g->B; a.workgroups = g->workgroups;
-    a.whole = g->whole; a.arrived = g->arrived;
+    a.whole = g->whole; a.arrived = g->arrived; a.scale_log2 = g->scale_log2;
     return a;
 }
 
@@ -606,8 +620,10 @@ __global__ __launch_bounds__(kKqThreads, NC == 1 ? 4 : 2) void kvq_attn_kernel(K
             id = kq_ids(a, table, mine * 32, p.total);
             nid = kq_ids(a, table, min(mine + kKqWaves, p.s1 - 1) * 32, p.total);
             const KqBase at = kq_base<D>(a, base, id, mine * 32);
-            kq_load_k<D, FAR>(k, at);
-            kq_load_v<D, FAR>(v, a, at);
+            int lane2 = lane;
+            asm volatile("" : "+v"(lane2));                          // (a mask of lanes less to keep)
+            kq_load_k<D, FAR>(k, at, lane2);
+            kq_load_v<D, FAR>(v, a, at, lane2);
         }
         // this lane's columns: their queries' operands (d = D/4 * grp + 8 * c + 0..7) and ancestors
         const KqArgs aq = kq_args_query();
@@ -625,6 +641,7 @@ __global__ __launch_bounds__(kKqThreads, NC == 1 ? 4 : 2) void kvq_attn_kernel(K
             const uint32_t lo = (uint32_t)__shfl((int)(uint32_t)words, ii), hi = (uint32_t)__shfl((int)(uint32_t)(words >> 32), ii);
             if (grp == 0) s_anc[w * 16 + r] = i < p.nn ? (uint64_t)hi << 32 | lo : 0ull;
         }
+        if (lane < S::COLS) s_m[w * S::COLS + lane] = -kKqNone;      // the references of this wavefront's columns, as scores
         floatx4 oacc[S::NM][NC];
         float negref[NC], l_run[NC];
 #pragma unroll
@@ -642,9 +659,9 @@ __global__ __launch_bounds__(kKqThreads, NC == 1 ? 4 : 2) void kvq_attn_kernel(K
             KqIds nnid;
             kq_step<D, NC, FAR || NC == 1 ? 2 : 4>(k, v, id, qop, [&] {
                 nnid = kq_ids(a, table, min(s + 2 * kKqWaves, last) * 32, p.total);
-                kq_load_k<D, FAR>(k, kq_base<D>(a, base, nid, next * 32));
-            }, oacc, negref, l_run, s_anc, a, s * 32, p.L, p.total);
-            kq_load_v<D, FAR>(v, a, kq_base<D>(a, base, nid, next * 32));
+                kq_load_k<D, FAR>(k, kq_base<D>(a, base, nid, next * 32), lane);
+            }, oacc, negref, l_run, s_anc, s_m, a, s * 32, p.L, p.total);
+            kq_load_v<D, FAR>(v, a, kq_base<D>(a, base, nid, next * 32), lane);
             id = nid;
             nid = nnid;
         }
@@ -660,7 +677,11 @@ __global__ __launch_bounds__(kKqThreads, NC == 1 ? 4 : 2) void kvq_attn_kernel(K
 #pragma unroll
         for (int n = 0; n < NC; ++n) {
             const float l = kq_column_sum(l_run[n]);
-            if (grp == 0) { s_m[w * S::COLS + n * 16 + r] = -negref[n]; s_l[w * S::COLS + n * 16 + r] = l; }
+            float *const m = s_m + w * S::COLS + n * 16 + r;
+            if (grp == 0) {                                          // (a far reference in log2 units is good to 2^-24 of itself, as the scores are)
+                *m = l == 0.f ? -kKqNone : kq_is_far(negref[n]) ? fminf(fmaxf(*m * a.scale_log2, -kKqNone), kKqNone) : -negref[n];
+                s_l[w * S::COLS + n * 16 + r] = l;
+            }
         }
         __syncthreads();
         if (tid < S::COLS) {
@@ -677,7 +698,7 @@ __global__ __launch_bounds__(kKqThreads, NC == 1 ? 4 : 2) void kvq_attn_kernel(K
         __syncthreads();
         float scl[NC];
 #pragma unroll
-        for (int n = 0; n < NC; ++n) scl[n] = __builtin_amdgcn_exp2f(-negref[n] - s_M[n * 16 + r]);
+        for (int n = 0; n < NC; ++n) scl[n] = __builtin_amdgcn_exp2f(s_m[w * S::COLS + n * 16 + r] - s_M[n * 16 + r]);
 #pragma unroll
         for (int pass = 0; pass < S::PASSES; ++pass) {               // of a column: d = D/4 * part + (4 / PASSES * pass + e) * NM + m
             if (pass > 0) __syncthreads();
@@ -741,7 +762,9 @@ __global__ __launch_bounds__(kKqThreads, NC == 1 ? 4 : 2) void kvq_attn_kernel(K
             if ((int)publish_then_ticket(counter, reinterpret_cast<unsigned int *>(s_m)) != p.parts - 1) return;
             if (threadIdx.x == 0) store_shared_result(counter, 0u);
             const float *const from = a.part + (size_t)(unit << bits) * S::PART;
-            for (int x = threadIdx.x; x < S::COLS * D / 4; x += kKqThreads) {
+            int first = threadIdx.x;
+            asm volatile("" : "+v"(first));                          // (what comes of it is worked out here, and not kept from the start)
+            for (int x = first; x < S::COLS * D / 4; x += kKqThreads) {
                 const int mc = x / (D / 4), d = x % (D / 4) * 4, gc = p.cg * S::COLS + mc, mi = gc / a.G, mh = p.hk * a.G + gc - mi * a.G;
                 if (mi >= p.nn) continue;
                 float M = -kKqNone, l = 0.f;
