@@ -535,7 +535,8 @@ radar_status radar_draft_rerank_batch(const int32_t *pool_tokens, const float *p
  * +-6 (only where e was limited to 125).  No value is off by more than 2^e then.
  * The scale is kept as the byte e + 127.  A block that holds an infinity or NaN
  * has byte 255 and stands for 32 NaNs.  What codes stand for is exact in bf16
- * (bytes 253 and 254, which are never written, reach past its largest number).
+ * (bytes 253 and 254, which are never written, reach past its largest number;
+ * radar_kvq_read gives infinity there, attention may take all of the block for NaN).
  *
  * Layout.  The cache is n_blocks blocks of block_rows rows per layer, every block
  * [Hkv] chunks of radar_kvq_block_bytes(block_rows, D) = block_rows * (D + D/16)

@@ -7,7 +7,7 @@ namespace radar {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kScaleNaN = 255;             // scale byte of a block that held an infinity or NaN
+constexpr uint32_t kScaleMost = 252, kScaleNaN = 255;      // largest scale byte of finite values, and that of a block that held an infinity or NaN
 
 // Sections of a chunk (one KV head's rows of one block), in bytes from its start.  R rows, head dimension D.
 template <int D>

@@ -210,7 +210,7 @@ __global__ __launch_bounds__(kRwThreads) void kvq_append_kernel(RwArgs a) {
     top = max(top, (uint32_t)__shfl_xor((int)top, 2));
     // amax = (1 + m/128) 2^(E-127): the scale's exponent is E - 127 - 2, or one more from 1.75 on, where 6 would be too little by more than half a step
     const bool sound = top < 0x7f80u;
-    const uint32_t byte = (uint32_t)min(max((int)(top >> 7) - 2 + ((top & 127u) >= 96u ? 1 : 0), 1), 252);
+    const uint32_t byte = (uint32_t)min(max((int)(top >> 7) - 2 + ((top & 127u) >= 96u ? 1 : 0), 1), (int)kScaleMost);
     const float scale = kvq_scale(byte);
     const uint32_t x0 = x[0], x1 = x[1], x2 = x[2], x3 = x[3];      // (a bit cast of a vector's element would take its first)
     uint32_t w = 0;
@@ -218,7 +218,7 @@ __global__ __launch_bounds__(kRwThreads) void kvq_append_kernel(RwArgs a) {
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, x1), scale, 1);
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, x2), scale, 2);
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, x3), scale, 3);
-    const uint32_t code = rw_turned(in.is_v, sound ? w : 0u), mark = rw_turned(in.is_v, sound ? byte : (uint32_t)kScaleNaN);
+    const uint32_t code = rw_turned(in.is_v, sound ? w : 0u), mark = rw_turned(in.is_v, sound ? byte : kScaleNaN);
     if (r.n >= a.N || slot < 0 || slot >= a.total) return;
     const int R = 1 << a.rbits, row = slot & (R - 1);
     unsigned char *const chunk = a.cache + ((size_t)(slot >> a.rbits) * a.Hkv + r.h) * C::bytes(R);

@@ -192,15 +192,16 @@ __device__ __forceinline__ void kq_clear_v(KqV &s, int n) {
     s.scale = u32x2{(uint32_t)both, (uint32_t)(both >> 32)};
 }
 
-// A NaN block of V under a probability of zero would make NaN of queries that may not see it.  Only rows of the tree are hidden from anybody, so
-// in a step that reaches them NaN blocks become zeros, and NaN is put where a query does see one.  A lane's outputs are d = D/4 * (lane / 16) ...,
-// all of one block of 32.  Returns which of the step's 32 keys have a NaN in that block; all lanes call.
+// A NaN block of V under a probability of zero would make NaN of queries that may not see it, and so would one whose scale is larger than any that is
+// written: its larger codes are infinite.  Only rows of the tree are hidden from anybody, so in a step that reaches them such blocks become zeros, and NaN is
+// put where a query does see one.  A lane's outputs are d = D/4 * (lane / 16) ..., all of one block of 32.  Returns which of the step's 32 keys have
+// such a block there; all lanes call.
 template <int D>
 __device__ __forceinline__ uint32_t kq_hide_nan(KqV &s, int grp) {
     uint32_t bad = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-        if (((s.scale[e >> 2] >> (8 * (e & 3))) & 255u) == kScaleNaN) {
+        if (((s.scale[e >> 2] >> (8 * (e & 3))) & 255u) > kScaleMost) {
             bad |= 1u << e;
             s.code[e] = 0;
             s.scale[e >> 2] &= ~(255u << (8 * (e & 3)));
