@@ -525,8 +525,9 @@ radar_status radar_draft_rerank_batch(const int32_t *pool_tokens, const float *p
  * and radar_kvq_read gives rows back as bf16, e.g. to hand a prefix on.
  * A sequence that radar_kvq_blocks refuses has no part in the pass: its rows are
  * not written, and the later calls reach no block that is not its own.  What they
- * give for it (outputs, an accepted path, new_ctx_lens) stands for nothing: keep its
- * ctx_lens, or pass a negative length in its place.
+ * give for it (outputs, an accepted path, new_ctx_lens) stands for nothing, and its
+ * ctx_lens stays what it was.  (Given a negative length in its place they leave it
+ * out; to radar_kvq_blocks that would mean that it has ended.)
  *
  * Format.  32 consecutive values x of a row of a head share a scale 2^e and are
  * 4-bit codes (sign; 0, 0.5, 1, 1.5, 2, 3, 4, 6).  With amax the largest |x|, e is

@@ -45,7 +45,7 @@ struct KqArgs {
     int workgroups, least, shift, max_cgs;     // least share of the line; log2 steps per unit of it; column blocks of a KV head
     int unit_cost, whole;                      // what a unit costs besides its steps; whole: no line, 2^(whole - 1) workgroups for each unit
     float *part;                               // [2 * workgroups] partial results: outputs, maxima (log2 units), sums, in fp32
-    uint32_t *unit_tab;                        // first and last workgroup of a unit; alike: it is written already
+    uint32_t *unit_tab;                        // first and last workgroup of a unit; where they are the same it is written already
     unsigned int *arrived;                     // of a unit's workgroups, kKqArrived words apart
 };
 
