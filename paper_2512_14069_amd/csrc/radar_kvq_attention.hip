@@ -10,9 +10,9 @@
 // same eight d side by side: 32 bytes are the operands of eight products.
 //
 // What bounds it (one MI355X, D = 128, blocks of 16 rows): 64 single tokens over 512 to 8192 rows, 283 MB, the rows' bytes (69 us; 55 at a copy's
-// rate); four sequences of 16384 rows with 64 heads, 129 GFLOP, vector instructions (72% of the SIMDs' cycles) beside the matrix pipe (51%): 121 us,
-// 1.07 PFLOP/s; 16 ragged trees over 512 to 8192 rows 64 us, a third of it the ends of pieces and the second launch; one tree over 2048 rows 12.1
-// us, 240 workgroups of five rounds that join in pairs; one token over 256 rows 5.8 us, a launch.
+// rate); four sequences of 16384 rows with 64 heads, 129 GFLOP, vector instructions (72% of the SIMDs' cycles) beside the matrix pipe (51%): 119 us,
+// 1.09 PFLOP/s; 16 ragged trees over 512 to 8192 rows 66 us, a third of it the ends of pieces and the second launch; one tree over 2048 rows 12.0
+// us, 240 workgroups of five rounds that join in pairs; one token over 256 rows 6.1 us, a launch.
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -927,7 +927,8 @@ static KqPlan plan_kvq(const radar_kvq_attn_desc *d) {
     const int cols = d->Hq / d->cache.Hkv * d->T_max, D = d->cache.D;
     const int64_t steps = ((int64_t)d->S_max + 31) / 32;
     // Columns a workgroup, and how units are given out: whole; to 2, 4, ... 64 workgroups each, the last of which joins their parts; or all of them in a
-    // line, in equal shares.  Whichever takes least, from what rounds of steps and the rest took (us, one MI355X, D = 128, beside the 6 of any call).
+    // line, in equal shares.  Whichever takes least, from what rounds of steps and the rest took (us, one MI355X, D = 128, beside the 6 of any call;
+    // D = 64 goes by the same figures, which were not measured there).
     // The line costs 13 more (9 with few units), a second launch and two pieces a workgroup, and pays where units differ or are more than the joined
     // ones may be (the host knows the longest only; half of it is taken for the others).  us with 16 / 32 / 64 columns, "-" where there are too many units to join:
     //                                         whole       joined, by 2 ... 32                   line
