@@ -655,6 +655,85 @@ radar_status radar_tree_attention_kvq(const void *q, const void *cache, const in
                                       void *out, float *lse_out, const radar_kvq_attn_desc *desc,
                                       void *workspace, size_t workspace_bytes, void *stream);
 
+/* --------------------------------------------------------------------------
+ * Rotary positions and chunks of new tokens.  Before a sequence's first tree, and between trees where sequences come and go,
+ * the target takes prompts, pieces of prompts and single tokens: a serving step over a batch makes, per layer,
+ *   radar_kvq_blocks             (once) room for the new rows, and where each goes
+ *   radar_kvq_append_rope        q and k turned by their positions, k and v into the cache
+ *   radar_chunk_attention_kvq    every new row over its sequence's cached rows and the new ones up to itself
+ * and radar_rope turns q and k for caches of any other kind.
+ *
+ * Rows.  A batch's new tokens are either [B,T_max] (row_starts == NULL; N = B * T_max; n_new[b] of them are there, clamped to
+ * [0, T_max], all if n_new == NULL) or one sequence's behind the other's: sequence b has rows row_starts[b] ... row_starts[b+1] - 1
+ * of N, at most T_max of them (row_starts i32 [B+1] on the device, never falling; n_new must be NULL then).  T_max is what the call is planned for: the longest
+ * sequence's number of rows, or more.  Rows behind the last sequence, and rows of a sequence behind its T_max-th, are not there.
+ *
+ * radar_rope.  Row i of sequence b, row n of the tensors, has the positions p_a = positions[a][n] + ctx_lens[b] (positions == NULL: i + ctx_lens[b];
+ * ctx_lens == NULL: 0 in its place) on axes a < axes: one for text, three for time, height and width of images and video.  Tree
+ * nodes are rows with positions = tree_depth and ctx_lens.  With P = rotary_dim / 2, pair j < P is values (j, j + P) of a head's row, or
+ * (2 j, 2 j + 1) where interleaved, and is turned by t = p * inv_freq[j], p on the axis pair_axis[j]:
+ *     (x, y) -> scale * (x cos t - y sin t, x sin t + y cos t)
+ * Values from rotary_dim on are copied.  Angles and turns are computed in fp64 and rounded to fp32 and then to bf16 (angles are
+ * good to |t| 2^-53; beyond 2^31 radians no further promise is made).  Rows that are not there, and rows of a sequence with
+ * ctx_lens[b] < 0, are left as they were.  q_out may be q, and k_out k, with the same strides; other overlaps of an output are not allowed.
+ * q, q_out bf16 [N,Hq,D], k, k_out bf16 [N,Hkv,D], D contiguous, strides in elements, 0 => dense, rows 16-byte aligned; q or k may be NULL
+ * with its output; positions i32 [axes,N]; inv_freq f32 [P]; n_new, ctx_lens i32 [B].  No workspace; one kernel.
+ * Limits: D and rotary_dim multiples of 16, D <= 256; 1 <= axes <= 4; N < 2^31; about N / 8 * (Hq + Hkv) / 8 < 2^24. */
+typedef struct radar_rope_desc {
+    int32_t B, T_max;
+    int32_t Hq, Hkv, D;
+    int32_t rotary_dim;      /* 0 => D */
+    int32_t axes;
+    int32_t interleaved;     /* 0: pairs (j, j + P); 1: pairs (2 j, 2 j + 1) */
+    float   scale;           /* of cosines and sines; 0 => 1 */
+    int64_t N;
+    int64_t q_stride_n, q_stride_h, kv_stride_n, kv_stride_h;      /* kv: of k, and of v, which has the same */
+    int64_t q_out_stride_n, q_out_stride_h, k_out_stride_n, k_out_stride_h;
+    uint8_t pair_axis[128];  /* of pair j < P */
+} radar_rope_desc;
+
+radar_status radar_rope(const void *q, const void *k, void *q_out, void *k_out, const float *inv_freq, const int32_t *positions,
+                        const int32_t *ctx_lens, const int32_t *row_starts, const int32_t *n_new, const radar_rope_desc *desc, void *stream);
+
+/* radar_rope of q and k, and k and v into one layer's cache, as radar_rope followed by radar_kvq_append would, bit for bit:
+ * row i of sequence b goes to slots[b,i] (i32 [B,T_max], as radar_kvq_blocks writes them, also where the rows are one behind the other); a
+ * row whose slot is out of range, or that is not there, is not written; q is turned all the same.  v bf16 [N,Hkv,D] with k's strides;
+ * q and q_out may both be NULL; k_out's strides are ignored.  cache: the layer's first block.  desc->D and desc->Hkv are the cache's.
+ * Limits: those of both calls.  No workspace; one kernel. */
+radar_status radar_kvq_append_rope(const void *q, const void *k, const void *v, void *q_out, const float *inv_freq, const int32_t *positions,
+                                   const int32_t *ctx_lens, const int32_t *row_starts, const int32_t *n_new, const int32_t *slots, void *cache,
+                                   const radar_rope_desc *desc, const radar_kvq_desc *cache_desc, void *stream);
+
+/* Attention of chunks of new tokens over the paged 4-bit cache, for chunks of any length (radar_tree_attention_kvq takes up to
+ * RADAR_T_MAX rows of a tree).  Row i of sequence b, whose key and value are cache row ctx_lens[b] + i already, sees rows j <= ctx_lens[b] + i
+ * that are among the first S_max and in blocks that are there:
+ *     out[n,h,:] = softmax_j( scale * <q[n,h,:], k[j,h/G,:]> ) . v[j,h/G,:]          lse[n,h] = log sum_j exp(...)
+ * Where no row is there to be seen, out is zero and lse -inf.  A row that is not seen has no influence, whatever it holds (NaN blocks
+ * included).  Rows of a sequence with ctx_lens[b] < 0 are zero in out and lse, and so are rows i >= n_new[b] of [B,T_max]; rows behind the last
+ * sequence of row_starts are left as they were.
+ * q, out bf16 [N,Hq,D] (or [B,T_max,Hq,D]: a stride_b of its own), strides as for radar_tree_attention, stride_b ignored with row_starts; out
+ * must not overlap q; lse_out f32 [N,Hq] dense or NULL; block_tables i32 [B,max_blocks]; S_max: the rows
+ * that the call is planned for, at most max_blocks * block_rows (the longest ctx_lens[b] + rows where it is known).
+ * Limits: those of the cache; B <= 65535; N < 2^31; Hq <= 65535; the blocks of 64 of a KV head's queries, about (N * Hq / Hkv / 64 + B) * Hkv, < 2^22.
+ * One kernel.  The workspace's size depends on D only, and its counters are at its head: one, initialised once, serves calls of any shape that
+ * follow each other on one stream. */
+typedef struct radar_kvq_chunk_desc {
+    radar_kvq_desc cache;    /* layers and layer_stride are ignored */
+    int32_t B, T_max, Hq, max_blocks, S_max;
+    int32_t rows_per_split;  /* 0 => chosen by the library; else a multiple of 64: cache rows that one workgroup takes, and no fewer, before
+                                partial results are joined (as many as the workspace has room for) */
+    int64_t N;
+    int64_t q_stride_b, q_stride_t, q_stride_h;
+    int64_t out_stride_b, out_stride_t, out_stride_h;
+    float   softmax_scale;   /* 0 => 1/sqrt(D); must not be negative */
+} radar_kvq_chunk_desc;
+
+size_t radar_chunk_attention_kvq_workspace_bytes(const radar_kvq_chunk_desc *desc);
+
+radar_status radar_chunk_attention_kvq(const void *q, const void *cache, const int32_t *block_tables, const int32_t *ctx_lens,
+                                       const int32_t *row_starts, const int32_t *n_new, void *out, float *lse_out, const radar_kvq_chunk_desc *desc,
+                                       void *workspace, size_t workspace_bytes, void *stream);
+
 /* Counts, per call, the nodes i < n_nodes[b] whose parent breaks the tree
  * convention; *bad_count_out (device i32) is overwritten.  parents i32
  * [B,T_max]; n_nodes i32 [B] or NULL. */

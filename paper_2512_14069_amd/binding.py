@@ -87,6 +87,22 @@ class KvqAttnDesc(ctypes.Structure):
                 ("softmax_scale", ctypes.c_float)]
 
 
+class RopeDesc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("T_max", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("rotary_dim", ctypes.c_int32), ("axes", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("scale", ctypes.c_float), ("N", ctypes.c_int64),
+                ("q_stride_n", ctypes.c_int64), ("q_stride_h", ctypes.c_int64), ("kv_stride_n", ctypes.c_int64), ("kv_stride_h", ctypes.c_int64),
+                ("q_out_stride_n", ctypes.c_int64), ("q_out_stride_h", ctypes.c_int64), ("k_out_stride_n", ctypes.c_int64),
+                ("k_out_stride_h", ctypes.c_int64), ("pair_axis", ctypes.c_uint8 * 128)]
+
+
+class KvqChunkDesc(ctypes.Structure):
+    _fields_ = [("cache", KvqDesc), ("B", ctypes.c_int32), ("T_max", ctypes.c_int32), ("Hq", ctypes.c_int32), ("max_blocks", ctypes.c_int32),
+                ("S_max", ctypes.c_int32), ("rows_per_split", ctypes.c_int32), ("N", ctypes.c_int64),
+                ("q_stride_b", ctypes.c_int64), ("q_stride_t", ctypes.c_int64), ("q_stride_h", ctypes.c_int64),
+                ("out_stride_b", ctypes.c_int64), ("out_stride_t", ctypes.c_int64), ("out_stride_h", ctypes.c_int64),
+                ("softmax_scale", ctypes.c_float)]
+
+
 class PolicyParams(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("w_ih", "w_hh", "b_ih", "b_hh", "w1", "b1", "w2", "b2")] + \
                [("k", ctypes.c_int32), ("H", ctypes.c_int32), ("M", ctypes.c_int32)]
@@ -108,6 +124,7 @@ EXPORTS = [
     "radar_verify_accept_q_workspace_bytes", "radar_verify_accept_q",
     "radar_kvq_block_bytes", "radar_kvq_blocks", "radar_kvq_append", "radar_kvq_read", "radar_kvq_commit",
     "radar_tree_attention_kvq_workspace_bytes", "radar_tree_attention_kvq",
+    "radar_rope", "radar_kvq_append_rope", "radar_chunk_attention_kvq_workspace_bytes", "radar_chunk_attention_kvq",
     "radar_debug_validate_tree", "radar_profile_begin", "radar_profile_end", "radar_probe_hbm_read",
 ]
 
@@ -183,6 +200,14 @@ def load():
     lib.radar_tree_attention_kvq_workspace_bytes.argtypes = [ctypes.POINTER(KvqAttnDesc)]
     lib.radar_tree_attention_kvq.restype = i32
     lib.radar_tree_attention_kvq.argtypes = [vp] * 8 + [ctypes.POINTER(KvqAttnDesc), vp, sz, vp]
+    lib.radar_rope.restype = i32
+    lib.radar_rope.argtypes = [vp] * 9 + [ctypes.POINTER(RopeDesc), vp]
+    lib.radar_kvq_append_rope.restype = i32
+    lib.radar_kvq_append_rope.argtypes = [vp] * 11 + [ctypes.POINTER(RopeDesc), ctypes.POINTER(KvqDesc), vp]
+    lib.radar_chunk_attention_kvq_workspace_bytes.restype = sz
+    lib.radar_chunk_attention_kvq_workspace_bytes.argtypes = [ctypes.POINTER(KvqChunkDesc)]
+    lib.radar_chunk_attention_kvq.restype = i32
+    lib.radar_chunk_attention_kvq.argtypes = [vp] * 8 + [ctypes.POINTER(KvqChunkDesc), vp, sz, vp]
     lib.radar_policy_step.restype = i32
     lib.radar_policy_step.argtypes = [vp] * 3 + [ctypes.POINTER(PolicyParams)] + [vp] * 6 + [i32, vp]
     lib.radar_debug_validate_tree.restype = i32
@@ -916,6 +941,190 @@ def radar_tree_attention_kvq(q, cache, block_tables, ctx_lens, parents=None, n_n
             _ptr(None if lse_out is None else _dense(lse_out, "lse_out"), torch.float32, "lse_out"), ctypes.byref(desc), wp, wn, _stream())
     keep = (q, cache, data, block_tables, parents, ctx_lens, n_nodes, out, lse_out, desc, workspace)
     return _finish("radar_tree_attention_kvq", load().radar_tree_attention_kvq, args, keep, out, prepared)
+
+
+# ------------------------------------------------------------ rotary positions, chunks of new tokens
+
+class Rope:
+    """Rotary positions of a model: inv_freq f32 [P] (a GPU tensor, kept) for the first 2 P values of a head; `axes` positions a row, pair j turned by the
+    one that pair_axis[j] names (P whole numbers; default all 0); interleaved: pairs (2 j, 2 j + 1), else (j, j + P); scale: of cosines and sines."""
+
+    def __init__(self, inv_freq, axes=1, pair_axis=None, interleaved=False, scale=1.0):
+        P = inv_freq.numel()
+        if inv_freq.dim() != 1 or not 1 <= P <= 128:
+            raise ValueError(f"inv_freq: expected 1 to 128 frequencies, got shape {tuple(inv_freq.shape)}")
+        if scale == 0.0:
+            raise ValueError("scale must not be 0")
+        self.pair_axis = [0] * P if pair_axis is None else [int(a) for a in pair_axis]
+        if len(self.pair_axis) != P or not all(0 <= a < axes for a in self.pair_axis):
+            raise ValueError(f"pair_axis: expected {P} numbers of {axes} axes")
+        self.inv_freq, self.axes, self.interleaved, self.scale = inv_freq, int(axes), bool(interleaved), float(scale)
+
+    def desc(self):
+        d = RopeDesc()
+        d.rotary_dim, d.axes, d.interleaved, d.scale = 2 * len(self.pair_axis), self.axes, int(self.interleaved), self.scale
+        d.pair_axis[:len(self.pair_axis)] = self.pair_axis
+        return d
+
+
+def _new_rows(t, ctx_lens, row_starts, n_new, T_max, name):
+    """(B, T_max, N) of rows [B,T,...] or, with row_starts i32 [B+1], [N,...]."""
+    lead = tuple(t.shape[:-2])
+    if row_starts is None:
+        if len(lead) != 2:
+            raise ValueError(f"{name}: expected [B, T, heads, D], got {tuple(t.shape)}; rows one behind the other take row_starts")
+        B, T = lead
+        if T_max is not None and int(T_max) != T:
+            raise ValueError(f"T_max {T_max}: rows are [{B}, {T}]")
+        N = B * T
+    else:
+        if len(lead) != 1:
+            raise ValueError(f"{name}: expected [N, heads, D], got {tuple(t.shape)}")
+        if row_starts.dim() != 1 or row_starts.numel() < 2:
+            raise ValueError(f"row_starts: expected [B + 1], got {tuple(row_starts.shape)}")
+        if n_new is not None:
+            raise ValueError("n_new and row_starts: rows one behind the other are counted by row_starts")
+        B, N = row_starts.numel() - 1, lead[0]
+        T = max(N, 1) if T_max is None else int(T_max)
+    _sized(ctx_lens, (B,), "ctx_lens"), _sized(n_new, (B,), "n_new")
+    return B, T, N
+
+
+def _row_strides(t, N, name, what):
+    """Strides of rows and heads of [..., H, D]."""
+    if t.stride(-1) != 1:
+        raise ValueError(f"{name}: the innermost axis must be contiguous")
+    step, head = _rows_stride(t, name), t.stride(-2) if t.shape[-2] > 1 else 0
+    if (N > 1 and step == 0) or (t.shape[-2] > 1 and head == 0):
+        raise ValueError(f"{name}: broadcast rows or heads; make {what} contiguous")
+    return step, head
+
+
+def _same_rows(out, of, name):
+    """An output like `of`: made here, or given with the same shape."""
+    if out is None:
+        return torch.empty(of.shape, dtype=torch.bfloat16, device=of.device)
+    return _sized(out, of.shape, name)
+
+
+def _rope_call(q, k, q_out, k_out, rope, positions, ctx_lens, row_starts, n_new, T_max):
+    rows = k if q is None else q
+    B, T, N = _new_rows(rows, ctx_lens, row_starts, n_new, T_max, "q" if rows is q else "k")
+    d = rope.desc()
+    d.B, d.T_max, d.N, d.D = B, T, N, rows.shape[-1]
+    if k is not None and tuple(k.shape[:-2]) + (k.shape[-1],) != tuple(rows.shape[:-2]) + (rows.shape[-1],):
+        raise ValueError(f"q, k: rows {tuple(rows.shape)} and {tuple(k.shape)} differ")
+    if d.rotary_dim > d.D:
+        raise ValueError(f"{d.rotary_dim} values are turned, a head has {d.D}")
+    for t, h, sn, sh, name in ((q, "Hq", "q_stride_n", "q_stride_h", "q"), (k, "Hkv", "kv_stride_n", "kv_stride_h", "k"),
+                               (q_out, None, "q_out_stride_n", "q_out_stride_h", "q_out"), (k_out, None, "k_out_stride_n", "k_out_stride_h", "k_out")):
+        if t is None:
+            continue
+        if h:
+            setattr(d, h, t.shape[-2])
+        step, head = _row_strides(t, N, name, "it")
+        setattr(d, sn, step), setattr(d, sh, head)
+    if positions is not None:
+        shape = (rope.axes, N) if positions.dim() != 1 or rope.axes > 1 else (N,)
+        if tuple(positions.shape) != shape and tuple(positions.shape) != (rope.axes,) + tuple(rows.shape[:-2]):
+            raise ValueError(f"positions: expected {shape}, got {tuple(positions.shape)}")
+    ptrs = (_ptr(_dense(rope.inv_freq, "inv_freq"), torch.float32, "inv_freq"), _i32p(positions, "positions"), _i32p(ctx_lens, "ctx_lens"),
+            _i32p(row_starts, "row_starts"), _i32p(n_new, "n_new"))
+    return d, ptrs
+
+
+def radar_rope(q, k, rope, positions=None, ctx_lens=None, row_starts=None, n_new=None, T_max=None, q_out=None, k_out=None, prepared=False):
+    """Rows of q bf16 [B,T,Hq,D] and k [B,T,Hkv,D] (or [N,...] with row_starts i32 [B+1], at most T_max rows of a sequence) turned by `rope`; either may be
+    None.  Row i of sequence b is at positions[:, n] (i32 [axes,N]; None: i) + ctx_lens[b] (i32 [B]; None: 0); n_new i32 [B] or None: so many rows of
+    [B,T] are there.  Rows that are not there, and those of sequences with ctx_lens[b] < 0, are left as they are in the outputs.  q_out and k_out may be q and k.
+    Returns (q_out, k_out)."""
+    if q is None and k is None:
+        raise ValueError("neither q nor k")
+    q_out = None if q is None else _same_rows(q_out, q, "q_out")
+    k_out = None if k is None else _same_rows(k_out, k, "k_out")
+    _here(q, k, q_out, k_out, rope.inv_freq, positions, ctx_lens, row_starts, n_new)
+    d, ptrs = _rope_call(q, k, q_out, k_out, rope, positions, ctx_lens, row_starts, n_new, T_max)
+    if d.N == 0:
+        return _nothing((q_out, k_out), prepared)
+    b16 = lambda t, name: _ptr(t, torch.bfloat16, name)                                              # noqa: E731
+    args = (b16(q, "q"), b16(k, "k"), b16(q_out, "q_out"), b16(k_out, "k_out"), *ptrs, ctypes.byref(d), _stream())
+    return _finish("radar_rope", load().radar_rope, args, (q, k, q_out, k_out, rope, rope.inv_freq, positions, ctx_lens, row_starts, n_new, d), (q_out, k_out), prepared)
+
+
+def _nothing(out, prepared):
+    """A call over no rows."""
+    return BoundCall("", lambda: RADAR_OK, (), (), out) if prepared else out
+
+
+def radar_kvq_append_rope(cache, q, k, v, slots, rope, positions=None, ctx_lens=None, row_starts=None, n_new=None, layer=0, q_out=None, prepared=False):
+    """radar_rope of q and k and, in the same launch, radar_kvq_append of k and v into `layer` of the KvqCache: row i of sequence b goes to slots[b,i] (i32
+    [B,T_max], as radar_kvq_blocks gives them).  k, v bf16 [B,T,Hkv,D] or [N,Hkv,D] with the same strides; q may be None.  Returns q_out."""
+    if slots.dim() != 2:
+        raise ValueError(f"slots: expected [B, T_max], got {tuple(slots.shape)}")
+    if tuple(k.shape) != tuple(v.shape) or tuple(k.shape[-2:]) != (cache.Hkv, cache.D) or k.stride() != v.stride():
+        raise ValueError(f"k, v: expected [..., {cache.Hkv}, {cache.D}] with the same strides, got {tuple(k.shape)} and {tuple(v.shape)}")
+    q_out = None if q is None else _same_rows(q_out, q, "q_out")
+    data = _layer(cache, layer)
+    _here(q, k, v, q_out, slots, data, rope.inv_freq, positions, ctx_lens, row_starts, n_new)
+    d, ptrs = _rope_call(q, k, q_out, None, rope, positions, ctx_lens, row_starts, n_new, slots.shape[1])
+    if slots.shape[0] != d.B:
+        raise ValueError(f"slots: expected {d.B} sequences, got {slots.shape[0]}")
+    if d.N == 0:
+        return _nothing(q_out, prepared)
+    c = cache.desc()
+    b16 = lambda t, name: _ptr(t, torch.bfloat16, name)                                              # noqa: E731
+    args = (b16(q, "q"), b16(k, "k"), b16(v, "v"), b16(q_out, "q_out"), *ptrs, _i32p(slots, "slots"), _ptr(data, torch.uint8, "cache"), ctypes.byref(d),
+            ctypes.byref(c), _stream())
+    keep = (cache, data, q, k, v, q_out, slots, rope, rope.inv_freq, positions, ctx_lens, row_starts, n_new, d, c)
+    return _finish("radar_kvq_append_rope", load().radar_kvq_append_rope, args, keep, q_out, prepared)
+
+
+def radar_chunk_attention_kvq_workspace_bytes(desc):
+    return int(load().radar_chunk_attention_kvq_workspace_bytes(ctypes.byref(desc)))
+
+
+def kvq_chunk_desc(q, cache, max_blocks, B, T_max, N, S_max=None, out=None, rows_per_split=0, softmax_scale=0.0):
+    d = KvqChunkDesc()
+    d.cache = cache.desc()
+    d.B, d.T_max, d.N, d.Hq = B, T_max, N, q.shape[-2]
+    d.max_blocks = int(max_blocks)
+    d.S_max = d.max_blocks * cache.block_rows if S_max is None else int(S_max)
+    d.rows_per_split, d.softmax_scale = int(rows_per_split), float(softmax_scale)
+    for t, name in ((q, "q"), (out, "out")):
+        for axis, of in zip(range(t.dim() - 1 if t is not None else 0), "bth"[4 - t.dim():] if t is not None else ""):
+            if t.shape[axis] > 1:
+                if t.stride(axis) == 0:
+                    raise ValueError(f"{name}: broadcast along axis {axis}; make it contiguous")
+                setattr(d, f"{name}_stride_{of}", t.stride(axis))
+    return d
+
+
+def radar_chunk_attention_kvq(q, cache, block_tables, ctx_lens, row_starts=None, n_new=None, T_max=None, layer=0, S_max=None, out=None, lse_out=None,
+                              workspace=None, rows_per_split=0, softmax_scale=0.0, prepared=False):
+    """Attention of new rows over `layer` of a KvqCache that holds them already: q bf16 [B,T,Hq,D] (n_new i32 [B] or None: so many rows are there) or
+    [N,Hq,D] with row_starts i32 [B+1], at most T_max rows of a sequence (default: N); row i of sequence b sees rows up to ctx_lens[b] + i.  block_tables i32
+    [B,M]; S_max: the rows in use (the longest ctx_lens + T_max), default all that the tables hold.  Returns out, like q; lse_out f32 without D."""
+    if q.shape[-1] != cache.D or q.stride(-1) != 1:
+        raise ValueError(f"q: expected [..., Hq, {cache.D}], the innermost axis contiguous")
+    B, T, N = _new_rows(q, ctx_lens, row_starts, n_new, T_max, "q")
+    M = _sized(block_tables, (B, block_tables.shape[-1]), "block_tables").shape[1]
+    out = _same_rows(out, q, "out")
+    _sized(lse_out, q.shape[:-1], "lse_out")
+    if out.stride(-1) != 1:
+        raise ValueError("out: the innermost axis must be contiguous")
+    data = _layer(cache, layer)
+    _here(q, data, block_tables, ctx_lens, row_starts, n_new, out, lse_out, workspace)
+    if N == 0:
+        return _nothing(out, prepared)
+    desc = kvq_chunk_desc(q, cache, M, B, T, N, S_max, out, rows_per_split, softmax_scale)
+    if workspace is None:
+        workspace = new_workspace(radar_chunk_attention_kvq_workspace_bytes(desc), q.device)
+    wp, wn = _ws_args(workspace)
+    args = (_ptr(q, torch.bfloat16, "q"), _ptr(data, torch.uint8, "cache"), _i32p(block_tables, "block_tables"), _i32p(ctx_lens, "ctx_lens"),
+            _i32p(row_starts, "row_starts"), _i32p(n_new, "n_new"), _ptr(out, torch.bfloat16, "out"),
+            _ptr(None if lse_out is None else _dense(lse_out, "lse_out"), torch.float32, "lse_out"), ctypes.byref(desc), wp, wn, _stream())
+    keep = (q, cache, data, block_tables, ctx_lens, row_starts, n_new, out, lse_out, desc, workspace)
+    return _finish("radar_chunk_attention_kvq", load().radar_chunk_attention_kvq, args, keep, out, prepared)
 
 
 # ------------------------------------------------------------ verification

@@ -30,6 +30,26 @@ __device__ __forceinline__ void kvq_decode8(uint32_t w, float scale, uint32_t (&
     out[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
 }
 
+// Eight values of a row as codes (the nibbles of the result, lowest first) and the scale byte of the 32 that they are among, which four neighbouring
+// lanes have between them: all four call.  The largest magnitude is found on the bit patterns (larger than 0x7f7f: not a number or infinite).
+// amax = (1 + m/128) 2^(E-127): the scale's exponent is E - 127 - 2, or one more from 1.75 on, where 6 would be too little by more than half a step.
+struct KvqCodes { uint32_t code, mark; };
+__device__ __forceinline__ KvqCodes kvq_encode8(uint32_t x0, uint32_t x1, uint32_t x2, uint32_t x3) {
+    auto two = [](uint32_t x) { return max(x & 0x7fffu, (x >> 16) & 0x7fffu); };
+    uint32_t top = max(max(two(x0), two(x1)), max(two(x2), two(x3)));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+    const bool sound = top < 0x7f80u;
+    const uint32_t byte = (uint32_t)min(max((int)(top >> 7) - 2 + ((top & 127u) >= 96u ? 1 : 0), 1), (int)kScaleMost);
+    const float scale = kvq_scale(byte);
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, x0), scale, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, x1), scale, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, x2), scale, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, x3), scale, 3);
+    return KvqCodes{sound ? w : 0u, sound ? byte : kScaleNaN};
+}
+
 // Which limits of radar_kvq_desc a call's descriptor breaks (host).
 inline radar_status kvq_check(const radar_kvq_desc *d) {
     if (!d || d->n_blocks < 1 || d->Hkv < 1 || d->block_rows < 1) return RADAR_INVALID_ARG;

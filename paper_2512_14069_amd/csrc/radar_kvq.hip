@@ -157,8 +157,7 @@ __global__ __launch_bounds__(256) void kvq_slots_kernel(BlArgs a) {
 // Eight rows of the input and one head take 2 * D lanes: the first half of them K, the other V, a lane eight values (16
 // bytes of bf16, 4 of codes).  All go along the rows where they touch values, and so do lanes of K at the codes, which lie in one piece; there lanes
 // of V go down the eight rows, whose codes of the same eight values lie side by side: where the rows follow each other in the cache (prompts, trees)
-// all store and load whole lines.  A word and a scale change lanes between the two orders.  The largest magnitude of 32 values is that of four lanes,
-// found on their bit patterns (larger than 0x7f7f: not a number or infinite).
+// all store and load whole lines.  A word and a scale change lanes between the two orders.
 constexpr int kRwThreads = 256, kRwGroups = 2048, kRwLayers = 4;
 
 struct RwArgs {
@@ -203,22 +202,9 @@ __global__ __launch_bounds__(kRwThreads) void kvq_append_kernel(RwArgs a) {
     const int64_t n = min(in.n, a.N - 1);      // (lanes past the end go along: the maximum is taken over whole wavefronts)
     const int slot = a.slots[min(r.n, a.N - 1)];
     const u32x4 x = *reinterpret_cast<const u32x4 *>((in.is_v ? a.v : a.k) + n * a.stride_n + in.h * a.stride_h + in.piece * 8);
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) top = max(top, max(x[i] & 0x7fffu, (x[i] >> 16) & 0x7fffu));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 1));             // four neighbours share a scale
-    top = max(top, (uint32_t)__shfl_xor((int)top, 2));
-    // amax = (1 + m/128) 2^(E-127): the scale's exponent is E - 127 - 2, or one more from 1.75 on, where 6 would be too little by more than half a step
-    const bool sound = top < 0x7f80u;
-    const uint32_t byte = (uint32_t)min(max((int)(top >> 7) - 2 + ((top & 127u) >= 96u ? 1 : 0), 1), (int)kScaleMost);
-    const float scale = kvq_scale(byte);
     const uint32_t x0 = x[0], x1 = x[1], x2 = x[2], x3 = x[3];      // (a bit cast of a vector's element would take its first)
-    uint32_t w = 0;
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, x0), scale, 0);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, x1), scale, 1);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, x2), scale, 2);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, __builtin_bit_cast(bf16x2, x3), scale, 3);
-    const uint32_t code = rw_turned(in.is_v, sound ? w : 0u), mark = rw_turned(in.is_v, sound ? byte : kScaleNaN);
+    const KvqCodes c = kvq_encode8(x0, x1, x2, x3);
+    const uint32_t code = rw_turned(in.is_v, c.code), mark = rw_turned(in.is_v, c.mark);
     if (r.n >= a.N || slot < 0 || slot >= a.total) return;
     const int R = 1 << a.rbits, row = slot & (R - 1);
     unsigned char *const chunk = a.cache + ((size_t)(slot >> a.rbits) * a.Hkv + r.h) * C::bytes(R);
