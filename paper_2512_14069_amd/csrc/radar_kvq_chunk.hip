@@ -14,72 +14,146 @@
 namespace radar {
 
 constexpr int kKcCols = 64;                    // columns of a block
-constexpr int kKcTarget = 512;                 // what long contexts are divided into, workgroups
+constexpr int kKcTarget = 1024;                // most workgroups that what is divided is dealt to, and most parts
 constexpr int kKcPlanned = 512;                // most sequences whose work every workgroup counts through
 constexpr int kKcArrived = 16;                 // counters are 64 bytes apart: atomics on one line wait for each other
 
 struct KcArgs : KqCache {
     const __bf16 *q;
     const unsigned char *cache;
-    const int32_t *tables, *ctx_lens, *row_starts, *n_new;
+    const int32_t *tables;
     __bf16 *out;
     float *lse;
-    int B, T, Hq, Hkv, G, M, S, N;
+    int Hq, M;
     int64_t q_sb, q_st, q_sh, o_sb, o_st, o_sh;
-    int target, least;                         // workgroups that divided work is dealt to (0: nothing is divided); least steps of one
-    float *part;                               // [2 * kKcTarget] partial results: outputs, maxima (log2 units) and sums, in fp32
+    float *part;                               // [kKcTarget] partial results: outputs, maxima (log2 units) and sums, in fp32
     unsigned int *arrived;                     // of a block's workgroups, kKcArrived words apart
 };
+// What a workgroup finds its work by: the kernel's leading arguments, which are in registers when it starts.
+struct KcWork {
+    const int32_t *ctx_lens, *row_starts, *n_new;
+    int B, T, N, S;
+    uint32_t heads;                            // KV heads, and their queries' heads above the 16th bit
+    uint32_t dealt;                            // workgroups that divided work is dealt to (0: nothing is divided), and log2 of a level's keys above the 16th bit
+    int least;                                 // least steps of a part
+    uint32_t by_G;                             // 2^16 / G, rounded up
+    __host__ __device__ int Hkv() const { return (int)(heads & 0xffff); }
+    __host__ __device__ int G() const { return (int)(heads >> 16); }
+    __host__ __device__ int target() const { return (int)(dealt & 0xffff); }
+    __host__ __device__ int level_bits() const { return (int)(dealt >> 16); }
+};
+constexpr size_t kKcArgsAt = (sizeof(KcWork) + alignof(KcArgs) - 1) / alignof(KcArgs) * alignof(KcArgs);      // of the block behind them
 
 // A sequence: rows of its prefix, new rows, rows that the tensors have for it, keys that its last row sees; the first of its rows.
 struct KcSeq { int L, n, rows, total, row0; };
-__device__ __forceinline__ KcSeq kc_seq(const KcArgs &a, int b) {
+template <bool UNIFORM = false>                // the same sequence in every lane
+__device__ __forceinline__ KcSeq kc_seq(const KcWork &a, int b) {
+    auto word = [](const int32_t *p, int i) { return UNIFORM ? uniform_word(p, i) : p[i]; };
     KcSeq s;
     if (a.row_starts) {
-        const int from = min(max(a.row_starts[b], 0), a.N), to = min(max(a.row_starts[b + 1], from), a.N);
+        const int from = min(max(word(a.row_starts, b), 0), a.N), to = min(max(word(a.row_starts, b + 1), from), a.N);
         s.rows = min(to - from, a.T);
         s.row0 = from;
         s.n = s.rows;
     } else {
         s.rows = a.T;
         s.row0 = b * a.T;
-        s.n = a.n_new ? min(max(a.n_new[b], 0), a.T) : a.T;
+        s.n = a.n_new ? min(max(word(a.n_new, b), 0), a.T) : a.T;
     }
-    s.L = min(a.ctx_lens[b], a.S);             // (so that the new rows can be added in 32 bits)
-    if (s.L < 0) s.n = 0;
+    s.L = min(word(a.ctx_lens, b), a.S);       // (so that the new rows can be added in 32 bits)
+    if (s.L < 0) s.n = 0, s.L = -1;
     s.total = s.n > 0 ? min(s.L + s.n, a.S) : 0;
     return s;
 }
 
-// What a workgroup does: a block of columns of a KV head and the steps [s0, s1) of it, one of `parts` such.
-struct KcItem { int b, hk, cg, n, rows, row0, L, limit, s0, s1, parts, slot, unit; };
+// n / d, n < 2^23, by the reciprocal and one step either way.
+__device__ __forceinline__ uint32_t kc_quotient(uint32_t n, uint32_t d) {
+    int q = (int)((float)n * __builtin_amdgcn_rcpf((float)d)), r = (int)(n - (uint32_t)q * d);
+    if (r < 0) --q;
+    else if (r >= (int)d) ++q;
+    return (uint32_t)q;
+}
+// (r0 + c) / G for a place r0 < G in a row and a column c < 64 behind it: at most 127 by 64 (exact with 16 bits), or at most once.
+__device__ __forceinline__ int kc_rows_on(int t, const KcWork &a) {
+    if (a.G() > kKcCols) return t >= a.G() ? 1 : 0;
+    return (int)((uint32_t)t * a.by_G >> 16);
+}
+
+// What a workgroup does: a block of columns of a KV head, the first of them of row i0, and the steps [s0, s1) of it, one of `parts` such.
+struct KcItem { int b, hk, cg, i0, n, rows, row0, L, limit, s0, s1, parts, slot, unit; };
 constexpr int kKcState = 16;
 
-// Every item in one line: sequence by sequence, from the last block of columns, which has the most keys, to the first, part by part and KV head by KV head
-// (workgroups go to the eight XCDs in turn: a head's rows then stay in one L2).  A sequence's blocks are divided into parts of `per` steps, which is
-// the batch's work over what it is dealt to, so that there are no more items than blocks and that, and no more parts than twice that.
+// Every item in one line, those with the most keys first, so that the workgroups that start last have little to do: by level (eighths or so of the longest
+// context that a block's first row sees), in it sequence by sequence, from the last block of columns to the first, part by part and KV head by KV head (workgroups go
+// to the eight XCDs in turn: a head's rows then stay in one L2).  A sequence's blocks are divided into parts of `per` steps or a little more, which is the batch's
+// work over the workgroups that it is dealt to, so that there are no more items than blocks and workgroups, and no more parts than workgroups.  A step
+// of 16 columns counts for half a step of 64.  The quotients are by reciprocals, rounded to the safe side, as this is a chain that every workgroup goes through.
 // All lanes call; the result is the same in all of them.
-__device__ __forceinline__ bool kc_find(KcItem &x, const KcArgs &a, uint32_t item) {
-    const int lane = lane_id();
-    auto blocks_of = [&](int rows) { return (int)(((int64_t)rows * a.G + kKcCols - 1) / kKcCols); };
-    int per = INT32_MAX, p = 1, cgs;
-    uint32_t rel, slots = 0, units = 0;
+constexpr int kKcLevels = 8;
+__device__ __forceinline__ int kc_blocks(int rows, int G) { return (rows * G + kKcCols - 1) / kKcCols; }           // (rows * G < 2^28)
+// Blocks of a sequence whose first row sees `keys` keys of others or more.
+__device__ __forceinline__ int kc_beyond(const KcSeq &s, int cgs, int G, int keys) { return cgs - kc_blocks(min(max(keys - s.L, 0), s.rows), G); }
+__device__ __forceinline__ int kc_cost(const KcSeq &s, int G) {      // of a block of the sequence, in steps of 64 columns
+    const int steps = (s.total + 31) >> 5;
+    return s.n * G <= 16 ? steps >> 1 : steps;
+}
+__device__ __forceinline__ bool kc_find(KcItem &x, const KcWork &a, uint32_t item) {
+    const int lane = lane_id(), Hkv = a.Hkv(), G = a.G();
+    int p = 1, cgs, back = 0;                  // back: blocks behind this one
+    uint32_t rel, slot0 = 0, unit0 = 0;        // rel: of the block's items; the sequence's first partial result and counter
     KcSeq s;
-    if (a.target > 0) {
-        double work = 0.0;                     // (whole numbers below 2^53)
+    if (a.B == 1) {                            // one sequence: nothing to count through, all of it in scalar registers
+        s = kc_seq<true>(a, 0);
+        cgs = kc_blocks(s.rows, G);
+        const uint32_t units = (uint32_t)(Hkv * cgs);
+        p = max(min(a.target() / (int)max(units, 1u), ((s.total + 31) >> 5) / a.least), 1);
+        if (item >= units * (uint32_t)p) return false;
+        x.b = 0;
+        rel = item;
+    } else if (a.target() > 0) {
+        auto seq = [&](int b0) { return kc_seq(a, min(b0 + lane, a.B - 1)); };
+        s = seq(0);
+        float work = 0.f;
         for (int b0 = 0; b0 < a.B; b0 += kWave) {
-            const KcSeq t = kc_seq(a, min(b0 + lane, a.B - 1));
-            if (b0 + lane < a.B) work += (double)blocks_of(t.rows) * (double)a.Hkv * (double)((t.total + 31) >> 5);
+            const KcSeq t = b0 == 0 ? s : seq(b0);
+            if (b0 + lane < a.B) work += (float)(kc_blocks(t.rows, G) * Hkv) * (float)kc_cost(t, G);
         }
-        per = max((int)fmin(ceil(wave_sum_f64(work) / (double)a.target), 1e9), a.least);
-        uint32_t first = 0;
+        // (rounded up and down by more than what the sums and the reciprocal are off)
+        const float per = fmaxf(wave_sum_f32(work) * 1.001f * __builtin_amdgcn_rcpf((float)a.target()), (float)a.least), inv = 0.999f * __builtin_amdgcn_rcpf(per);
+        auto parts = [&](const KcSeq &t) { return max((int)((float)kc_cost(t, G) * inv), 1); };
+        // the level: the highest on or above which there are more items than this one's number
+        const int bits = a.level_bits();
+        int level = 0;
+        uint32_t first = 0;                    // items above the level
+        if (bits < 31) {                       // (64 sequences at most)
+            const int c = kc_blocks(s.rows, G);
+            const uint32_t each = lane < a.B ? (uint32_t)(Hkv * parts(s)) : 0u;
+            int most = kKcLevels;              // no items there
+            while (most - level > 1) {
+                const int mid = (level + most) >> 1;
+                const uint32_t n = readlane_u32(wave_scan_u32(each * (uint32_t)kc_beyond(s, c, G, mid << bits)), kWave - 1);
+                if (n > item) level = mid;
+                else { most = mid; first = n; }
+            }
+        }
         int b0 = 0, hit = -1;
         for (; b0 < a.B; b0 += kWave) {
-            s = kc_seq(a, min(b0 + lane, a.B - 1));
-            cgs = blocks_of(s.rows);
-            p = max((((s.total + 31) >> 5) + per - 1) / per, 1);
-            const uint32_t mine = b0 + lane < a.B ? (uint32_t)(a.Hkv * cgs) : 0u, items = mine * (uint32_t)p;
-            const uint32_t incl = wave_scan_u32(items), split = wave_scan_u32(p > 1 ? items : 0u), whole = wave_scan_u32(p > 1 ? mine : 0u);
+            if (b0 > 0) s = seq(b0);
+            cgs = kc_blocks(s.rows, G);
+            p = parts(s);
+            const bool there = b0 + lane < a.B;
+            int lower = cgs, upper = 0;        // blocks on the level or above, and above
+            if (bits < 31) {
+                if (level > 0) lower = kc_beyond(s, cgs, G, level << bits);
+                if (level + 1 < kKcLevels) upper = kc_beyond(s, cgs, G, (level + 1) << bits);
+            }
+            const uint32_t mine = there ? (uint32_t)(Hkv * cgs) : 0u, items = there ? (uint32_t)(Hkv * (lower - upper) * p) : 0u;
+            const uint32_t incl = wave_scan_u32(items);
+            uint32_t split = 0, whole = 0;
+            if (__ballot(p > 1) != 0) {
+                split = wave_scan_u32(p > 1 ? mine * (uint32_t)p : 0u);
+                whole = wave_scan_u32(p > 1 ? mine : 0u);
+            }
             const uint64_t behind = __ballot(first + incl > item);
             if (behind != 0) {
                 hit = __ffsll((unsigned long long)behind) - 1;
@@ -87,15 +161,17 @@ __device__ __forceinline__ bool kc_find(KcItem &x, const KcArgs &a, uint32_t ite
                 if (rel >= readlane_u32(items, hit)) return false;   // (only where row_starts falls)
                 p = (int)readlane_u32((uint32_t)p, hit);
                 cgs = (int)readlane_u32((uint32_t)cgs, hit);
+                back = (int)readlane_u32((uint32_t)upper, hit);
                 if (p > 1) {
-                    slots += readlane_u32(split, hit) - readlane_u32(items, hit);
-                    units += readlane_u32(whole, hit) - readlane_u32(mine, hit);
+                    const uint32_t m = readlane_u32(mine, hit);
+                    slot0 += readlane_u32(split, hit) - m * (uint32_t)p;
+                    unit0 += readlane_u32(whole, hit) - m;
                 }
                 break;
             }
             first += readlane_u32(incl, kWave - 1);
-            slots += readlane_u32(split, kWave - 1);
-            units += readlane_u32(whole, kWave - 1);
+            slot0 += readlane_u32(split, kWave - 1);
+            unit0 += readlane_u32(whole, kWave - 1);
         }
         if (hit < 0) return false;
         x.b = b0 + hit;
@@ -103,46 +179,57 @@ __device__ __forceinline__ bool kc_find(KcItem &x, const KcArgs &a, uint32_t ite
         s.total = (int)readlane_u32((uint32_t)s.total, hit); s.row0 = (int)readlane_u32((uint32_t)s.row0, hit);
     } else {
         // too many sequences to count through: blocks of columns begin at first row * G / 64 + b, which leaves every sequence room
-        const int block = (int)(item / (uint32_t)a.Hkv);
+        const int block = (int)kc_quotient(item, (uint32_t)Hkv);
         int off;
         if (a.row_starts) {
-            auto begin = [&](int b) { return (int64_t)min(max(a.row_starts[b], 0), a.N) * a.G / kKcCols + b; };
+            auto begin = [&](int b) { return (int64_t)min(max(a.row_starts[b], 0), a.N) * G / kKcCols + b; };
             x.b = max(last_at_most(a.B, block, begin), 0);
             off = (int)begin(x.b);
         } else {
-            const int each = blocks_of(a.T);
+            const int each = kc_blocks(a.T, G);
             x.b = block / each;
             off = x.b * each;
         }
         x.b = __builtin_amdgcn_readfirstlane(x.b);
         if (x.b >= a.B) return false;
         s = kc_seq(a, x.b);
-        cgs = blocks_of(s.rows);
-        rel = (uint32_t)(block - off) * (uint32_t)a.Hkv + item % (uint32_t)a.Hkv;
+        cgs = kc_blocks(s.rows, G);
+        rel = item - (uint32_t)off * (uint32_t)Hkv;
         if (block < off || block - off >= cgs) return false;
     }
-    const uint32_t turn = rel / (uint32_t)a.Hkv, back = turn / (uint32_t)p;
-    x.hk = (int)(rel - turn * (uint32_t)a.Hkv);
-    x.cg = cgs - 1 - (int)back;
-    const int part = (int)(turn - back * (uint32_t)p);
+    const uint32_t turn = kc_quotient(rel, (uint32_t)Hkv), nth = p > 1 ? kc_quotient(turn, (uint32_t)p) : turn;
+    x.hk = (int)(rel - turn * (uint32_t)Hkv);
+    x.cg = cgs - 1 - back - (int)nth;
+    const int part = (int)(turn - nth * (uint32_t)p);
     x.n = s.n; x.rows = s.rows; x.row0 = s.row0; x.L = s.L;
-    const int c0 = x.cg * kKcCols, i0 = c0 / a.G, i1 = min((c0 + kKcCols - 1) / a.G, s.n - 1);
-    x.limit = i0 < s.n ? min(s.L + i1 + 1, s.total) : 0;
+    const int c0 = x.cg * kKcCols;
+    x.i0 = c0 / G;
+    const int i1 = min(x.i0 + kc_rows_on(c0 - x.i0 * G + kKcCols - 1, a), s.n - 1);
+    x.limit = x.i0 < s.n ? min(s.L + i1 + 1, s.total) : 0;
     const int steps = (x.limit + 31) >> 5;
-    int wanted = p > 1 ? max((steps + per - 1) / per, 1) : 1;
-    x.unit = (int)units + x.cg * a.Hkv + x.hk;
-    // (there is room by the bounds above; row_starts that falls may break them)
-    const int64_t slot0 = (int64_t)slots + rel - (int64_t)part * a.Hkv;
-    if (slot0 < 0 || slot0 + (int64_t)(wanted - 1) * a.Hkv >= 2 * kKcTarget || (uint32_t)x.unit >= (uint32_t)kKcTarget) wanted = 1;
-    const int each = (steps + wanted - 1) / wanted;
-    x.parts = steps > 0 ? (steps + each - 1) / each : 1;
-    if (part >= x.parts) return false;
+    x.unit = (int)unit0 + x.cg * Hkv + x.hk;
+    x.slot = 0;
+    x.parts = 1;
+    int each = steps;
+    if (p > 1) {
+        // of a sequence that is divided, as many parts as are as long as its last block's
+        const int longest = (s.total + 31) >> 5, wanted_steps = (longest + p - 1) / p;
+        int wanted = min((steps + wanted_steps - 1) / max(wanted_steps, 1), p);
+        x.slot = (int)(slot0 + (uint32_t)(x.cg * Hkv + x.hk) * (uint32_t)p);
+        // (there is room by the bounds above; row_starts that falls may break them)
+        if (x.cg < 0 || x.slot < 0 || x.slot > kKcTarget - wanted || (uint32_t)x.unit >= (uint32_t)kKcTarget) wanted = 1;
+        each = (steps + wanted - 1) / max(wanted, 1);
+        if (steps > 0) x.parts = (steps + each - 1) / each;
+        x.slot += part;
+    }
+    if (x.cg < 0 || part >= x.parts) return false;
     x.s0 = part * each;
     x.s1 = min(x.s0 + each, steps);
-    x.slot = (int)(slots + rel);
     return true;
 }
 
+// An item waits in LDS, of which every wavefront has its own copy: taken from there it is in scalar registers, and nothing that was worked out to find it
+// is kept in vector registers through the loop (which would spill).
 template <typename T>
 __device__ __forceinline__ T kc_recall(const int *from) {            // the same in every lane
     constexpr int N = sizeof(T) / 4;
@@ -161,41 +248,34 @@ __device__ __forceinline__ void kc_remember(int *to, KcItem x) {
 }
 
 // The arguments, read where a phase of the kernel needs them.
-__device__ __forceinline__ KcArgs kc_args_plan() {
-    const ArgBlock<KcArgs> g = args_from_here<KcArgs>(0);
-    KcArgs a;
-    a.ctx_lens = g->ctx_lens; a.row_starts = g->row_starts; a.n_new = g->n_new; a.B = g->B; a.T = g->T; a.Hkv = g->Hkv; a.G = g->G; a.S = g->S; a.N = g->N;
-    a.target = g->target; a.least = g->least;
+__device__ __forceinline__ KcWork kc_args_work() {
+    const ArgBlock<KcWork> g = args_from_here<KcWork>(0);
+    KcWork a;
+    a.row_starts = g->row_starts; a.heads = g->heads; a.by_G = g->by_G;
     return a;
 }
 __device__ __forceinline__ KcArgs kc_args_loop() {
-    const ArgBlock<KcArgs> g = args_from_here<KcArgs>(0);
+    const ArgBlock<KcArgs> g = args_from_here<KcArgs>(kKcArgsAt);
     KcArgs a;
     a.tables = g->tables; a.cache = g->cache; a.M = g->M; a.rbits = g->rbits; a.n_blocks = g->n_blocks; a.block_bytes = g->block_bytes;
-    a.scale_log2 = g->scale_log2; a.G = g->G;
-    return a;
-}
-__device__ __forceinline__ KcArgs kc_args_query() {
-    const ArgBlock<KcArgs> g = args_from_here<KcArgs>(0);
-    KcArgs a;
-    a.q = g->q; a.q_sb = g->q_sb; a.q_st = g->q_st; a.q_sh = g->q_sh; a.G = g->G; a.row_starts = g->row_starts;
+    a.scale_log2 = g->scale_log2; a.q = g->q; a.q_sb = g->q_sb; a.q_st = g->q_st; a.q_sh = g->q_sh;
     return a;
 }
 __device__ __forceinline__ KcArgs kc_args_end() {
-    const ArgBlock<KcArgs> g = args_from_here<KcArgs>(0);
+    const ArgBlock<KcArgs> g = args_from_here<KcArgs>(kKcArgsAt);
     KcArgs a;
-    a.out = g->out; a.o_sb = g->o_sb; a.o_st = g->o_st; a.o_sh = g->o_sh; a.lse = g->lse; a.G = g->G; a.Hq = g->Hq; a.part = g->part;
-    a.row_starts = g->row_starts; a.arrived = g->arrived; a.scale_log2 = g->scale_log2;
+    a.out = g->out; a.o_sb = g->o_sb; a.o_st = g->o_st; a.o_sh = g->o_sh; a.lse = g->lse; a.Hq = g->Hq; a.part = g->part; a.arrived = g->arrived;
+    a.scale_log2 = g->scale_log2;
     return a;
 }
 
 // Where row i, head h of an item's sequence is in out, and its place in lse.
-__device__ __forceinline__ __bf16 *kc_out(const KcArgs &a, const KcItem &x, int i, int h) {
-    const size_t row = a.row_starts ? (size_t)(x.row0 + i) * a.o_st : (size_t)x.b * a.o_sb + (size_t)i * a.o_st;
+__device__ __forceinline__ __bf16 *kc_out(const KcArgs &a, bool packed, const KcItem &x, int i, int h) {
+    const size_t row = packed ? (size_t)(x.row0 + i) * a.o_st : (size_t)x.b * a.o_sb + (size_t)i * a.o_st;
     return a.out + row + (size_t)h * a.o_sh;
 }
 template <int N>
-__device__ __forceinline__ void kc_write(const KcArgs &a, const KcItem &x, int i, int h, int d, const float (&acc)[N], float M, float l) {
+__device__ __forceinline__ void kc_write(const KcArgs &a, bool packed, const KcItem &x, int i, int h, int d, const float (&acc)[N], float M, float l) {
     const float inv = l == 0.f ? 0.f : 1.0f / l;                     // (no key seen)
     __bf16 o[N] __attribute__((aligned(16)));
 #pragma unroll
@@ -203,7 +283,7 @@ __device__ __forceinline__ void kc_write(const KcArgs &a, const KcItem &x, int i
     typedef uint32_t words __attribute__((ext_vector_type(N / 2)));
     words w;
     __builtin_memcpy(&w, o, sizeof(w));
-    *reinterpret_cast<words *>(kc_out(a, x, i, h) + d) = w;
+    *reinterpret_cast<words *>(kc_out(a, packed, x, i, h) + d) = w;
     if (a.lse && d == 0) a.lse[(size_t)(x.row0 + i) * a.Hq + h] = l == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(l)) * kqLn2;
 }
 
@@ -217,53 +297,63 @@ struct KcShape {
     }
     static constexpr int PART = COLS * D + 2 * COLS;                 // floats of a partial result
 };
-template <int D, int KW>
-constexpr int kc_lds_bytes() { return KcShape<D, 4, KW>::room() + (KW + 1) * kKcCols * 8 + kKcCols * 4 + KW * kKcState * 4; }
+// NC: of the widest block that the kernel takes.
+template <int D, int NC, int KW>
+constexpr int kc_lds_bytes() { return KcShape<D, NC, KW>::room() + (KW + 1) * 16 * NC * 8 + 16 * NC * 4 + KW * kKcState * 4; }
 
 // One item.  KW wavefronts take its steps in turn and meet in LDS at the end.
-template <int D, int NC, int KW, bool FAR>
+template <int D, int NC, int MOST, int KW, bool FAR>
 __device__ __forceinline__ void kc_item(unsigned char *smem, const int *state) {
     using S = KcShape<D, NC, KW>;
     constexpr int THREADS = KW * kWave;
     u32x4 *const s_q = reinterpret_cast<u32x4 *>(smem);              // [column block][chunk][lane], the lanes' operands
     float *const s_o = reinterpret_cast<float *>(smem);              // [wavefront][column][ROW]
-    float *const s_m = reinterpret_cast<float *>(smem + KcShape<D, 4, KW>::room()), *const s_l = s_m + KW * kKcCols;
-    float *const s_M = s_l + KW * kKcCols, *const s_L = s_M + kKcCols;
-    int *const s_lim = reinterpret_cast<int *>(s_L + kKcCols);       // keys that a column sees
+    float *const s_m = reinterpret_cast<float *>(smem + KcShape<D, MOST, KW>::room()), *const s_l = s_m + KW * 16 * MOST;
+    float *const s_M = s_l + KW * 16 * MOST, *const s_L = s_M + 16 * MOST;
+    int *const s_lim = reinterpret_cast<int *>(s_L + 16 * MOST);       // keys that a column sees
     const int lane = lane_id(), w = KW > 1 ? __builtin_amdgcn_readfirstlane(wave_id()) : 0, r = lane & 15, grp = lane >> 4;
 
     KcItem p = kc_recall<KcItem>(state);
     KcArgs a = kc_args_loop();
+    const KcWork g = kc_args_work();
     const int32_t *const table = (const int32_t *)(uintptr_t)kq_scalar(a.tables + (size_t)p.b * a.M);
     const kq_bytes base = (kq_bytes)(uintptr_t)kq_scalar(a.cache + (size_t)p.hk * KvqChunk<D>::bytes(1 << a.rbits));
-    const int mine = p.s0 + w;
-    const int hidden = min(p.L + p.cg * kKcCols / a.G + 1, p.limit);           // of the first column
+    const int mine = p.s0 + w, hidden = min(p.L + p.i0 + 1, p.limit);          // (keys that the first column sees)
+    const bool active = mine < p.s1;
     KqK<D> k;
     KqV v;
     KqIds id{0, 0}, nid{0, 0};
-    if (mine < p.s1) {
+    if (active) {
         id = kq_ids(a, table, mine * 32, p.limit);
         nid = kq_ids(a, table, min(mine + KW, p.s1 - 1) * 32, p.limit);
+    }
+    // the queries are asked for while the blocks' numbers are on their way, and the first step's codes behind them
+    constexpr int QS = (NC * S::CH + KW - 1) / KW;
+    u32x4 y[QS];
+    {
+        const int G = g.G(), r0 = p.cg * kKcCols - p.i0 * G;
+        const __bf16 *const q0 = a.q + (g.row_starts ? (size_t)p.row0 * a.q_st : (size_t)p.b * a.q_sb) + (size_t)(p.hk * G) * a.q_sh;
+#pragma unroll
+        for (int j = 0; j < QS; ++j) {
+            const int x = w + j * KW, t = r0 + x / S::CH * 16 + r, on = kc_rows_on(t, g), i = p.i0 + on;
+            y[j] = u32x4{0, 0, 0, 0};
+            if (i < p.n && x < NC * S::CH) y[j] = *reinterpret_cast<const u32x4 *>(q0 + (size_t)i * a.q_st + (size_t)(t - on * G) * a.q_sh + (D / 4) * grp + 8 * (x % S::CH));
+        }
+        if (w == 0 && lane < S::COLS) {
+            const int i = p.i0 + kc_rows_on(r0 + lane, g);
+            s_lim[lane] = i < p.n ? min(p.L + i + 1, p.limit) : 0;
+        }
+    }
+    if (active) {
         const KqBase at = kq_base<D>(a, base, id, mine * 32);
         int lane2 = lane;
         asm volatile("" : "+v"(lane2));
         kq_load_k<D, FAR>(k, at, lane2);
         kq_load_v<D, FAR>(v, a, at, lane2);
     }
-    {
-        const KcArgs aq = kc_args_query();
-        const __bf16 *const q0 = aq.q + (aq.row_starts ? (size_t)p.row0 * aq.q_st : (size_t)p.b * aq.q_sb) + (size_t)(p.hk * aq.G) * aq.q_sh;
-        for (int x = w; x < NC * S::CH; x += KW) {
-            const int col = p.cg * kKcCols + x / S::CH * 16 + r, i = col / aq.G;
-            u32x4 y = {0, 0, 0, 0};
-            if (i < p.n) y = *reinterpret_cast<const u32x4 *>(q0 + (size_t)i * aq.q_st + (size_t)(col - i * aq.G) * aq.q_sh + (D / 4) * grp + 8 * (x % S::CH));
-            s_q[x * kWave + lane] = y;
-        }
-        if (w == 0 && lane < S::COLS) {
-            const int i = (p.cg * kKcCols + lane) / aq.G;
-            s_lim[lane] = i < p.n ? min(p.L + i + 1, p.limit) : 0;
-        }
-    }
+#pragma unroll
+    for (int j = 0; j < QS; ++j)
+        if (w + j * KW < NC * S::CH) s_q[(w + j * KW) * kWave + lane] = y[j];
     if (lane < S::COLS) s_m[w * S::COLS + lane] = -kKqNone;          // the references of this wavefront's columns, as scores
     floatx4 oacc[S::NM][NC];
     float negref[NC], l_run[NC];
@@ -294,11 +384,15 @@ __device__ __forceinline__ void kc_item(unsigned char *smem, const int *state) {
     __builtin_amdgcn_s_setprio(0);
 
     a = kc_args_end();
+    const KcWork e = kc_args_work();
+    const int G = e.G();
+    const bool packed = e.row_starts != nullptr;
     p = kc_recall<KcItem>(state);
+    const int r0 = p.cg * kKcCols - p.i0 * G;
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));                                    // (addresses are worked out here, and not kept from the start)
     const int r2 = tid & 15, grp2 = (tid >> 4) & 3;
-    const int live = min(p.n * a.G - p.cg * kKcCols, S::COLS);       // columns of the block that there are
+    const int live = min(p.n * G - p.cg * kKcCols, S::COLS);         // columns of the block that there are
     float *const to = a.part + (size_t)p.slot * KcShape<D, 4, KW>::PART;
     auto hand_over = [&](int col, int d, float x0, float x1) {
         store_shared_result(reinterpret_cast<uint64_t *>(to + col * D + d), (uint64_t)__float_as_uint(x1) << 32 | __float_as_uint(x0));
@@ -314,7 +408,7 @@ __device__ __forceinline__ void kc_item(unsigned char *smem, const int *state) {
     if constexpr (KW == 1) {
 #pragma unroll
         for (int n = 0; n < NC; ++n) {
-            const int col = n * 16 + r2, gc = p.cg * kKcCols + col, i = gc / a.G, h = p.hk * a.G + gc - i * a.G;
+            const int col = n * 16 + r2, on = kc_rows_on(r0 + col, e), i = p.i0 + on, h = p.hk * G + r0 + col - on * G;
             const float l = kq_column_sum(l_run[n]), M = reference(n, l);
             if (col >= live) continue;
 #pragma unroll
@@ -328,7 +422,7 @@ __device__ __forceinline__ void kc_item(unsigned char *smem, const int *state) {
                     for (int m = 0; m < S::NM; m += 2) hand_over(col, d + m, x[m], x[m + 1]);
                     if (d == 0) hand_over_sum(col, M, l);
                 } else {
-                    kc_write(a, p, i, h, d, x, M, l);
+                    kc_write(a, packed, p, i, h, d, x, M, l);
                 }
             }
         }
@@ -375,7 +469,7 @@ __device__ __forceinline__ void kc_item(unsigned char *smem, const int *state) {
             __syncthreads();
             int lane2 = threadIdx.x;
             asm volatile("" : "+v"(lane2));
-            const int col = lane2 / TPC, mx = lane2 % TPC * 4, gc = p.cg * kKcCols + col, i = gc / a.G, h = p.hk * a.G + gc - i * a.G;
+            const int col = lane2 / TPC, mx = lane2 % TPC * 4, on = kc_rows_on(r0 + col, e), i = p.i0 + on, h = p.hk * G + r0 + col - on * G;
             if (col < live) {
                 const float M = s_M[col], l = s_L[col];
 #pragma unroll
@@ -390,26 +484,25 @@ __device__ __forceinline__ void kc_item(unsigned char *smem, const int *state) {
                         if (d == 0) hand_over_sum(col, M, l);
                     } else {
                         const float o[4] = {acc[0], acc[1], acc[2], acc[3]};
-                        kc_write(a, p, i, h, d, o, M, l);
+                        kc_write(a, packed, p, i, h, d, o, M, l);
                     }
                 }
             }
         }
     }
     if (p.parts == 1) return;
-    // The block's workgroup that arrives last has all the parts, its own among them, join.  (A part's slots lie Hkv items apart, as the items do.)
+    // The block's workgroup that arrives last has all the parts, its own among them, join.
     __syncthreads();
     unsigned int *const counter = a.arrived + p.unit * kKcArrived;
     if ((int)publish_then_ticket(counter, reinterpret_cast<unsigned int *>(s_m)) != p.parts - 1) return;
     if (threadIdx.x == 0) store_shared_result(counter, 0u);
-    const KcArgs b = kc_args_plan();
-    const int each = (((p.limit + 31) >> 5) + p.parts - 1) / p.parts, first_slot = p.slot - p.s0 / each * b.Hkv;
-    const float *const from = a.part + (size_t)first_slot * KcShape<D, 4, KW>::PART;
-    const size_t apart = (size_t)b.Hkv * KcShape<D, 4, KW>::PART;
+    const int each = (((p.limit + 31) >> 5) + p.parts - 1) / p.parts;
+    const float *const from = a.part + (size_t)(p.slot - p.s0 / each) * KcShape<D, 4, KW>::PART;
+    constexpr size_t apart = KcShape<D, 4, KW>::PART;
     int first = threadIdx.x;
     asm volatile("" : "+v"(first));
     for (int x = first; x < live * (D / 4); x += THREADS) {
-        const int col = x / (D / 4), d = x % (D / 4) * 4, gc = p.cg * kKcCols + col, i = gc / a.G, h = p.hk * a.G + gc - i * a.G;
+        const int col = x / (D / 4), d = x % (D / 4) * 4, on = kc_rows_on(r0 + col, e), i = p.i0 + on, h = p.hk * G + r0 + col - on * G;
         float M = -kKqNone, l = 0.f;
         floatx4 acc = {0.f, 0.f, 0.f, 0.f};
         constexpr int U = 4;
@@ -439,33 +532,37 @@ __device__ __forceinline__ void kc_item(unsigned char *smem, const int *state) {
             }
         }
         const float o[4] = {acc[0], acc[1], acc[2], acc[3]};
-        kc_write(a, p, i, h, d, o, M, l);
+        kc_write(a, packed, p, i, h, d, o, M, l);
     }
 }
 
-template <int D, int KW, bool FAR>
-__global__ __launch_bounds__(KW * kWave, 2) void kvq_chunk_kernel(KcArgs) {
+// MOST = 1: for calls whose sequences have 16 columns at most (single tokens), with registers for twice as many wavefronts.
+template <int D, int MOST, int KW, bool FAR>
+__global__ __launch_bounds__(KW * kWave, MOST == 1 ? 4 : 2) void kvq_chunk_kernel(const int32_t *ctx_lens, const int32_t *row_starts, const int32_t *n_new, int B, int T, int N,
+                                                                                 int S, uint32_t heads, uint32_t dealt, int least, uint32_t by_G, KcArgs) {
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
-    int *const state = reinterpret_cast<int *>(smem + kc_lds_bytes<D, KW>() - KW * kKcState * 4) + (KW > 1 ? wave_id() : 0) * kKcState;
+    int *const state = reinterpret_cast<int *>(smem + kc_lds_bytes<D, MOST, KW>() - KW * kKcState * 4) + (KW > 1 ? wave_id() : 0) * kKcState;
+    const KcWork work{ctx_lens, row_starts, n_new, B, T, N, S, heads, dealt, least, by_G};
     KcItem p;
-    {
-        const KcArgs a = kc_args_plan();
-        if (!kc_find(p, a, blockIdx.x)) return;                      // (the same in all wavefronts)
-        kc_remember(state, p);
-        const int c0 = p.cg * kKcCols, live = min(max(p.n * a.G - c0, 0), kKcCols), there = min(p.rows * a.G - c0, kKcCols);
-        if (live < there && p.s0 == 0) {                             // rows that are not there, of sequences that are not there: zeros
-            const KcArgs e = kc_args_end();
-            for (int x = threadIdx.x; x < (there - live) * (D / 8); x += KW * kWave) {
-                const int gc = c0 + live + x / (D / 8), i = gc / a.G, h = p.hk * a.G + gc - i * a.G;
-                *reinterpret_cast<u32x4 *>(kc_out(e, p, i, h) + x % (D / 8) * 8) = u32x4{0, 0, 0, 0};
-                if (e.lse && x % (D / 8) == 0) e.lse[(size_t)(p.row0 + i) * e.Hq + h] = 0.f;
-            }
+    if (!kc_find(p, work, blockIdx.x)) return;                       // (the same in all wavefronts)
+    kc_remember(state, p);
+    const int G = work.G(), c0 = p.cg * kKcCols, live = min(max(p.n * G - c0, 0), kKcCols), there = min(p.rows * G - c0, kKcCols);
+    if (live < there && p.s0 == 0) {                                 // rows that are not there, of sequences that are not there: zeros
+        const KcArgs e = kc_args_end();
+        for (int x = threadIdx.x; x < (there - live) * (D / 8); x += KW * kWave) {
+            const int t = c0 - p.i0 * G + live + x / (D / 8), on = kc_rows_on(t, work), i = p.i0 + on, h = p.hk * G + t - on * G;
+            *reinterpret_cast<u32x4 *>(kc_out(e, row_starts != nullptr, p, i, h) + x % (D / 8) * 8) = u32x4{0, 0, 0, 0};
+            if (e.lse && x % (D / 8) == 0) e.lse[(size_t)(p.row0 + i) * e.Hq + h] = 0.f;
         }
-        if (live == 0) return;
     }
-    const int live = p.n * kc_args_plan().G - p.cg * kKcCols;
-    if (__builtin_amdgcn_readfirstlane(live) <= 16) kc_item<D, 1, KW, FAR>(smem, state);
-    else kc_item<D, 4, KW, FAR>(smem, state);
+    if (live == 0) return;
+    if constexpr (MOST == 1) {
+        kc_item<D, 1, MOST, KW, FAR>(smem, state);
+    } else {
+        if (__builtin_amdgcn_readfirstlane(live) <= 16) kc_item<D, 1, MOST, KW, FAR>(smem, state);
+        else if (__builtin_amdgcn_readfirstlane(live) <= 32) kc_item<D, 2, MOST, KW, FAR>(smem, state);
+        else kc_item<D, 4, MOST, KW, FAR>(smem, state);
+    }
 }
 
 }  // namespace radar
@@ -494,8 +591,38 @@ struct KcRoom { size_t off_part, bytes; };
 static KcRoom chunk_room(int D) {
     KcRoom r;
     r.off_part = (size_t)kKcTarget * kKcArrived * sizeof(unsigned int);       // counters first: all calls leave them at zero
-    r.bytes = r.off_part + (size_t)2 * kKcTarget * kKcCols * (D + 2) * sizeof(float);
+    r.bytes = r.off_part + (size_t)kKcTarget * kKcCols * (D + 2) * sizeof(float);
     return r;
+}
+
+struct KcPlan {
+    int kw, target, least, level_bits;
+    bool narrow;
+    int64_t items;
+};
+static KcPlan plan_chunk(const radar_kvq_chunk_desc *d, int64_t blocks) {
+    KcPlan p;
+    const int64_t units = blocks * d->cache.Hkv, G = d->Hq / d->cache.Hkv;
+    p.narrow = (int64_t)d->T_max * G <= 16;
+    const double hi = (d->S_max + 31) / 32, lo = std::max(d->S_max - d->T_max, 0) / 32, mid = 0.5 * (hi + lo);
+    // us: a round of steps with one and with two wavefronts a SIMD; what a block costs besides
+    double best = 1e300;
+    p.kw = p.narrow && units >= 1024 ? 4 : 8;
+    for (int x = 0; x < 4 && !p.narrow; ++x) {
+        const int kw = 1 << x;
+        const double end[] = {4.0, 5.5, 7.0, 12.0}, slots = 2048.0 / kw, round = units * kw <= 1024 ? 1.27 : 1.65;
+        const double one = hi / kw * round + end[x], all = (double)units / slots * (mid / kw * round + end[x]), us = std::max(one, all);
+        if (us < best) { best = us; p.kw = kw; }
+    }
+    p.target = d->B <= kKcPlanned ? std::min(kKcTarget, (p.narrow ? 4096 : 2048) / p.kw) : 0;
+    // the least steps of a part: a part costs about a third of a round to join, so that the longest context is best divided by the root of its steps
+    // (us, one sequence of 16384 rows, a single token, parts of 16 / 32 steps: 13.4 12.6; 2048 rows 9.2 10.9, 64 rows behind them 20.1 23.2)
+    p.least = d->rows_per_split ? d->rows_per_split / 32 : std::max(2 * p.kw, (int)(1.5 * std::sqrt(hi)));
+    p.level_bits = 31;
+    if (d->B > 1 && d->B <= kWave)                         // (one sequence's blocks are in that order anyway)
+        for (p.level_bits = 5; ((int64_t)d->S_max >> p.level_bits) >= kKcLevels; ++p.level_bits) {}
+    p.items = units + p.target;
+    return p;
 }
 
 extern "C" size_t radar_chunk_attention_kvq_workspace_bytes(const radar_kvq_chunk_desc *d) {
@@ -503,20 +630,29 @@ extern "C" size_t radar_chunk_attention_kvq_workspace_bytes(const radar_kvq_chun
     return chunk_room(d->cache.D).bytes;
 }
 
-template <int D, int KW, bool FAR>
-static hipError_t launch_chunk(const KcArgs &a, int64_t items, hipStream_t s) {
-    constexpr int bytes = kc_lds_bytes<D, KW>();
+template <int D, int MOST, int KW, bool FAR>
+static hipError_t launch_chunk(const KcWork &w, const KcArgs &a, int64_t items, hipStream_t s) {
+    constexpr int bytes = kc_lds_bytes<D, MOST, KW>();
     static std::atomic<uint64_t> configured{0};            // devices on which the kernel may have so much LDS (two threads may both say so)
     int device = 0;
     hipError_t e = hipGetDevice(&device);
     if (e != hipSuccess) return e;
     const uint64_t bit = 1ull << (device & 63);
     if (device > 63 || !(configured.load(std::memory_order_relaxed) & bit)) {
-        e = hipFuncSetAttribute(reinterpret_cast<const void *>(&kvq_chunk_kernel<D, KW, FAR>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        e = hipFuncSetAttribute(reinterpret_cast<const void *>(&kvq_chunk_kernel<D, MOST, KW, FAR>), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
         if (e != hipSuccess) return e;
         configured.fetch_or(bit, std::memory_order_relaxed);
     }
-    return launch("kvq_chunk", kvq_chunk_kernel<D, KW, FAR>, dim3((unsigned)items), dim3(KW * kWave), bytes, s, a);
+    return launch("kvq_chunk", kvq_chunk_kernel<D, MOST, KW, FAR>, dim3((unsigned)items), dim3(KW * kWave), bytes, s, w.ctx_lens, w.row_starts, w.n_new,
+                  w.B, w.T, w.N, w.S, w.heads, w.dealt, w.least, w.by_G, a);
+}
+template <int D, bool FAR>
+static hipError_t launch_chunk(const KcWork &w, const KcArgs &a, const KcPlan &p, hipStream_t s) {
+    if (p.narrow) return p.kw == 8 ? launch_chunk<D, 1, 8, FAR>(w, a, p.items, s) : launch_chunk<D, 1, 4, FAR>(w, a, p.items, s);
+    return p.kw == 8   ? launch_chunk<D, 4, 8, FAR>(w, a, p.items, s)
+           : p.kw == 4 ? launch_chunk<D, 4, 4, FAR>(w, a, p.items, s)
+           : p.kw == 2 ? launch_chunk<D, 4, 2, FAR>(w, a, p.items, s)
+                       : launch_chunk<D, 4, 1, FAR>(w, a, p.items, s);
 }
 
 extern "C" radar_status radar_chunk_attention_kvq(const void *q, const void *cache, const int32_t *block_tables, const int32_t *ctx_lens,
@@ -533,9 +669,9 @@ extern "C" radar_status radar_chunk_attention_kvq(const void *q, const void *cac
     if (((uintptr_t)workspace & 255) != 0) return RADAR_INVALID_ARG;
     KcArgs a;
     a.q = static_cast<const __bf16 *>(q); a.cache = static_cast<const unsigned char *>(cache);
-    a.tables = block_tables; a.ctx_lens = ctx_lens; a.row_starts = row_starts; a.n_new = n_new;
+    a.tables = block_tables;
     a.out = static_cast<__bf16 *>(out); a.lse = lse_out;
-    a.B = d->B; a.T = d->T_max; a.Hq = d->Hq; a.Hkv = (int)Hkv; a.G = a.Hq / a.Hkv; a.M = d->max_blocks; a.S = d->S_max; a.N = (int)d->N;
+    a.Hq = d->Hq; a.M = d->max_blocks;
     a.rbits = kvq_log2(d->cache.block_rows); a.n_blocks = d->cache.n_blocks;
     const int64_t D = d->cache.D;
     a.block_bytes = Hkv * d->cache.block_rows * (D + D / 16);
@@ -553,21 +689,12 @@ extern "C" radar_status radar_chunk_attention_kvq(const void *q, const void *cac
     char *ws = static_cast<char *>(workspace);
     a.arrived = reinterpret_cast<unsigned int *>(ws);
     a.part = reinterpret_cast<float *>(ws + room.off_part);
-    const int64_t units = blocks * Hkv;
-    const int kw = units < 512 ? 8 : units < 1024 ? 4 : units < 4096 ? 2 : 1;
-    a.target = d->B <= kKcPlanned ? kKcTarget : 0;
-    a.least = d->rows_per_split ? d->rows_per_split / 32 : 4 * kw;
-    const int64_t items = units + a.target;
+    const KcPlan p = plan_chunk(d, blocks);
+    const KcWork w{ctx_lens, row_starts, n_new, d->B, d->T_max, (int)d->N, d->S_max, (uint32_t)Hkv | (uint32_t)(d->Hq / d->cache.Hkv) << 16,
+                   (uint32_t)p.target | (uint32_t)p.level_bits << 16, p.least, (uint32_t)((65535 + d->Hq / Hkv) / (d->Hq / Hkv))};
     hipStream_t s = static_cast<hipStream_t>(stream);
     const bool far = (int64_t)a.n_blocks * a.block_bytes > UINT32_MAX;
-    auto go = [&](auto near_kernel, auto far_kernel) { return far ? far_kernel(a, items, s) : near_kernel(a, items, s); };
-    const hipError_t e = D == 128 ? (kw == 8   ? go(launch_chunk<128, 8, false>, launch_chunk<128, 8, true>)
-                                     : kw == 4 ? go(launch_chunk<128, 4, false>, launch_chunk<128, 4, true>)
-                                     : kw == 2 ? go(launch_chunk<128, 2, false>, launch_chunk<128, 2, true>)
-                                               : go(launch_chunk<128, 1, false>, launch_chunk<128, 1, true>))
-                                  : (kw == 8   ? go(launch_chunk<64, 8, false>, launch_chunk<64, 8, true>)
-                                     : kw == 4 ? go(launch_chunk<64, 4, false>, launch_chunk<64, 4, true>)
-                                     : kw == 2 ? go(launch_chunk<64, 2, false>, launch_chunk<64, 2, true>)
-                                               : go(launch_chunk<64, 1, false>, launch_chunk<64, 1, true>));
+    const hipError_t e = D == 128 ? (far ? launch_chunk<128, true>(w, a, p, s) : launch_chunk<128, false>(w, a, p, s))
+                                  : (far ? launch_chunk<64, true>(w, a, p, s) : launch_chunk<64, false>(w, a, p, s));
     return e == hipSuccess ? RADAR_OK : RADAR_HIP_ERROR;
 }
