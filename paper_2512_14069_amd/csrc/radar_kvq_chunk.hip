@@ -13,7 +13,7 @@
 
 namespace radar {
 
-constexpr int kKcCols = 64;                    // columns of a block
+constexpr int kKcCols = 64;                    // columns of the widest block
 constexpr int kKcTarget = 1024;                // most workgroups that what is divided is dealt to, and most parts
 constexpr int kKcPlanned = 512;                // most sequences whose work every workgroup counts through
 constexpr int kKcArrived = 16;                 // counters are 64 bytes apart: atomics on one line wait for each other
@@ -35,7 +35,7 @@ struct KcWork {
     int B, T, N, S;
     uint32_t heads;                            // KV heads, and their queries' heads above the 16th bit
     uint32_t dealt;                            // workgroups that divided work is dealt to (0: nothing is divided), and log2 of a level's keys above the 16th bit
-    int least;                                 // least steps of a part
+    int least;                                 // least steps of a part (of four times as many nothing is divided: handing over and joining takes 6 us or so)
     uint32_t by_G;                             // 2^16 / G, rounded up
     __host__ __device__ int Hkv() const { return (int)(heads & 0xffff); }
     __host__ __device__ int G() const { return (int)(heads >> 16); }
@@ -90,13 +90,17 @@ constexpr int kKcState = 16;
 // of 16 columns counts for half a step of 64.  The quotients are by reciprocals, rounded to the safe side, as this is a chain that every workgroup goes through.
 // All lanes call; the result is the same in all of them.
 constexpr int kKcLevels = 8;
-__device__ __forceinline__ int kc_blocks(int rows, int G) { return (rows * G + kKcCols - 1) / kKcCols; }           // (rows * G < 2^28)
+template <int COLS>
+__device__ __forceinline__ int kc_blocks(int rows, int G) { return (rows * G + COLS - 1) / COLS; }                 // (rows * G < 2^28)
 // Blocks of a sequence whose first row sees `keys` keys of others or more.
-__device__ __forceinline__ int kc_beyond(const KcSeq &s, int cgs, int G, int keys) { return cgs - kc_blocks(min(max(keys - s.L, 0), s.rows), G); }
-__device__ __forceinline__ int kc_cost(const KcSeq &s, int G) {      // of a block of the sequence, in steps of 64 columns
+template <int COLS>
+__device__ __forceinline__ int kc_beyond(const KcSeq &s, int cgs, int G, int keys) { return cgs - kc_blocks<COLS>(min(max(keys - s.L, 0), s.rows), G); }
+template <int COLS>
+__device__ __forceinline__ int kc_cost(const KcSeq &s, int G) {      // of a block of the sequence, in steps
     const int steps = (s.total + 31) >> 5;
-    return s.n * G <= 16 ? steps >> 1 : steps;
+    return COLS == 64 && s.n * G <= 16 ? steps >> 1 : steps;
 }
+template <int COLS>
 __device__ __forceinline__ bool kc_find(KcItem &x, const KcWork &a, uint32_t item) {
     const int lane = lane_id(), Hkv = a.Hkv(), G = a.G();
     int p = 1, cgs, back = 0;                  // back: blocks behind this one
@@ -104,9 +108,10 @@ __device__ __forceinline__ bool kc_find(KcItem &x, const KcWork &a, uint32_t ite
     KcSeq s;
     if (a.B == 1) {                            // one sequence: nothing to count through, all of it in scalar registers
         s = kc_seq<true>(a, 0);
-        cgs = kc_blocks(s.rows, G);
+        cgs = kc_blocks<COLS>(s.rows, G);
         const uint32_t units = (uint32_t)(Hkv * cgs);
-        p = max(min(a.target() / (int)max(units, 1u), ((s.total + 31) >> 5) / a.least), 1);
+        const int cost = (s.total + 31) >> 5;
+        if (cost >= 4 * a.least) p = max(min(a.target() / (int)max(units, 1u), cost / a.least), 1);
         if (item >= units * (uint32_t)p) return false;
         x.b = 0;
         rel = item;
@@ -116,22 +121,22 @@ __device__ __forceinline__ bool kc_find(KcItem &x, const KcWork &a, uint32_t ite
         float work = 0.f;
         for (int b0 = 0; b0 < a.B; b0 += kWave) {
             const KcSeq t = b0 == 0 ? s : seq(b0);
-            if (b0 + lane < a.B) work += (float)(kc_blocks(t.rows, G) * Hkv) * (float)kc_cost(t, G);
+            if (b0 + lane < a.B) work += (float)(kc_blocks<COLS>(t.rows, G) * Hkv) * (float)kc_cost<COLS>(t, G);
         }
         // (rounded up and down by more than what the sums and the reciprocal are off)
         const float per = fmaxf(wave_sum_f32(work) * 1.001f * __builtin_amdgcn_rcpf((float)a.target()), (float)a.least), inv = 0.999f * __builtin_amdgcn_rcpf(per);
-        auto parts = [&](const KcSeq &t) { return max((int)((float)kc_cost(t, G) * inv), 1); };
+        auto parts = [&](const KcSeq &t) { return (t.total + 31) >> 5 < 4 * a.least ? 1 : max((int)((float)kc_cost<COLS>(t, G) * inv), 1); };
         // the level: the highest on or above which there are more items than this one's number
         const int bits = a.level_bits();
         int level = 0;
         uint32_t first = 0;                    // items above the level
         if (bits < 31) {                       // (64 sequences at most)
-            const int c = kc_blocks(s.rows, G);
+            const int c = kc_blocks<COLS>(s.rows, G);
             const uint32_t each = lane < a.B ? (uint32_t)(Hkv * parts(s)) : 0u;
             int most = kKcLevels;              // no items there
             while (most - level > 1) {
                 const int mid = (level + most) >> 1;
-                const uint32_t n = readlane_u32(wave_scan_u32(each * (uint32_t)kc_beyond(s, c, G, mid << bits)), kWave - 1);
+                const uint32_t n = readlane_u32(wave_scan_u32(each * (uint32_t)kc_beyond<COLS>(s, c, G, mid << bits)), kWave - 1);
                 if (n > item) level = mid;
                 else { most = mid; first = n; }
             }
@@ -139,13 +144,13 @@ __device__ __forceinline__ bool kc_find(KcItem &x, const KcWork &a, uint32_t ite
         int b0 = 0, hit = -1;
         for (; b0 < a.B; b0 += kWave) {
             if (b0 > 0) s = seq(b0);
-            cgs = kc_blocks(s.rows, G);
+            cgs = kc_blocks<COLS>(s.rows, G);
             p = parts(s);
             const bool there = b0 + lane < a.B;
             int lower = cgs, upper = 0;        // blocks on the level or above, and above
             if (bits < 31) {
-                if (level > 0) lower = kc_beyond(s, cgs, G, level << bits);
-                if (level + 1 < kKcLevels) upper = kc_beyond(s, cgs, G, (level + 1) << bits);
+                if (level > 0) lower = kc_beyond<COLS>(s, cgs, G, level << bits);
+                if (level + 1 < kKcLevels) upper = kc_beyond<COLS>(s, cgs, G, (level + 1) << bits);
             }
             const uint32_t mine = there ? (uint32_t)(Hkv * cgs) : 0u, items = there ? (uint32_t)(Hkv * (lower - upper) * p) : 0u;
             const uint32_t incl = wave_scan_u32(items);
@@ -178,22 +183,22 @@ __device__ __forceinline__ bool kc_find(KcItem &x, const KcWork &a, uint32_t ite
         s.L = (int)readlane_u32((uint32_t)s.L, hit); s.n = (int)readlane_u32((uint32_t)s.n, hit); s.rows = (int)readlane_u32((uint32_t)s.rows, hit);
         s.total = (int)readlane_u32((uint32_t)s.total, hit); s.row0 = (int)readlane_u32((uint32_t)s.row0, hit);
     } else {
-        // too many sequences to count through: blocks of columns begin at first row * G / 64 + b, which leaves every sequence room
+        // too many sequences to count through: blocks of columns begin at first row * G / COLS + b, which leaves every sequence room
         const int block = (int)kc_quotient(item, (uint32_t)Hkv);
         int off;
         if (a.row_starts) {
-            auto begin = [&](int b) { return (int64_t)min(max(a.row_starts[b], 0), a.N) * G / kKcCols + b; };
+            auto begin = [&](int b) { return (int64_t)min(max(a.row_starts[b], 0), a.N) * G / COLS + b; };
             x.b = max(last_at_most(a.B, block, begin), 0);
             off = (int)begin(x.b);
         } else {
-            const int each = kc_blocks(a.T, G);
+            const int each = kc_blocks<COLS>(a.T, G);
             x.b = block / each;
             off = x.b * each;
         }
         x.b = __builtin_amdgcn_readfirstlane(x.b);
         if (x.b >= a.B) return false;
         s = kc_seq(a, x.b);
-        cgs = kc_blocks(s.rows, G);
+        cgs = kc_blocks<COLS>(s.rows, G);
         rel = item - (uint32_t)off * (uint32_t)Hkv;
         if (block < off || block - off >= cgs) return false;
     }
@@ -202,9 +207,9 @@ __device__ __forceinline__ bool kc_find(KcItem &x, const KcWork &a, uint32_t ite
     x.cg = cgs - 1 - back - (int)nth;
     const int part = (int)(turn - nth * (uint32_t)p);
     x.n = s.n; x.rows = s.rows; x.row0 = s.row0; x.L = s.L;
-    const int c0 = x.cg * kKcCols;
+    const int c0 = x.cg * COLS;
     x.i0 = c0 / G;
-    const int i1 = min(x.i0 + kc_rows_on(c0 - x.i0 * G + kKcCols - 1, a), s.n - 1);
+    const int i1 = min(x.i0 + kc_rows_on(c0 - x.i0 * G + COLS - 1, a), s.n - 1);
     x.limit = x.i0 < s.n ? min(s.L + i1 + 1, s.total) : 0;
     const int steps = (x.limit + 31) >> 5;
     x.unit = (int)unit0 + x.cg * Hkv + x.hk;
@@ -291,8 +296,11 @@ template <int D, int NC, int KW>
 struct KcShape {
     static constexpr int NM = D / 16, CH = D / 32, COLS = 16 * NC;
     static constexpr int PASSES = NC * D > 256 ? 2 : 1, EP = 4 / PASSES, DP = D / PASSES, ROW = DP + 4;       // of the merge in LDS
+    // The merge is each wavefront's for a share of the columns (2048 rows, four wavefronts: 48.8 us, 50.8 with all of it through LDS; eight: registers spill).
+    static constexpr bool SPREAD = NC == 4 && (KW == 2 || KW == 4);
+    static constexpr bool AS_HELD = SPREAD || KW == 1;               // partial results as registers hold them: [column block][output][lane], else [column][D]
     static constexpr int room() {                                    // queries' operands, then the merge's buffer
-        const int q = COLS * D * 2, merge = KW > 1 ? KW * COLS * ROW * 4 : 0;
+        const int q = COLS * D * 2, merge = SPREAD ? NC * KW * NM / 2 * kWave * 16 : KW > 1 ? KW * COLS * ROW * 4 : 0;
         return q > merge ? q : merge;
     }
     static constexpr int PART = COLS * D + 2 * COLS;                 // floats of a partial result
@@ -331,7 +339,7 @@ __device__ __forceinline__ void kc_item(unsigned char *smem, const int *state) {
     constexpr int QS = (NC * S::CH + KW - 1) / KW;
     u32x4 y[QS];
     {
-        const int G = g.G(), r0 = p.cg * kKcCols - p.i0 * G;
+        const int G = g.G(), r0 = p.cg * 16 * MOST - p.i0 * G;
         const __bf16 *const q0 = a.q + (g.row_starts ? (size_t)p.row0 * a.q_st : (size_t)p.b * a.q_sb) + (size_t)(p.hk * G) * a.q_sh;
 #pragma unroll
         for (int j = 0; j < QS; ++j) {
@@ -388,14 +396,14 @@ __device__ __forceinline__ void kc_item(unsigned char *smem, const int *state) {
     const int G = e.G();
     const bool packed = e.row_starts != nullptr;
     p = kc_recall<KcItem>(state);
-    const int r0 = p.cg * kKcCols - p.i0 * G;
+    const int r0 = p.cg * 16 * MOST - p.i0 * G;
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));                                    // (addresses are worked out here, and not kept from the start)
     const int r2 = tid & 15, grp2 = (tid >> 4) & 3;
-    const int live = min(p.n * G - p.cg * kKcCols, S::COLS);         // columns of the block that there are
-    float *const to = a.part + (size_t)p.slot * KcShape<D, 4, KW>::PART;
-    auto hand_over = [&](int col, int d, float x0, float x1) {
-        store_shared_result(reinterpret_cast<uint64_t *>(to + col * D + d), (uint64_t)__float_as_uint(x1) << 32 | __float_as_uint(x0));
+    const int live = min(p.n * G - p.cg * 16 * MOST, S::COLS);       // columns of the block that there are
+    float *const to = a.part + (size_t)p.slot * KcShape<D, MOST, KW>::PART;
+    auto hand_over = [&](int at, float x0, float x1) {
+        store_shared_result(reinterpret_cast<uint64_t *>(to + at), (uint64_t)__float_as_uint(x1) << 32 | __float_as_uint(x0));
     };
     auto hand_over_sum = [&](int col, float M, float l) {
         store_shared_result(reinterpret_cast<uint64_t *>(to + S::COLS * D + 2 * col), (uint64_t)__float_as_uint(l) << 32 | __float_as_uint(M));
@@ -405,26 +413,34 @@ __device__ __forceinline__ void kc_item(unsigned char *smem, const int *state) {
         const float m = s_m[w * S::COLS + n * 16 + r2];
         return l == 0.f ? -kKqNone : kq_is_far(negref[n]) ? fminf(fmaxf(m * a.scale_log2, -kKqNone), kKqNone) : -negref[n];
     };
+    // a lane's outputs of its column in block n
+    auto leave = [&](int n, float M, float l) {
+        const int col = n * 16 + r2, on = kc_rows_on(r0 + col, e), i = p.i0 + on, h = p.hk * G + r0 + col - on * G;
+        if (col >= live) return;
+        if (p.parts > 1) {
+#pragma unroll
+            for (int m = 0; m < S::NM; ++m) {
+                const floatx4 x = oacc[m][n];
+                const int at = ((n * S::NM + m) * kWave + (tid & (kWave - 1))) * 4;
+                hand_over(at, x[0], x[1]);
+                hand_over(at + 2, x[2], x[3]);
+            }
+            if (grp2 == 0) hand_over_sum(col, M, l);
+            return;
+        }
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            float x[S::NM];
+#pragma unroll
+            for (int m = 0; m < S::NM; ++m) x[m] = oacc[m][n][y];
+            kc_write(a, packed, p, i, h, D / 4 * grp2 + y * S::NM, x, M, l);
+        }
+    };
     if constexpr (KW == 1) {
 #pragma unroll
         for (int n = 0; n < NC; ++n) {
-            const int col = n * 16 + r2, on = kc_rows_on(r0 + col, e), i = p.i0 + on, h = p.hk * G + r0 + col - on * G;
-            const float l = kq_column_sum(l_run[n]), M = reference(n, l);
-            if (col >= live) continue;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int d = D / 4 * grp2 + e * S::NM;
-                float x[S::NM];
-#pragma unroll
-                for (int m = 0; m < S::NM; ++m) x[m] = oacc[m][n][e];
-                if (p.parts > 1) {
-#pragma unroll
-                    for (int m = 0; m < S::NM; m += 2) hand_over(col, d + m, x[m], x[m + 1]);
-                    if (d == 0) hand_over_sum(col, M, l);
-                } else {
-                    kc_write(a, packed, p, i, h, d, x, M, l);
-                }
-            }
+            const float l = kq_column_sum(l_run[n]);
+            leave(n, reference(n, l), l);
         }
     } else {
 #pragma unroll
@@ -451,6 +467,35 @@ __device__ __forceinline__ void kc_item(unsigned char *smem, const int *state) {
         float scl[NC];
 #pragma unroll
         for (int n = 0; n < NC; ++n) scl[n] = __builtin_amdgcn_exp2f(s_m[w * S::COLS + n * 16 + r2] - s_M[n * 16 + r2]);
+        if constexpr (S::SPREAD) {
+            // Every wavefront adds up 16 of the columns, or 32.  The others' shares of them come through LDS as they lie in the registers, half the outputs at a time.
+            floatx4 *const s_x = reinterpret_cast<floatx4 *>(smem);  // [column block][wavefront][output][lane]
+            auto owner = [&](int n) { return n / (NC / KW); };
+            auto place = [&](int n, int from, int m) { return ((n * KW + from) * (S::NM / 2) + m) * kWave + (tid & (kWave - 1)); };
+            auto one_half = [&](auto which) {
+                constexpr int M0 = decltype(which)::value;
+                if (M0 > 0) __syncthreads();
+#pragma unroll
+                for (int n = 0; n < NC; ++n)
+#pragma unroll
+                    for (int m = 0; m < S::NM / 2; ++m) {
+                        oacc[M0 + m][n] *= scl[n];
+                        if (w != owner(n)) s_x[place(n, w, m)] = oacc[M0 + m][n];
+                    }
+                __syncthreads();
+#pragma unroll
+                for (int n = 0; n < NC; ++n) {
+                    if (w != owner(n)) continue;
+#pragma unroll
+                    for (int x = 1; x < KW; ++x)
+#pragma unroll
+                        for (int m = 0; m < S::NM / 2; ++m) oacc[M0 + m][n] += s_x[place(n, (w + x) & (KW - 1), m)];
+                    if constexpr (M0 > 0) leave(n, s_M[n * 16 + r2], s_L[n * 16 + r2]);
+                }
+            };
+            one_half(std::integral_constant<int, 0>{});
+            one_half(std::integral_constant<int, S::NM / 2>{});
+        } else {
         constexpr int Q4 = S::DP / 4, TPC = THREADS / S::COLS < Q4 ? THREADS / S::COLS : Q4, IPT = Q4 / TPC;      // fours of a pass; lanes of a column
 #pragma unroll
         for (int pass = 0; pass < S::PASSES; ++pass) {               // of a column: d = D/4 * part + (4 / PASSES * pass + e) * NM + m
@@ -479,8 +524,8 @@ __device__ __forceinline__ void kc_item(unsigned char *smem, const int *state) {
 #pragma unroll
                     for (int y = 1; y < KW; ++y) acc += *reinterpret_cast<const floatx4 *>(s_o + (y * S::COLS + col) * S::ROW + x);
                     if (p.parts > 1) {
-                        hand_over(col, d, acc[0], acc[1]);
-                        hand_over(col, d + 2, acc[2], acc[3]);
+                        hand_over(col * D + d, acc[0], acc[1]);
+                        hand_over(col * D + d + 2, acc[2], acc[3]);
                         if (d == 0) hand_over_sum(col, M, l);
                     } else {
                         const float o[4] = {acc[0], acc[1], acc[2], acc[3]};
@@ -488,6 +533,7 @@ __device__ __forceinline__ void kc_item(unsigned char *smem, const int *state) {
                     }
                 }
             }
+        }
         }
     }
     if (p.parts == 1) return;
@@ -497,46 +543,78 @@ __device__ __forceinline__ void kc_item(unsigned char *smem, const int *state) {
     if ((int)publish_then_ticket(counter, reinterpret_cast<unsigned int *>(s_m)) != p.parts - 1) return;
     if (threadIdx.x == 0) store_shared_result(counter, 0u);
     const int each = (((p.limit + 31) >> 5) + p.parts - 1) / p.parts;
-    const float *const from = a.part + (size_t)(p.slot - p.s0 / each) * KcShape<D, 4, KW>::PART;
-    constexpr size_t apart = KcShape<D, 4, KW>::PART;
+    const float *const from = a.part + (size_t)(p.slot - p.s0 / each) * KcShape<D, MOST, KW>::PART;
+    constexpr size_t apart = KcShape<D, MOST, KW>::PART;
     int first = threadIdx.x;
     asm volatile("" : "+v"(first));
-    for (int x = first; x < live * (D / 4); x += THREADS) {
-        const int col = x / (D / 4), d = x % (D / 4) * 4, on = kc_rows_on(r0 + col, e), i = p.i0 + on, h = p.hk * G + r0 + col - on * G;
-        float M = -kKqNone, l = 0.f;
-        floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-        constexpr int U = 4;
+    // M and l are the column's, o four outputs of it from each part, in turn
+    struct Sum { float M = -kKqNone, l = 0.f; };
+    auto join = [&](int col, auto &acc, auto place) {                // acc: fours, the x-th of them at place(x)
+        constexpr int Q = sizeof(acc) / sizeof(floatx4), U = Q == 1 ? 4 : 1;
+        Sum t;
+#pragma unroll
+        for (int x = 0; x < Q; ++x) acc[x] = floatx4{0.f, 0.f, 0.f, 0.f};
         for (int y0 = 0; y0 < p.parts; y0 += U) {
-            uint64_t ml[U], lo[U], hi[U];
+            uint64_t ml[U], lo[U][Q], hi[U][Q];
 #pragma unroll
             for (int y = 0; y < U; ++y) {
                 const float *const part = from + (size_t)min(y0 + y, p.parts - 1) * apart;
                 ml[y] = load_shared_result(reinterpret_cast<const uint64_t *>(part + S::COLS * D + 2 * col));
-                lo[y] = load_shared_result(reinterpret_cast<const uint64_t *>(part + col * D + d));
-                hi[y] = load_shared_result(reinterpret_cast<const uint64_t *>(part + col * D + d + 2));
+#pragma unroll
+                for (int x = 0; x < Q; ++x) {
+                    lo[y][x] = load_shared_result(reinterpret_cast<const uint64_t *>(part + place(x)));
+                    hi[y][x] = load_shared_result(reinterpret_cast<const uint64_t *>(part + place(x) + 2));
+                }
             }
-            float Mn = M;
+            float Mn = t.M;
 #pragma unroll
             for (int y = 0; y < U; ++y) Mn = fmaxf(Mn, __uint_as_float((uint32_t)ml[y]));
-            const float f0 = __builtin_amdgcn_exp2f(M - Mn);
-            M = Mn;
-            l *= f0;
-            acc *= f0;
+            const float f0 = __builtin_amdgcn_exp2f(t.M - Mn);
+            t.M = Mn;
+            t.l *= f0;
+#pragma unroll
+            for (int x = 0; x < Q; ++x) acc[x] *= f0;
 #pragma unroll
             for (int y = 0; y < U; ++y) {
                 if (y0 + y >= p.parts) break;                        // (the last part once more)
                 const float f = __builtin_amdgcn_exp2f(__uint_as_float((uint32_t)ml[y]) - Mn);
-                l += __uint_as_float((uint32_t)(ml[y] >> 32)) * f;
-                acc += floatx4{__uint_as_float((uint32_t)lo[y]), __uint_as_float((uint32_t)(lo[y] >> 32)), __uint_as_float((uint32_t)hi[y]),
-                               __uint_as_float((uint32_t)(hi[y] >> 32))} * f;
+                t.l += __uint_as_float((uint32_t)(ml[y] >> 32)) * f;
+#pragma unroll
+                for (int x = 0; x < Q; ++x)
+                    acc[x] += floatx4{__uint_as_float((uint32_t)lo[y][x]), __uint_as_float((uint32_t)(lo[y][x] >> 32)), __uint_as_float((uint32_t)hi[y][x]),
+                                      __uint_as_float((uint32_t)(hi[y][x] >> 32))} * f;
             }
         }
-        const float o[4] = {acc[0], acc[1], acc[2], acc[3]};
-        kc_write(a, packed, p, i, h, d, o, M, l);
+        return t;
+    };
+    if constexpr (S::AS_HELD) {
+        constexpr int Q = S::NM / 2;                                 // a lane's turn: half the outputs of its column and quarter
+        for (int x = first; x < NC * 2 * kWave; x += THREADS) {
+            const int n = x / (2 * kWave), half = x / kWave % 2, l2 = x % kWave, col = n * 16 + l2 % 16;
+            if (col >= live) continue;
+            floatx4 acc[Q];
+            const Sum t = join(col, acc, [&](int y) { return ((n * S::NM + half * Q + y) * kWave + l2) * 4; });
+            const int on = kc_rows_on(r0 + col, e), i = p.i0 + on, h = p.hk * G + r0 + col - on * G;
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+                float o[Q];
+#pragma unroll
+                for (int m = 0; m < Q; ++m) o[m] = acc[m][y];
+                kc_write(a, packed, p, i, h, D / 4 * (l2 / 16) + y * S::NM + half * Q, o, t.M, t.l);
+            }
+        }
+    } else {
+        for (int x = first; x < live * (D / 4); x += THREADS) {
+            const int col = x / (D / 4), d = x % (D / 4) * 4, on = kc_rows_on(r0 + col, e), i = p.i0 + on, h = p.hk * G + r0 + col - on * G;
+            floatx4 acc[1];
+            const Sum t = join(col, acc, [&](int) { return col * D + d; });
+            const float o[4] = {acc[0][0], acc[0][1], acc[0][2], acc[0][3]};
+            kc_write(a, packed, p, i, h, d, o, t.M, t.l);
+        }
     }
 }
 
-// MOST = 1: for calls whose sequences have 16 columns at most (single tokens), with registers for twice as many wavefronts.
+// MOST: blocks of 16, 32 or 64 columns.  With 16, for single tokens and where there are few rows, registers are left for twice as many wavefronts.
 template <int D, int MOST, int KW, bool FAR>
 __global__ __launch_bounds__(KW * kWave, MOST == 1 ? 4 : 2) void kvq_chunk_kernel(const int32_t *ctx_lens, const int32_t *row_starts, const int32_t *n_new, int B, int T, int N,
                                                                                  int S, uint32_t heads, uint32_t dealt, int least, uint32_t by_G, KcArgs) {
@@ -544,9 +622,10 @@ __global__ __launch_bounds__(KW * kWave, MOST == 1 ? 4 : 2) void kvq_chunk_kerne
     int *const state = reinterpret_cast<int *>(smem + kc_lds_bytes<D, MOST, KW>() - KW * kKcState * 4) + (KW > 1 ? wave_id() : 0) * kKcState;
     const KcWork work{ctx_lens, row_starts, n_new, B, T, N, S, heads, dealt, least, by_G};
     KcItem p;
-    if (!kc_find(p, work, blockIdx.x)) return;                       // (the same in all wavefronts)
+    constexpr int COLS = 16 * MOST;
+    if (!kc_find<COLS>(p, work, blockIdx.x)) return;                       // (the same in all wavefronts)
     kc_remember(state, p);
-    const int G = work.G(), c0 = p.cg * kKcCols, live = min(max(p.n * G - c0, 0), kKcCols), there = min(p.rows * G - c0, kKcCols);
+    const int G = work.G(), c0 = p.cg * COLS, live = min(max(p.n * G - c0, 0), COLS), there = min(p.rows * G - c0, COLS);
     if (live < there && p.s0 == 0) {                                 // rows that are not there, of sequences that are not there: zeros
         const KcArgs e = kc_args_end();
         for (int x = threadIdx.x; x < (there - live) * (D / 8); x += KW * kWave) {
@@ -556,13 +635,9 @@ __global__ __launch_bounds__(KW * kWave, MOST == 1 ? 4 : 2) void kvq_chunk_kerne
         }
     }
     if (live == 0) return;
-    if constexpr (MOST == 1) {
-        kc_item<D, 1, MOST, KW, FAR>(smem, state);
-    } else {
-        if (__builtin_amdgcn_readfirstlane(live) <= 16) kc_item<D, 1, MOST, KW, FAR>(smem, state);
-        else if (__builtin_amdgcn_readfirstlane(live) <= 32) kc_item<D, 2, MOST, KW, FAR>(smem, state);
-        else kc_item<D, 4, MOST, KW, FAR>(smem, state);
-    }
+    if (MOST == 1 || __builtin_amdgcn_readfirstlane(live) <= 16) kc_item<D, 1, MOST, KW, FAR>(smem, state);
+    else if (MOST == 2 || __builtin_amdgcn_readfirstlane(live) <= 32) kc_item<D, MOST == 1 ? 1 : 2, MOST, KW, FAR>(smem, state);
+    else kc_item<D, MOST, MOST, KW, FAR>(smem, state);
 }
 
 }  // namespace radar
@@ -582,9 +657,9 @@ static radar_status check_chunk(const radar_kvq_chunk_desc *d) {
 }
 
 // Blocks of columns of a KV head, at most: of [B,T_max], or of N rows in B sequences.
-static int64_t chunk_blocks(const radar_kvq_chunk_desc *d, bool packed) {
+static int64_t chunk_blocks(const radar_kvq_chunk_desc *d, bool packed, int cols) {
     const int64_t G = d->Hq / d->cache.Hkv;
-    return packed ? d->N * G / kKcCols + d->B : (int64_t)d->B * (((int64_t)d->T_max * G + kKcCols - 1) / kKcCols);
+    return packed ? d->N * G / cols + d->B : (int64_t)d->B * (((int64_t)d->T_max * G + cols - 1) / cols);
 }
 
 struct KcRoom { size_t off_part, bytes; };
@@ -595,33 +670,48 @@ static KcRoom chunk_room(int D) {
     return r;
 }
 
+// Columns of a block and wavefronts of a workgroup: whichever takes least by a model of rounds (a step of every wavefront), what a block costs besides and
+// what a part costs to join.  Its figures are a fit to the times of all seven kinds in 65 shapes (1 to 16384 rows in 1 to 256 sequences behind 0 to 65536, groups of 1, 4 and 8,
+// D = 64 and 128, one MI355X); what it picks took 1.4% longer than the best one in the mean, 15% at most.  us, best and worst kind: 64 rows 5.6 (16 columns, four
+// wavefronts) to 12; 64 behind 16384 29 (32, eight) to 104; 512 behind 16384 127 (64, eight) to 215; 2048 49 (64, four) to 89; 16384 1829 (64, one) to 3298.
+struct KcKind {
+    int most, kw, slots;                                   // blocks of 16 * most columns; wavefronts; workgroups that the chip holds at once
+    double alone, full, end;                               // us: a round with one wavefront a SIMD, and with as many as there is room for; what a block costs besides
+};
+constexpr KcKind kKcKinds[] = {{1, 8, 512, 0.33, 1.32, 4.7}, {1, 4, 1024, 1.08, 1.47, 3.9}, {2, 8, 256, 0.96, 0.94, 5.8},
+                               {4, 8, 256, 0.99, 1.54, 7.3}, {4, 4, 512, 1.18, 1.59, 4.9}, {4, 2, 1024, 1.26, 1.73, 5.0}, {4, 1, 2048, 1.31, 1.37, 4.5}};
 struct KcPlan {
-    int kw, target, least, level_bits;
-    bool narrow;
+    int kind, target, least, level_bits;
     int64_t items;
 };
-static KcPlan plan_chunk(const radar_kvq_chunk_desc *d, int64_t blocks) {
+static KcPlan plan_chunk(const radar_kvq_chunk_desc *d, bool packed) {
     KcPlan p;
-    const int64_t units = blocks * d->cache.Hkv, G = d->Hq / d->cache.Hkv;
-    p.narrow = (int64_t)d->T_max * G <= 16;
-    const double hi = (d->S_max + 31) / 32, lo = std::max(d->S_max - d->T_max, 0) / 32, mid = 0.5 * (hi + lo);
-    // us: a round of steps with one and with two wavefronts a SIMD; what a block costs besides
-    double best = 1e300;
-    p.kw = p.narrow && units >= 1024 ? 4 : 8;
-    for (int x = 0; x < 4 && !p.narrow; ++x) {
-        const int kw = 1 << x;
-        const double end[] = {4.0, 5.5, 7.0, 12.0}, slots = 2048.0 / kw, round = units * kw <= 1024 ? 1.27 : 1.65;
-        const double one = hi / kw * round + end[x], all = (double)units / slots * (mid / kw * round + end[x]), us = std::max(one, all);
-        if (us < best) { best = us; p.kw = kw; }
-    }
-    p.target = d->B <= kKcPlanned ? std::min(kKcTarget, (p.narrow ? 4096 : 2048) / p.kw) : 0;
+    const int64_t G = d->Hq / d->cache.Hkv;
+    const double hi = (double)(((int64_t)d->S_max + 31) / 32), lo = (double)(std::max(d->S_max - d->T_max, 0) / 32), mid = 0.5 * (hi + lo);
     // the least steps of a part: a part costs about a third of a round to join, so that the longest context is best divided by the root of its steps
     // (us, one sequence of 16384 rows, a single token, parts of 16 / 32 steps: 13.4 12.6; 2048 rows 9.2 10.9, 64 rows behind them 20.1 23.2)
-    p.least = d->rows_per_split ? d->rows_per_split / 32 : std::max(2 * p.kw, (int)(1.5 * std::sqrt(hi)));
+    auto least = [&](const KcKind &k) { return d->rows_per_split ? d->rows_per_split / 32 : std::max(2 * k.kw, (int)(1.5 * std::sqrt(hi))); };
+    double best = 1e300;
+    p.kind = 0;
+    p.items = 0;
+    for (int x = 0; x < (int)(sizeof(kKcKinds) / sizeof(kKcKinds[0])); ++x) {
+        const KcKind &k = kKcKinds[x];
+        const int64_t units = chunk_blocks(d, packed, 16 * k.most) * d->cache.Hkv;
+        if (units >= (1 << 22) || (k.most > 1 && (int64_t)d->T_max * G <= 8 * k.most)) continue;
+        const int64_t dealt = std::min(kKcTarget, k.slots) / units, long_enough = (int64_t)hi / least(k);
+        const double parts = hi < 4.0 * least(k) ? 1.0 : (double)std::max<int64_t>(std::min(dealt, long_enough), 1);
+        const double round = units * parts * k.kw <= 1024 ? k.alone : k.full, join = parts > 1 ? 0.53 + 0.4 * parts * k.most : 0.0;
+        const double one = std::ceil(hi / parts / k.kw) * round + k.end + join, all = units * parts / k.slots * (mid / parts / k.kw * round + k.end + join);
+        const double us = std::max(one, all);
+        if (us < best) { best = us; p.kind = x; p.items = units; }
+    }
+    const KcKind &k = kKcKinds[p.kind];
+    p.target = d->B <= kKcPlanned ? std::min(kKcTarget, k.slots) : 0;
+    p.least = least(k);
     p.level_bits = 31;
     if (d->B > 1 && d->B <= kWave)                         // (one sequence's blocks are in that order anyway)
         for (p.level_bits = 5; ((int64_t)d->S_max >> p.level_bits) >= kKcLevels; ++p.level_bits) {}
-    p.items = units + p.target;
+    p.items += p.target;
     return p;
 }
 
@@ -648,11 +738,15 @@ static hipError_t launch_chunk(const KcWork &w, const KcArgs &a, int64_t items, 
 }
 template <int D, bool FAR>
 static hipError_t launch_chunk(const KcWork &w, const KcArgs &a, const KcPlan &p, hipStream_t s) {
-    if (p.narrow) return p.kw == 8 ? launch_chunk<D, 1, 8, FAR>(w, a, p.items, s) : launch_chunk<D, 1, 4, FAR>(w, a, p.items, s);
-    return p.kw == 8   ? launch_chunk<D, 4, 8, FAR>(w, a, p.items, s)
-           : p.kw == 4 ? launch_chunk<D, 4, 4, FAR>(w, a, p.items, s)
-           : p.kw == 2 ? launch_chunk<D, 4, 2, FAR>(w, a, p.items, s)
-                       : launch_chunk<D, 4, 1, FAR>(w, a, p.items, s);
+    switch (p.kind) {
+        case 0: return launch_chunk<D, 1, 8, FAR>(w, a, p.items, s);
+        case 1: return launch_chunk<D, 1, 4, FAR>(w, a, p.items, s);
+        case 2: return launch_chunk<D, 2, 8, FAR>(w, a, p.items, s);
+        case 3: return launch_chunk<D, 4, 8, FAR>(w, a, p.items, s);
+        case 4: return launch_chunk<D, 4, 4, FAR>(w, a, p.items, s);
+        case 5: return launch_chunk<D, 4, 2, FAR>(w, a, p.items, s);
+        default: return launch_chunk<D, 4, 1, FAR>(w, a, p.items, s);
+    }
 }
 
 extern "C" radar_status radar_chunk_attention_kvq(const void *q, const void *cache, const int32_t *block_tables, const int32_t *ctx_lens,
@@ -662,8 +756,8 @@ extern "C" radar_status radar_chunk_attention_kvq(const void *q, const void *cac
     const radar_status st = check_chunk(d);
     if (st != RADAR_OK) return st;
     if (!row_starts && d->N != (int64_t)d->B * d->T_max) return RADAR_INVALID_ARG;
-    const int64_t blocks = chunk_blocks(d, row_starts != nullptr), Hkv = d->cache.Hkv;
-    if (blocks * Hkv >= (1 << 22)) return RADAR_UNSUPPORTED_SHAPE;
+    const int64_t Hkv = d->cache.Hkv;
+    if (chunk_blocks(d, row_starts != nullptr, kKcCols) * Hkv >= (1 << 22)) return RADAR_UNSUPPORTED_SHAPE;
     const KcRoom room = chunk_room(d->cache.D);
     if (workspace_bytes < room.bytes) return RADAR_WORKSPACE_TOO_SMALL;
     if (((uintptr_t)workspace & 255) != 0) return RADAR_INVALID_ARG;
@@ -689,7 +783,7 @@ extern "C" radar_status radar_chunk_attention_kvq(const void *q, const void *cac
     char *ws = static_cast<char *>(workspace);
     a.arrived = reinterpret_cast<unsigned int *>(ws);
     a.part = reinterpret_cast<float *>(ws + room.off_part);
-    const KcPlan p = plan_chunk(d, blocks);
+    const KcPlan p = plan_chunk(d, row_starts != nullptr);
     const KcWork w{ctx_lens, row_starts, n_new, d->B, d->T_max, (int)d->N, d->S_max, (uint32_t)Hkv | (uint32_t)(d->Hq / d->cache.Hkv) << 16,
                    (uint32_t)p.target | (uint32_t)p.level_bits << 16, p.least, (uint32_t)((65535 + d->Hq / Hkv) / (d->Hq / Hkv))};
     hipStream_t s = static_cast<hipStream_t>(stream);

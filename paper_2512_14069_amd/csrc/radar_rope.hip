@@ -18,7 +18,7 @@ namespace radar {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kRpThreads = 256, kRpRows = 8;
-constexpr int64_t kRpGroups = 1024;            // workgroups to aim for: four a CU
+constexpr int64_t kRpGroups = 512;             // workgroups to aim for (960 rows of trees: 7.4 us with 512, 8.0 with 256, 9.1 with 1024)
 
 struct RpArgs {
     const __bf16 *q, *k, *v;
@@ -122,70 +122,98 @@ __global__ __launch_bounds__(kRpThreads) void rope_kernel(RpArgs g) {
     const int64_t n0 = (int64_t)blockIdx.x * kRpRows;
     const int y = blockIdx.y, role = y < g.q_blocks ? 0 : y < g.q_blocks + g.k_blocks ? 1 : 2;
 
-    // ---- the rows: sequence, number in it, whether it is there (one wavefront), positions, slots
+    // ---- a lane's place, and its first values, which are asked for before anything is known of the rows (all N rows are memory of the tensors)
+    const int per = kRpRows * LP, heads = kRpThreads / per;          // lanes of a head's eight rows; heads a round
+    const int place = tid / per, rest = tid - place * per, row = rest / LP, p = rest - row * LP;
+    const RpPieces at = rp_pieces(g, p);
+    constexpr int V_LANES = CACHE ? kRpRows * D0 / 8 : 1, V_HEADS = kRpThreads / V_LANES;          // v: of a head's eight rows; heads a round
+    const int l = tid % V_LANES, part = l / kWave * 8, row_in = l % kWave / 8, piece_in = part + l % 8;
+    const bool is_v = CACHE && role == 2, is_q = role == 0;
+    const int H = is_q ? g.Hq : g.Hkv, rounds = is_q ? g.per_q : is_v ? g.per_v : g.per_k, step = is_v ? V_HEADS : heads;
+    const int h0 = (y - (is_q ? 0 : is_v ? g.q_blocks + g.k_blocks : g.q_blocks)) * rounds * step + (is_v ? tid / V_LANES : place);
+    const int64_t n = min(n0 + (is_v ? row_in : row), g.N - 1), in_h = is_q ? g.q_sh : g.kv_sh;
+    const __bf16 *const from = (is_q ? g.q : is_v ? g.v : g.k) + n * (is_q ? g.q_sn : g.kv_sn);
+    u32x4 a, b;
+    auto ask = [&](int h) {                                          // (past the heads: the last one once more)
+        const __bf16 *const of = from + min(h, H - 1) * in_h;
+        if (is_v) {
+            a = *reinterpret_cast<const u32x4 *>(of + piece_in * 8);
+        } else {
+            a = *reinterpret_cast<const u32x4 *>(of + at.a * 8);
+            b = *reinterpret_cast<const u32x4 *>(of + at.b * 8);
+        }
+    };
+    ask(h0);
+
+    // ---- the rows: sequence, number in it, whether it is there, positions, slots.  One wavefront finds them; what it loads is asked for as soon as an
+    // address is known, whether the row is there or not.
     if (wave_id() == 0) {
-        const int64_t n = n0 + min(lane, kRpRows - 1);
-        int b = 0, i = 0;
-        bool there = n < g.N;
+        const int64_t mine = min(n0 + min(lane, kRpRows - 1), g.N - 1);
+        int position[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+            if (g.positions && x < g.axes) position[x] = g.positions[x * g.N + mine];
+        int seq, i, ctx;
+        bool there = n0 + lane < g.N;
         if (g.row_starts) {
-            const int first = max(last_at_most(g.B, n0, [&](int x) { return (int64_t)g.row_starts[x]; }), 0);
-            // the next 64 sequences' starts tell where the seven rows behind the first one are; where so many have no row, one by one
-            const int next = g.row_starts[min(first + 1 + lane, g.B)];
-            b = first;
+            // up to 63 sequences at once, else the 63 from the first row's on; where a row lies behind them all, one by one
+            const int base = g.B < kWave ? 0 : max(last_at_most(g.B, n0, [&](int x) { return (int64_t)g.row_starts[x]; }), 0);
+            const int start = g.row_starts[min(base + lane, g.B)], context = g.ctx_lens ? g.ctx_lens[min(base + lane, g.B - 1)] : 0;
+            int hit = 0;
 #pragma unroll
             for (int r = 0; r < kRpRows; ++r) {
-                const uint64_t passed = __ballot(first + 1 + lane < g.B && (int64_t)next <= n0 + r);
-                if (r == lane) b = first + (passed == 0 ? 0 : 64 - __clzll((long long)passed));
+                const uint64_t begun = __ballot(base + lane < g.B && (int64_t)start <= n0 + r);
+                if (r == lane && begun != 0) hit = 63 - __clzll((long long)begun);
             }
-            if (lane < kRpRows)
-                while (b - first >= kWave && b + 1 < g.B && (int64_t)g.row_starts[b + 1] <= n) ++b;
-            const int64_t at = n - g.row_starts[b];
-            there = there && at >= 0 && at < g.T && n < (int64_t)g.row_starts[b + 1];
-            i = there ? (int)at : 0;
+            seq = base + hit;
+            int from = __shfl(start, hit), to = __shfl(start, min(hit + 1, kWave - 1));
+            ctx = __shfl(context, hit);
+            if (hit == kWave - 1 && lane < kRpRows) {
+                while (seq + 1 < g.B && (int64_t)g.row_starts[seq + 1] <= mine) ++seq;
+                from = g.row_starts[seq];
+                to = g.row_starts[seq + 1];
+                ctx = g.ctx_lens ? g.ctx_lens[seq] : 0;
+            }
+            there = there && mine >= from && mine < to && mine - from < g.T;
+            i = there ? (int)mine - from : 0;
         } else {
-            const uint32_t row = (uint32_t)min(n, g.N - 1);
-            b = (int)(row / (uint32_t)g.T);
-            i = (int)(row - (uint32_t)b * (uint32_t)g.T);
-            there = there && (!g.n_new || i < g.n_new[b]);
+            seq = (int)((uint32_t)mine / (uint32_t)g.T);
+            i = (int)((uint32_t)mine - (uint32_t)seq * (uint32_t)g.T);
+            ctx = g.ctx_lens ? g.ctx_lens[seq] : 0;
+            there = there && (!g.n_new || i < g.n_new[seq]);
         }
-        const int ctx = g.ctx_lens ? g.ctx_lens[b] : 0;
         there = there && ctx >= 0;
         if (lane < kRpRows) {
-            s_row[lane] = RpRow{there, CACHE && there ? g.slots[(size_t)b * g.T + i] : -1};
+            s_row[lane] = RpRow{there, CACHE ? g.slots[(size_t)seq * g.T + i] : -1};
 #pragma unroll
-            for (int a = 0; a < 4; ++a)
-                s_pos[a][lane] = (int64_t)ctx + (g.positions && there && a < g.axes ? g.positions[a * g.N + n] : i);
+            for (int x = 0; x < 4; ++x) s_pos[x][lane] = (int64_t)ctx + (g.positions ? position[x] : i);
         }
     }
     __syncthreads();
 
-    if (CACHE && role == 2) {
-        // ---- v: along the rows where they are read, down the eight rows where they are stored (they lie side by side in the cache)
-        if constexpr (CACHE) {
+    if constexpr (CACHE) {
+        if (is_v) {
+            // ---- v: along the rows where they are read, down the eight rows where they are stored (they lie side by side in the cache)
             using C = KvqChunk<D0>;
-            constexpr int LANES = kRpRows * D0 / 8, HEADS = kRpThreads / LANES;          // of a head's eight rows; heads a round
-            const int l = tid % LANES, part = l / kWave * 8, h0 = (y - g.q_blocks - g.k_blocks) * g.per_v * HEADS + tid / LANES;
-            const int row_in = l % kWave / 8, piece_in = part + l % 8, row_out = l % 8, piece_out = part + l % kWave / 8;
+            const int row_out = l % 8, piece_out = part + l % kWave / 8, turn = l % 8 * 8 + l % kWave / 8;
             const RpRow to = s_row[row_out];
             const bool stored = to.there && to.slot >= 0 && to.slot < g.total;
-            const int64_t n = min(n0 + row_in, g.N - 1);
-            const int R = 1 << g.rbits, row = stored ? to.slot & (R - 1) : 0;
-            const __bf16 *const from = g.v + n * g.kv_sn + piece_in * 8;
+            const int R = 1 << g.rbits, slot_row = stored ? to.slot & (R - 1) : 0;
             unsigned char *const block = g.cache + (size_t)(stored ? to.slot >> g.rbits : 0) * g.Hkv * C::bytes(R);
-            for (int x = 0; x < g.per_v; ++x) {
-                const int h = h0 + x * HEADS;              // (the same in the whole wavefront)
+            for (int x = 0; x < rounds; ++x) {
+                const int h = h0 + x * V_HEADS;            // (the same in the whole wavefront)
                 if (h >= g.Hkv) break;
-                const u32x4 w = *reinterpret_cast<const u32x4 *>(from + h * g.kv_sh);
-                const uint32_t w0 = w[0], w1 = w[1], w2 = w[2], w3 = w[3];
+                const uint32_t w0 = a[0], w1 = a[1], w2 = a[2], w3 = a[3];
+                if (x + 1 < rounds) ask(h + V_HEADS);
                 const KvqCodes c = kvq_encode8(w0, w1, w2, w3);
-                const uint32_t code = (uint32_t)__shfl((int)c.code, l % 8 * 8 + l % kWave / 8), mark = (uint32_t)__shfl((int)c.mark, l % 8 * 8 + l % kWave / 8);
+                const uint32_t code = (uint32_t)__shfl((int)c.code, turn), mark = (uint32_t)__shfl((int)c.mark, turn);
                 if (!stored) continue;
                 unsigned char *const chunk = block + (size_t)h * C::bytes(R);
-                *reinterpret_cast<uint32_t *>(chunk + C::v_piece(R, row, piece_out)) = code;
-                if ((piece_out & 3) == 0) chunk[C::v_scale(R, row, piece_out >> 2)] = (unsigned char)mark;
+                *reinterpret_cast<uint32_t *>(chunk + C::v_piece(R, slot_row, piece_out)) = code;
+                if ((piece_out & 3) == 0) chunk[C::v_scale(R, slot_row, piece_out >> 2)] = (unsigned char)mark;
             }
+            return;
         }
-        return;
     }
 
     // ---- sines and cosines of eight rows
@@ -197,9 +225,6 @@ __global__ __launch_bounds__(kRpThreads) void rope_kernel(RpArgs g) {
         s_cs[(row * 8 + (j & 7)) * LP + (j >> 3)] = double2{c * g.scale, s * g.scale};
     }
     __syncthreads();
-    const int per = kRpRows * LP, heads = kRpThreads / per;          // lanes of a head's eight rows; heads a round
-    const int place = tid / per, rest = tid - place * per, row = rest / LP, p = rest - row * LP;
-    const RpPieces at = rp_pieces(g, p);
     double c[8], s[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
@@ -207,45 +232,40 @@ __global__ __launch_bounds__(kRpThreads) void rope_kernel(RpArgs g) {
         c[e] = cs.x;
         s[e] = cs.y;
     }
-    const int64_t n = min(n0 + row, g.N - 1);
     const bool there = s_row[row].there != 0;
 
-    if (!CACHE || role == 0) {
+    if (!CACHE || is_q) {
         // ---- rows of q, or of k that go out as rows
-        const bool is_q = role == 0;
-        const int H = is_q ? g.Hq : g.Hkv, rounds = is_q ? g.per_q : g.per_k, h0 = (is_q ? y : y - g.q_blocks) * rounds * heads + place;
         if (!there || place >= heads) return;
-        const int64_t in_h = is_q ? g.q_sh : g.kv_sh, out_h = is_q ? g.qo_sh : g.ko_sh;
-        const __bf16 *const from = (is_q ? g.q : g.k) + n * (is_q ? g.q_sn : g.kv_sn);
+        const int64_t out_h = is_q ? g.qo_sh : g.ko_sh;
         __bf16 *const to = (is_q ? g.q_out : g.k_out) + n * (is_q ? g.qo_sn : g.ko_sn);
         for (int x = 0; x < rounds; ++x) {
             const int h = h0 + x * heads;
             if (h >= H) return;
-            u32x4 a = *reinterpret_cast<const u32x4 *>(from + h * in_h + at.a * 8), b = *reinterpret_cast<const u32x4 *>(from + h * in_h + at.b * 8);
-            if (at.turned) rp_turn(a, b, c, s, g.adjacent != 0);
-            *reinterpret_cast<u32x4 *>(to + h * out_h + at.a * 8) = a;
-            *reinterpret_cast<u32x4 *>(to + h * out_h + at.b * 8) = b;
+            u32x4 o = a, z = b;
+            if (x + 1 < rounds) ask(h + heads);
+            if (at.turned) rp_turn(o, z, c, s, g.adjacent != 0);
+            *reinterpret_cast<u32x4 *>(to + h * out_h + at.a * 8) = o;
+            *reinterpret_cast<u32x4 *>(to + h * out_h + at.b * 8) = z;
         }
     } else if constexpr (CACHE) {
         // ---- k: turned into LDS, and from there along the rows into the cache
         using C = KvqChunk<D0>;
         constexpr int PIECES = D0 / 8;
-        const int h0 = (y - g.q_blocks) * g.per_k * heads;
-        for (int x = 0; x < g.per_k; ++x) {
-            const int first = h0 + x * heads;
+        for (int x = 0; x < rounds; ++x) {
+            const int first = h0 - place + x * heads;
             if (first >= g.Hkv) return;                    // (the same for the whole workgroup)
-            const int h = min(first + place, g.Hkv - 1);
-            const __bf16 *const from = g.k + n * g.kv_sn + h * g.kv_sh;
-            u32x4 a = *reinterpret_cast<const u32x4 *>(from + at.a * 8), b = *reinterpret_cast<const u32x4 *>(from + at.b * 8);
-            if (at.turned) rp_turn(a, b, c, s, g.adjacent != 0);
+            u32x4 o = a, z = b;
+            if (x + 1 < rounds) ask(first + place + heads);
+            if (at.turned) rp_turn(o, z, c, s, g.adjacent != 0);
             if (x > 0) __syncthreads();
-            s_k[(place * kRpRows + row) * PIECES + at.a] = a;
-            s_k[(place * kRpRows + row) * PIECES + at.b] = b;
+            s_k[(place * kRpRows + row) * PIECES + at.a] = o;
+            s_k[(place * kRpRows + row) * PIECES + at.b] = z;
             __syncthreads();
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const int z = tid + u * kRpThreads, piece = z % PIECES, r2 = z / PIECES % kRpRows, h2 = first + z / (PIECES * kRpRows);
-                const u32x4 w = s_k[z];
+                const int i = tid + u * kRpThreads, piece = i % PIECES, r2 = i / PIECES % kRpRows, h2 = first + i / (PIECES * kRpRows);
+                const u32x4 w = s_k[i];
                 const uint32_t w0 = w[0], w1 = w[1], w2 = w[2], w3 = w[3];
                 const KvqCodes e = kvq_encode8(w0, w1, w2, w3);
                 const RpRow to = s_row[r2];
