@@ -712,7 +712,7 @@ radar_status radar_kvq_append_rope(const void *q, const void *k, const void *v, 
  * included).  Rows of a sequence with ctx_lens[b] < 0 are zero in out and lse, and so are rows i >= n_new[b] of [B,T_max]; rows behind the last
  * sequence of row_starts are left as they were.
  * q, out bf16 [N,Hq,D] (or [B,T_max,Hq,D]: a stride_b of its own), strides as for radar_tree_attention, stride_b ignored with row_starts; out
- * must not overlap q; lse_out f32 [N,Hq] dense or NULL; block_tables i32 [B,max_blocks]; S_max: the rows
+ * must not overlap q (the same address is refused); lse_out f32 [N,Hq] dense or NULL; block_tables i32 [B,max_blocks]; S_max: the rows
  * that the call is planned for, at most max_blocks * block_rows (the longest ctx_lens[b] + rows where it is known).
  * Limits: those of the cache; B <= 65535; N < 2^31; Hq <= 65535; the blocks of 64 of a KV head's queries, about (N * Hq / Hkv / 64 + B) * Hkv, < 2^22.
  * One kernel.  The workspace's size depends on D only, and its counters are at its head: one, initialised once, serves calls of any shape that
@@ -761,7 +761,8 @@ radar_status radar_debug_validate_tree(const int32_t *parents, const int32_t *n_
 typedef struct radar_kernel_time {
     char name[48];      /* "expand", "expand_stream", "expand_finish", "rerank", "accept",
                            "accept_length_distribution", "tree_attn_group_share",
-                           "tree_attn_merge", ... */
+                           "tree_attn_merge", "rope", "kvq_append_rope", "kvq_chunk_64x4" (blocks of 64
+                           columns, four wavefronts a workgroup), ... */
     int64_t calls;
     double total_us;
     double min_us;

@@ -186,3 +186,83 @@ def attention(q, cache, R, D, layer, tables, ctx, parents=None, n_nodes=None, S_
                     spread[b, i, h] = (w / w.sum()) @ np.abs(V[mine, g])
                     reach[b, i, h] = scale * (np.abs(K[mine, g]) @ np.abs(q[b, i, h])).max()
     return (out, lse, spread, reach) if want_sizes else (out, lse)
+
+
+# ------------------------------------------------------------------ rotary positions, chunks of new tokens
+
+def new_rows(B, T, ctx=None, row_starts=None, n_new=None, N=None):
+    """(row of the tensors, sequence, row of it) of every new row that there is: [B,T], or one sequence's behind the other's from row_starts[b] on."""
+    got = []
+    for b in range(B):
+        if ctx is not None and ctx[b] < 0:
+            continue
+        if row_starts is None:
+            got += [(b * T + i, b, i) for i in range(T if n_new is None else min(max(int(n_new[b]), 0), T))]
+        else:
+            got += [(int(row_starts[b]) + i, b, i) for i in range(min(int(row_starts[b + 1]) - int(row_starts[b]), T))]
+    return got
+
+
+def turn(x, position, inv_freq, pair_axis, interleaved=False, scale=1.0):
+    """One row x float64 [H, D] turned by its positions (whole numbers, one an axis), before any rounding; inv_freq float32 [P]."""
+    P = len(inv_freq)
+    t = np.array([float(position[a]) for a in pair_axis]) * inv_freq.astype(np.float64)
+    c, s = np.cos(t) * scale, np.sin(t) * scale
+    out = np.array(x, np.float64)
+    one, two = (slice(0, 2 * P, 2), slice(1, 2 * P, 2)) if interleaved else (slice(0, P), slice(P, 2 * P))
+    out[:, one], out[:, two] = x[:, one] * c - x[:, two] * s, x[:, one] * s + x[:, two] * c
+    return out
+
+
+def all_rows(cache, R, D, layer, table, n):
+    """Rows 0 ... n-1 of a sequence as float64 K, V [n, H, D], and which of them are there (the others: zeros)."""
+    j = np.arange(n)
+    blk = np.asarray(table)[np.minimum(j // R, len(table) - 1)]
+    there = (j // R < len(table)) & (blk >= 0) & (blk < cache.shape[1])
+    chunk = cache[layer, np.where(there, blk, 0)]                    # [n, H, bytes]
+    got = [np.zeros((n, cache.shape[2], D)) for _ in range(2)]
+    for row in range(R):
+        mine = np.nonzero(j % R == row)[0]
+        if len(mine) == 0:
+            continue
+        places, half, sc = _code_places(R, D, row)
+        for x, at, s_at in zip(got, places, sc):
+            x[mine] = decode((chunk[mine][:, :, at] >> (4 * half).astype(np.uint8)) & 15, chunk[mine][:, :, s_at])
+    for x in got:
+        x[~there] = 0.0
+    return got[0], got[1], there
+
+
+def chunk_attention(q, cache, R, D, layer, tables, ctx, T, row_starts=None, n_new=None, S_max=None, scale=0.0):
+    """q float64 [N,Hq,D] -> out float64 [N,Hq,D], lse [N,Hq], sum_j p_j |v_j| [N,Hq,D], max_j scale sum_d |q k| [N,Hq], and which rows are there.  Row i of
+    sequence b sees rows up to ctx[b] + i of its own."""
+    N, Hq, _ = q.shape
+    H = cache.shape[2]
+    scale = scale or 1.0 / np.sqrt(D)
+    S_max = tables.shape[1] * R if S_max is None else S_max
+    out, lse, spread, reach, there = np.zeros(q.shape), np.zeros((N, Hq)), np.zeros(q.shape), np.zeros((N, Hq)), np.zeros(N, bool)
+    rows = new_rows(len(ctx), T, ctx, row_starts, n_new)
+    for b in range(len(ctx)):
+        mine = np.array([(n, i) for n, bb, i in rows if bb == b], np.int64).reshape(-1, 2)
+        if len(mine) == 0:
+            continue
+        n_at, i_of = mine.T
+        there[n_at] = True
+        S = min(int(ctx[b]) + int(i_of.max()) + 1, S_max)
+        K, V, have = all_rows(cache, R, D, layer, tables[b], S)
+        sees = (np.arange(S)[None] <= int(ctx[b]) + i_of[:, None]) & have
+        for h in range(Hq):
+            k, v = K[:, h // (Hq // H)], V[:, h // (Hq // H)]
+            with np.errstate(invalid="ignore", divide="ignore"):
+                x = np.where(sees, scale * (q[n_at, h] @ k.T), -np.inf)
+                top = np.where(sees.any(1), x.max(1), 0.0)
+                w = np.where(sees, np.exp(x - top[:, None]), 0.0)
+                total = w.sum(1)
+                lse[n_at, h] = top + np.log(total)
+                w = w / np.where(total == 0, 1.0, total)[:, None]
+                bad = np.isnan(v)
+                o = w @ np.where(bad, 0.0, v)
+                out[n_at, h] = np.where((sees.astype(float) @ bad) > 0, np.nan, o)
+                spread[n_at, h] = w @ np.abs(np.where(bad, 0.0, v))
+                reach[n_at, h] = np.where(sees, scale * (np.abs(q[n_at, h]) @ np.abs(k).T), 0.0).max(1)
+    return out, lse, spread, reach, there

@@ -46,6 +46,8 @@ constexpr size_t kKcArgsAt = (sizeof(KcWork) + alignof(KcArgs) - 1) / alignof(Kc
 
 // A sequence: rows of its prefix, new rows, rows that the tensors have for it, keys that its last row sees; the first of its rows.
 struct KcSeq { int L, n, rows, total, row0; };
+// Keys that row i behind L >= 0 others sees, of `most`: the sum may pass 31 bits.
+__device__ __forceinline__ int kc_seen(int L, int i, int most) { return (int)min((uint32_t)L + (uint32_t)i + 1u, (uint32_t)most); }
 template <bool UNIFORM = false>                // the same sequence in every lane
 __device__ __forceinline__ KcSeq kc_seq(const KcWork &a, int b) {
     auto word = [](const int32_t *p, int i) { return UNIFORM ? uniform_word(p, i) : p[i]; };
@@ -60,9 +62,9 @@ __device__ __forceinline__ KcSeq kc_seq(const KcWork &a, int b) {
         s.row0 = b * a.T;
         s.n = a.n_new ? min(max(word(a.n_new, b), 0), a.T) : a.T;
     }
-    s.L = min(word(a.ctx_lens, b), a.S);       // (so that the new rows can be added in 32 bits)
+    s.L = min(word(a.ctx_lens, b), a.S);
     if (s.L < 0) s.n = 0, s.L = -1;
-    s.total = s.n > 0 ? min(s.L + s.n, a.S) : 0;
+    s.total = s.n > 0 ? kc_seen(s.L, s.n - 1, a.S) : 0;
     return s;
 }
 
@@ -210,7 +212,7 @@ __device__ __forceinline__ bool kc_find(KcItem &x, const KcWork &a, uint32_t ite
     const int c0 = x.cg * COLS;
     x.i0 = c0 / G;
     const int i1 = min(x.i0 + kc_rows_on(c0 - x.i0 * G + COLS - 1, a), s.n - 1);
-    x.limit = x.i0 < s.n ? min(s.L + i1 + 1, s.total) : 0;
+    x.limit = x.i0 < s.n ? kc_seen(s.L, i1, s.total) : 0;
     const int steps = (x.limit + 31) >> 5;
     x.unit = (int)unit0 + x.cg * Hkv + x.hk;
     x.slot = 0;
@@ -326,7 +328,7 @@ __device__ __forceinline__ void kc_item(unsigned char *smem, const int *state) {
     const KcWork g = kc_args_work();
     const int32_t *const table = (const int32_t *)(uintptr_t)kq_scalar(a.tables + (size_t)p.b * a.M);
     const kq_bytes base = (kq_bytes)(uintptr_t)kq_scalar(a.cache + (size_t)p.hk * KvqChunk<D>::bytes(1 << a.rbits));
-    const int mine = p.s0 + w, hidden = min(p.L + p.i0 + 1, p.limit);          // (keys that the first column sees)
+    const int mine = p.s0 + w, hidden = kc_seen(p.L, p.i0, p.limit);          // (keys that the first column sees)
     const bool active = mine < p.s1;
     KqK<D> k;
     KqV v;
@@ -349,7 +351,7 @@ __device__ __forceinline__ void kc_item(unsigned char *smem, const int *state) {
         }
         if (w == 0 && lane < S::COLS) {
             const int i = p.i0 + kc_rows_on(r0 + lane, g);
-            s_lim[lane] = i < p.n ? min(p.L + i + 1, p.limit) : 0;
+            s_lim[lane] = i < p.n ? kc_seen(p.L, i, p.limit) : 0;
         }
     }
     if (active) {
@@ -721,7 +723,7 @@ extern "C" size_t radar_chunk_attention_kvq_workspace_bytes(const radar_kvq_chun
 }
 
 template <int D, int MOST, int KW, bool FAR>
-static hipError_t launch_chunk(const KcWork &w, const KcArgs &a, int64_t items, hipStream_t s) {
+static hipError_t launch_chunk(const char *name, const KcWork &w, const KcArgs &a, int64_t items, hipStream_t s) {
     constexpr int bytes = kc_lds_bytes<D, MOST, KW>();
     static std::atomic<uint64_t> configured{0};            // devices on which the kernel may have so much LDS (two threads may both say so)
     int device = 0;
@@ -733,26 +735,26 @@ static hipError_t launch_chunk(const KcWork &w, const KcArgs &a, int64_t items, 
         if (e != hipSuccess) return e;
         configured.fetch_or(bit, std::memory_order_relaxed);
     }
-    return launch("kvq_chunk", kvq_chunk_kernel<D, MOST, KW, FAR>, dim3((unsigned)items), dim3(KW * kWave), bytes, s, w.ctx_lens, w.row_starts, w.n_new,
+    return launch(name, kvq_chunk_kernel<D, MOST, KW, FAR>, dim3((unsigned)items), dim3(KW * kWave), bytes, s, w.ctx_lens, w.row_starts, w.n_new,
                   w.B, w.T, w.N, w.S, w.heads, w.dealt, w.least, w.by_G, a);
 }
 template <int D, bool FAR>
 static hipError_t launch_chunk(const KcWork &w, const KcArgs &a, const KcPlan &p, hipStream_t s) {
     switch (p.kind) {
-        case 0: return launch_chunk<D, 1, 8, FAR>(w, a, p.items, s);
-        case 1: return launch_chunk<D, 1, 4, FAR>(w, a, p.items, s);
-        case 2: return launch_chunk<D, 2, 8, FAR>(w, a, p.items, s);
-        case 3: return launch_chunk<D, 4, 8, FAR>(w, a, p.items, s);
-        case 4: return launch_chunk<D, 4, 4, FAR>(w, a, p.items, s);
-        case 5: return launch_chunk<D, 4, 2, FAR>(w, a, p.items, s);
-        default: return launch_chunk<D, 4, 1, FAR>(w, a, p.items, s);
+        case 0: return launch_chunk<D, 1, 8, FAR>("kvq_chunk_16x8", w, a, p.items, s);
+        case 1: return launch_chunk<D, 1, 4, FAR>("kvq_chunk_16x4", w, a, p.items, s);
+        case 2: return launch_chunk<D, 2, 8, FAR>("kvq_chunk_32x8", w, a, p.items, s);
+        case 3: return launch_chunk<D, 4, 8, FAR>("kvq_chunk_64x8", w, a, p.items, s);
+        case 4: return launch_chunk<D, 4, 4, FAR>("kvq_chunk_64x4", w, a, p.items, s);
+        case 5: return launch_chunk<D, 4, 2, FAR>("kvq_chunk_64x2", w, a, p.items, s);
+        default: return launch_chunk<D, 4, 1, FAR>("kvq_chunk_64x1", w, a, p.items, s);
     }
 }
 
 extern "C" radar_status radar_chunk_attention_kvq(const void *q, const void *cache, const int32_t *block_tables, const int32_t *ctx_lens,
                                                   const int32_t *row_starts, const int32_t *n_new, void *out, float *lse_out,
                                                   const radar_kvq_chunk_desc *d, void *workspace, size_t workspace_bytes, void *stream) {
-    if (!q || !cache || !block_tables || !ctx_lens || !out || !workspace || (row_starts && n_new)) return RADAR_INVALID_ARG;
+    if (!q || !cache || !block_tables || !ctx_lens || !out || !workspace || out == q || (row_starts && n_new)) return RADAR_INVALID_ARG;
     const radar_status st = check_chunk(d);
     if (st != RADAR_OK) return st;
     if (!row_starts && d->N != (int64_t)d->B * d->T_max) return RADAR_INVALID_ARG;

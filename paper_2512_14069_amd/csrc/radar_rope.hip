@@ -309,6 +309,9 @@ static radar_status rope_args(const void *q, const void *k, const void *v, void 
     g->kv_sh = or_dense(d->kv_stride_h, D); g->kv_sn = or_dense(d->kv_stride_n, D * d->Hkv);
     g->qo_sh = or_dense(d->q_out_stride_h, D); g->qo_sn = or_dense(d->q_out_stride_n, D * d->Hq);
     g->ko_sh = or_dense(d->k_out_stride_h, D); g->ko_sn = or_dense(d->k_out_stride_n, D * d->Hkv);
+    // in place: the same rows
+    if (q && q == q_out && (g->q_sh != g->qo_sh || g->q_sn != g->qo_sn)) return RADAR_INVALID_ARG;
+    if (k && k == k_out && (g->kv_sh != g->ko_sh || g->kv_sn != g->ko_sn)) return RADAR_INVALID_ARG;
     const int64_t all[] = {g->q_sh, g->q_sn, g->kv_sh, g->kv_sn, g->qo_sh, g->qo_sn, g->ko_sh, g->ko_sn};
     for (int64_t s : all)
         if (s < 0 || (s & 7) != 0) return RADAR_INVALID_ARG;
