@@ -22,14 +22,16 @@
 
 namespace radar {
 
-struct KqArgs : KqCache {
+struct KqArgs {
     const __bf16 *q;
     const unsigned char *cache;
     const int32_t *tables, *parents, *ctx_lens, *n_nodes;
     __bf16 *out;
     float *lse;
-    int B, T, Hq, Hkv, G, M, S;
+    int B, T, Hq, Hkv, G, M, S, rbits, n_blocks;
     int64_t q_sb, q_st, q_sh, o_sb, o_st, o_sh;
+    float scale_log2;
+    int64_t block_bytes;                       // of a block, all heads
     int workgroups, least, shift, max_cgs;     // least share of the line; log2 steps per unit of it; column blocks of a KV head
     int unit_cost, whole;                      // what a unit costs besides its steps; whole: no line, 2^(whole - 1) workgroups for each unit
     float *part;                               // [2 * workgroups] partial results: outputs, maxima (log2 units), sums, in fp32
@@ -339,7 +341,7 @@ __global__ __launch_bounds__(kKqThreads, NC == 1 ? 4 : 2) void kvq_attn_kernel(K
             kq_step<D, NC, FAR || NC == 1 ? 2 : 4>(k, v, id, qop, [&] {
                 nnid = kq_ids(a, table, min(s + 2 * kKqWaves, last) * 32, p.total);
                 kq_load_k<D, FAR>(k, kq_base<D>(a, base, nid, next * 32), lane);
-            }, oacc, negref, l_run, [&](int col) { return kq_allowed(s_anc[col], s * 32 - p.L); }, s_m, a, s * 32, p.L, p.total);
+            }, oacc, negref, l_run, [&](int col, int first) { return kq_allowed(s_anc[col], first); }, s_m, a, s * 32, p.L, p.total);
             kq_load_v<D, FAR>(v, a, kq_base<D>(a, base, nid, next * 32), lane);
             id = nid;
             nid = nnid;

@@ -18,7 +18,10 @@ constexpr int kKcTarget = 1024;                // most workgroups that what is d
 constexpr int kKcPlanned = 512;                // most sequences whose work every workgroup counts through
 constexpr int kKcArrived = 16;                 // counters are 64 bytes apart: atomics on one line wait for each other
 
-struct KcArgs : KqCache {
+struct KcArgs {
+    int rbits, n_blocks;
+    int64_t block_bytes;                       // of a block, all heads
+    float scale_log2;
     const __bf16 *q;
     const unsigned char *cache;
     const int32_t *tables;
@@ -383,7 +386,7 @@ __device__ __forceinline__ void kc_item(unsigned char *smem, const int *state) {
         kq_step<D, NC, FAR || NC == 1 ? 2 : 4>(k, v, id, qop, [&] {
             nnid = kq_ids(a, table, min(s + 2 * KW, last) * 32, p.limit);
             kq_load_k<D, FAR>(k, kq_base<D>(a, base, nid, next * 32), lane);
-        }, oacc, negref, l_run, [&](int col) {
+        }, oacc, negref, l_run, [&](int col, int) {
             const int sees = s_lim[col] - s * 32;
             return sees >= 32 ? ~0u : sees <= 0 ? 0u : (1u << sees) - 1;
         }, s_m, a, s * 32, hidden, p.limit);

@@ -17,12 +17,8 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 constexpr float kqLog2e = 1.4426950408889634f;
 constexpr float kqLn2 = 0.6931471805599453f;
 
-// What a step has to know of the cache and the call.
-struct KqCache {
-    int rbits, n_blocks;
-    int64_t block_bytes;                       // of a block, all heads
-    float scale_log2;
-};
+// Args, below: what a step has to know of the cache and the call, in a kernel's own arguments: rbits, n_blocks, block_bytes (of a block, all heads) and
+// scale_log2.
 
 typedef const __attribute__((address_space(1))) unsigned char *kq_bytes;      // global memory
 __device__ __forceinline__ uint64_t kq_scalar(const void *p) {
@@ -57,18 +53,20 @@ struct KqV { uint32_t code[8]; u32x2 scale; };
 
 // The blocks of a step's first and second 16 keys (blocks are 16 rows or more): their numbers, the same in every lane.
 struct KqIds { int a, b; };
-__device__ __forceinline__ KqIds kq_ids(const KqCache &a, const int32_t *table, int key0, int total) {
+template <typename Args>
+__device__ __forceinline__ KqIds kq_ids(const Args &a, const int32_t *table, int key0, int total) {
     const int last = total - 1;
     return KqIds{uniform_word(table, min(key0, last) >> a.rbits), uniform_word(table, min(key0 + 16, last) >> a.rbits)};
 }
-__device__ __forceinline__ bool kq_there(const KqCache &a, int blk) { return (uint32_t)blk < (uint32_t)a.n_blocks; }
+template <typename Args>
+__device__ __forceinline__ bool kq_there(const Args &a, int blk) { return (uint32_t)blk < (uint32_t)a.n_blocks; }
 
 // Where the two halves' codes and scales begin: a row is D/2 bytes of codes further on, K's or V's, and D/32 bytes of scales.  All of it in
 // scalar registers; a lane adds the place of its own rows, worked out once.  Two blocks of a layer of less than 4 GB are at most 32 bits apart
 // (FAR: of any layer): a load then takes the lower of the two as its scalar base and an offset in one vector register.
 struct KqBase { kq_bytes code, scale; uint64_t code_up, scale_up; bool second_up; };       // the lower one, how far up the other is, which it is
-template <int D>
-__device__ __forceinline__ KqBase kq_base(const KqCache &a, kq_bytes base, KqIds id, int key0) {
+template <int D, typename Args>
+__device__ __forceinline__ KqBase kq_base(const Args &a, kq_bytes base, KqIds id, int key0) {
     const int R = 1 << a.rbits, row_a = key0 & (R - 1), row_b = (key0 + 16) & (R - 1);
     const uint32_t ia = kq_there(a, id.a) ? (uint32_t)id.a : 0u, ib = kq_there(a, id.b) ? (uint32_t)id.b : 0u;
     KqBase s;
@@ -108,8 +106,8 @@ __device__ __forceinline__ void kq_load_k(KqK<D> &k, KqBase s, int lane) {
     }
     k.scale = kq_read<u32x2, FAR>(s.scale, s.scale_up, is_up, (uint32_t)((group * C::kScales + blk) * 8));
 }
-template <int D, bool FAR>
-__device__ __forceinline__ void kq_load_v(KqV &v, const KqCache &a, KqBase s, int lane) {
+template <int D, bool FAR, typename Args>
+__device__ __forceinline__ void kq_load_v(KqV &v, const Args &a, KqBase s, int lane) {
     using C = KvqChunk<D>;
     const int r = lane & 15, grp = lane >> 4, piece = D == 128 ? r : r >> 1, blk = D == 128 ? r >> 2 : r >> 3;
     const bool is_up = (grp >= 2) == s.second_up;
@@ -162,10 +160,10 @@ __device__ __forceinline__ bool kq_is_far(float negref) { return __builtin_amdgc
 
 // One wavefront, one step: scores of 32 keys, softmax against the running reference, outputs.  The loads of the wavefront's next step are
 // asked for as soon as the registers of this one's are free: K's after the scores, V's at the end.
-// allow(column) has a bit for each of the 32 keys that the column sees; from key `hidden` on there are such that not all columns see.
-template <int D, int NC, int AHEAD, typename QOp, typename NextK, typename Allow>
+// From key `hidden` on there are keys that not all columns see; allow(column, key0 - hidden) has a bit for each of the 32 that the column sees.
+template <int D, int NC, int AHEAD, typename QOp, typename NextK, typename Allow, typename Args>
 __device__ __forceinline__ void kq_step(const KqK<D> &k, KqV &v, KqIds id, QOp qop, NextK next_k, floatx4 (&oacc)[D / 16][NC], float (&negref)[NC],
-                                        float (&l_run)[NC], Allow allow, float *s_ref, const KqCache &a, int key0, int hidden, int total) {
+                                        float (&l_run)[NC], Allow allow, float *s_ref, const Args &a, int key0, int hidden, int total) {
     constexpr int NM = D / 16, CH = D / 32, COLS = 16 * NC;          // output tiles; steps of the scores' product; columns
     const int lane = lane_id(), r = lane & 15;
     floatx4 sacc[2][NC];
@@ -229,7 +227,7 @@ __device__ __forceinline__ void kq_step(const KqK<D> &k, KqV &v, KqIds id, QOp q
         const uint32_t there = (1u << n_there) - 1;
 #pragma unroll
         for (int n = 0; n < NC; ++n) {
-            const uint32_t mine = (allow(n * 16 + r) >> (8 * grp)) & there;
+            const uint32_t mine = (allow(n * 16 + r, key0 - hidden) >> (8 * grp)) & there;
 #pragma unroll
             for (int e = 0; e < 8; ++e) sacc[e >> 2][n][e & 3] = (mine >> e) & 1u ? sacc[e >> 2][n][e & 3] : -INFINITY;
         }
@@ -329,7 +327,7 @@ __device__ __forceinline__ void kq_step(const KqK<D> &k, KqV &v, KqIds id, QOp q
         asm volatile("" : "+v"(lane2));
 #pragma unroll
         for (int n = 0; n < NC; ++n) {
-            const bool sees = (nan_keys & allow(n * 16 + (lane2 & 15))) != 0;
+            const bool sees = (nan_keys & allow(n * 16 + (lane2 & 15), key0 - hidden)) != 0;
 #pragma unroll
             for (int m = 0; m < NM; ++m) oacc[m][n] = sees ? floatx4{NAN, NAN, NAN, NAN} : oacc[m][n];
         }
