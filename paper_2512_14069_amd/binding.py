@@ -959,6 +959,10 @@ class Rope:
         if len(self.pair_axis) != P or not all(0 <= a < axes for a in self.pair_axis):
             raise ValueError(f"pair_axis: expected {P} numbers of {axes} axes")
         self.inv_freq, self.axes, self.interleaved, self.scale = inv_freq, int(axes), bool(interleaved), float(scale)
+        self._axis = bytes(self.pair_axis)
+
+    def _native(self, positions, ctx_lens, row_starts, n_new, T_max):
+        return self.inv_freq, self.axes, self._axis, int(self.interleaved), self.scale, positions, ctx_lens, row_starts, n_new, T_max or 0
 
     def desc(self):
         d = RopeDesc()
@@ -1042,6 +1046,8 @@ def radar_rope(q, k, rope, positions=None, ctx_lens=None, row_starts=None, n_new
         raise ValueError("neither q nor k")
     q_out = None if q is None else _same_rows(q_out, q, "q_out")
     k_out = None if k is None else _same_rows(k_out, k, "k_out")
+    if T_max != 0 and (native := _direct(prepared)) and native.rope(*rope._native(positions, ctx_lens, row_starts, n_new, T_max), q, k, q_out, k_out):
+        return q_out, k_out
     _here(q, k, q_out, k_out, rope.inv_freq, positions, ctx_lens, row_starts, n_new)
     d, ptrs = _rope_call(q, k, q_out, k_out, rope, positions, ctx_lens, row_starts, n_new, T_max)
     if d.N == 0:
@@ -1064,6 +1070,9 @@ def radar_kvq_append_rope(cache, q, k, v, slots, rope, positions=None, ctx_lens=
     if tuple(k.shape) != tuple(v.shape) or tuple(k.shape[-2:]) != (cache.Hkv, cache.D) or k.stride() != v.stride():
         raise ValueError(f"k, v: expected [..., {cache.Hkv}, {cache.D}] with the same strides, got {tuple(k.shape)} and {tuple(v.shape)}")
     q_out = None if q is None else _same_rows(q_out, q, "q_out")
+    if slots.shape[1] != 0 and (native := _direct(prepared)) and native.kvq_append_rope(
+            *rope._native(positions, ctx_lens, row_starts, n_new, slots.shape[1]), q, k, q_out, v, slots, cache.data, cache.block_rows, cache.D, layer):
+        return q_out
     data = _layer(cache, layer)
     _here(q, k, v, q_out, slots, data, rope.inv_freq, positions, ctx_lens, row_starts, n_new)
     d, ptrs = _rope_call(q, k, q_out, None, rope, positions, ctx_lens, row_starts, n_new, slots.shape[1])
@@ -1104,6 +1113,11 @@ def radar_chunk_attention_kvq(q, cache, block_tables, ctx_lens, row_starts=None,
     """Attention of new rows over `layer` of a KvqCache that holds them already: q bf16 [B,T,Hq,D] (n_new i32 [B] or None: so many rows are there) or
     [N,Hq,D] with row_starts i32 [B+1], at most T_max rows of a sequence (default: N); row i of sequence b sees rows up to ctx_lens[b] + i.  block_tables i32
     [B,M]; S_max: the rows in use (the longest ctx_lens + T_max), default all that the tables hold.  Returns out, like q; lse_out f32 without D."""
+    if workspace is not None and S_max != 0 and T_max != 0 and (native := _direct(prepared)):
+        done = native.chunk_attention_kvq(q, cache.data, cache.block_rows, cache.D, block_tables, ctx_lens, row_starts, n_new, T_max or 0, layer, S_max or 0, out, lse_out,
+                                          workspace, rows_per_split, softmax_scale)
+        if done is not None:
+            return done
     if q.shape[-1] != cache.D or q.stride(-1) != 1:
         raise ValueError(f"q: expected [..., Hq, {cache.D}], the innermost axis contiguous")
     B, T, N = _new_rows(q, ctx_lens, row_starts, n_new, T_max, "q")

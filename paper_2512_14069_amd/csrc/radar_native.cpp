@@ -16,6 +16,7 @@
 #include <Python.h>
 #include <cxxabi.h>
 #include <dlfcn.h>
+#include <string.h>
 
 #include <ATen/ATen.h>
 #include <c10/hip/HIPStream.h>
@@ -42,6 +43,9 @@ struct Library {
     decltype(&radar_kvq_append) kvq_append;
     decltype(&radar_kvq_commit) kvq_commit;
     decltype(&radar_tree_attention_kvq) tree_attention_kvq;
+    decltype(&radar_rope) rope;
+    decltype(&radar_kvq_append_rope) kvq_append_rope;
+    decltype(&radar_chunk_attention_kvq) chunk_attention_kvq;
 } lib;
 
 // Reads a call's arguments in order; `ok` turns false at the first one that does not fit.
@@ -482,6 +486,148 @@ PyObject *tree_attention_kvq(PyObject *, PyObject *const *args, Py_ssize_t n) {
     return fresh.defined() ? THPVariable_Wrap(std::move(fresh)) : done(rc, out_obj);
 }
 
+// A batch's new rows: [B,T,heads,D], or [N,heads,D] and where each sequence's begin.  most: of a sequence's rows, 0: not given.
+struct NewRows { int64_t B, T, N; };
+bool new_rows(const at::Tensor *x, const at::Tensor *ctx, const at::Tensor *starts, const at::Tensor *fresh, int32_t most, NewRows *rows) {
+    if (starts) {
+        if (x->dim() != 3 || starts->dim() != 1 || starts->numel() < 2 || fresh) return false;
+        *rows = NewRows{starts->numel() - 1, most > 0 ? most : x->size(0), x->size(0)};
+    } else {
+        if (x->dim() != 4 || (most > 0 && x->size(1) != most)) return false;
+        *rows = NewRows{x->size(0), x->size(1), x->size(0) * x->size(1)};
+    }
+    return rows->N > 0 && rows->B <= INT32_MAX && rows->T <= INT32_MAX && sized(ctx, {rows->B}) && sized(fresh, {rows->B});
+}
+// Strides of the rows and heads of [...,H,D]: the leading dimensions as one evenly spaced axis.
+bool row_strides(const at::Tensor *x, int64_t *row, int64_t *head) {
+    const int64_t dims = x->dim();
+    if (dims < 3 || x->stride(dims - 1) != 1 || x->size(dims - 2) > INT32_MAX || x->size(dims - 1) > INT32_MAX) return false;
+    int64_t first = 0, step = 0;
+    for (int64_t i = dims - 3; i >= 0; --i) {
+        if (x->size(i) == 1) continue;
+        if (x->stride(i) == 0 || (step != 0 && x->stride(i) != step)) return false;
+        if (step == 0) first = x->stride(i);
+        step = x->stride(i) * x->size(i);
+    }
+    *row = first;
+    *head = x->size(dims - 2) > 1 ? x->stride(dims - 2) : 0;
+    return x->size(dims - 2) == 1 || *head != 0;
+}
+
+// inv_freq, axes, pair_axis (bytes), interleaved, scale, positions, ctx_lens, row_starts, n_new, T_max (0: not given), q, k, q_out, k_out: what turns and
+// appends share
+struct RopeCall {
+    const at::Tensor *inv, *positions, *ctx, *starts, *fresh, *q, *k, *q_out, *k_out;
+    radar_rope_desc d{};
+    bool read(Reader &r, bool cache) {
+        inv = r.f32();
+        d.axes = r.integer();
+        PyObject *axis = r.peek();
+        r.skip();
+        d.interleaved = r.integer();
+        d.scale = r.real();
+        positions = r.i32(true); ctx = r.i32(true); starts = r.i32(true); fresh = r.i32(true);
+        const int32_t most = r.integer();
+        q = r.tensor(at::kBFloat16, false, true); k = r.tensor(at::kBFloat16, false, !cache);
+        q_out = r.tensor(at::kBFloat16, false, true);
+        k_out = cache ? nullptr : r.tensor(at::kBFloat16, false, true);
+        const at::Tensor *x = q ? q : k;
+        NewRows rows;
+        if (!r.ok || !x || (q != nullptr) != (q_out != nullptr) || (!cache && (k != nullptr) != (k_out != nullptr)) || !PyBytes_Check(axis)) return false;
+        const int64_t P = inv->numel();
+        if (inv->dim() != 1 || P < 1 || P > 128 || PyBytes_GET_SIZE(axis) != P || !new_rows(x, ctx, starts, fresh, most, &rows)) return false;
+        memcpy(d.pair_axis, PyBytes_AS_STRING(axis), (size_t)P);
+        if (q && k) {                                                // the same rows
+            if (q->dim() != k->dim() || q->size(q->dim() - 1) != k->size(k->dim() - 1)) return false;
+            for (int64_t i = 0; i < q->dim() - 2; ++i)
+                if (q->size(i) != k->size(i)) return false;
+        }
+        if ((q && q_out->sizes() != q->sizes()) || (k_out && k_out->sizes() != k->sizes())) return false;
+        if (positions) {                                             // [axes,N], [axes] and the rows' own dimensions, [N] of one axis
+            const int64_t dims = positions->dim();
+            if (positions->numel() != d.axes * rows.N || dims < 1 || (dims == 1 ? d.axes != 1 : positions->size(0) != d.axes) || dims > (starts ? 2 : 3) ||
+                (dims == 3 && positions->size(1) != rows.B)) return false;
+        }
+        if ((q && (!row_strides(q, &d.q_stride_n, &d.q_stride_h) || !row_strides(q_out, &d.q_out_stride_n, &d.q_out_stride_h))) ||
+            (k && !row_strides(k, &d.kv_stride_n, &d.kv_stride_h)) || (k_out && !row_strides(k_out, &d.k_out_stride_n, &d.k_out_stride_h))) return false;
+        d.B = (int32_t)rows.B; d.T_max = (int32_t)rows.T; d.N = rows.N;
+        d.Hq = q ? (int32_t)q->size(q->dim() - 2) : 0; d.Hkv = k ? (int32_t)k->size(k->dim() - 2) : 0; d.D = (int32_t)x->size(x->dim() - 1);
+        d.rotary_dim = (int32_t)(2 * P);
+        return true;
+    }
+    static void *at(const at::Tensor *t) { return t ? t->data_ptr() : nullptr; }
+};
+
+// what RopeCall reads
+PyObject *rope(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    Reader r(args, n);
+    RopeCall c;
+    if (!c.read(r, false) || !here({c.inv, c.positions, c.ctx, c.starts, c.fresh, c.q, c.k, c.q_out, c.k_out})) Py_RETURN_NONE;
+    auto p = [](const at::Tensor *t) { return Reader::pointer<int32_t>(t); };
+    return done(call(lib.rope, c.at(c.q), c.at(c.k), c.at(c.q_out), c.at(c.k_out), Reader::pointer<float>(c.inv), p(c.positions), p(c.ctx), p(c.starts), p(c.fresh),
+                     &c.d, stream()));
+}
+
+// what RopeCall reads but for k_out, v, slots, cache, layer
+PyObject *kvq_append_rope(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    Reader r(args, n);
+    RopeCall c;
+    radar_kvq_desc d{};
+    if (!c.read(r, true)) Py_RETURN_NONE;
+    const at::Tensor *v = r.tensor(at::kBFloat16, false), *slots = r.i32(), *data = read_cache(r, &d);
+    const int32_t layer = r.integer();
+    if (!r.ok || layer < 0 || layer >= d.layers || v->sizes() != c.k->sizes() || v->strides() != c.k->strides() || !sized(slots, {c.d.B, c.d.T_max}) ||
+        c.d.Hkv != d.Hkv || c.d.D != d.D || !here({c.inv, c.positions, c.ctx, c.starts, c.fresh, c.q, c.k, c.q_out, v, slots, data})) Py_RETURN_NONE;
+    auto p = [](const at::Tensor *t) { return Reader::pointer<int32_t>(t); };
+    return done(call(lib.kvq_append_rope, c.at(c.q), c.at(c.k), v->data_ptr(), c.at(c.q_out), Reader::pointer<float>(c.inv), p(c.positions), p(c.ctx), p(c.starts),
+                     p(c.fresh), p(slots), (void *)layer_of(data, layer), &c.d, &d, stream()));
+}
+
+// q, cache, block_tables, ctx_lens, row_starts, n_new, T_max (0: not given), layer, S_max (0: all that the tables hold), out (None: allocated here), lse_out, workspace,
+// rows_per_split, softmax_scale -> out
+PyObject *chunk_attention_kvq(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    Reader r(args, n);
+    const at::Tensor *q = r.tensor(at::kBFloat16, false);
+    radar_kvq_chunk_desc d{};
+    const at::Tensor *data = read_cache(r, &d.cache), *tables = r.i32(), *ctx = r.i32(), *starts = r.i32(true), *fresh = r.i32(true);
+    const int32_t most = r.integer(), layer = r.integer();
+    d.S_max = r.integer();
+    PyObject *out_obj = r.peek();
+    const at::Tensor *out = r.tensor(at::kBFloat16, false, true);
+    const at::Tensor *lse = r.f32(true);
+    void *ws; size_t ws_bytes;
+    const at::Tensor *room = nullptr;
+    if (PyObject *o = r.peek(); o != nullptr && THPVariable_Check(o)) room = &THPVariable_Unpack(o);
+    r.workspace(&ws, &ws_bytes);
+    d.rows_per_split = r.integer();
+    d.softmax_scale = r.real();
+    NewRows rows;
+    if (!r.ok || layer < 0 || layer >= d.cache.layers || tables->dim() != 2 || !new_rows(q, ctx, starts, fresh, most, &rows)) Py_RETURN_NONE;
+    const int64_t last = q->dim() - 1, M = tables->size(1);
+    if (tables->size(0) != rows.B || M > INT32_MAX || q->size(last) != d.cache.D || q->stride(last) != 1 || q->size(last - 1) > INT32_MAX ||
+        (lse && lse->sizes() != q->sizes().slice(0, last)) || (out && (out->sizes() != q->sizes() || out->stride(last) != 1)) ||
+        !here({q, data, tables, ctx, starts, fresh, out, lse, room})) Py_RETURN_NONE;
+    if (d.S_max == 0) {
+        if (M * d.cache.block_rows > INT32_MAX) Py_RETURN_NONE;
+        d.S_max = (int32_t)(M * d.cache.block_rows);
+    }
+    d.B = (int32_t)rows.B; d.T_max = (int32_t)rows.T; d.N = rows.N; d.Hq = (int32_t)q->size(last - 1); d.max_blocks = (int32_t)M;
+    at::Tensor made;
+    if (out == nullptr) { made = at::empty(q->sizes(), q->options().memory_format(c10::nullopt)); out = &made; }
+    int64_t *const qs[] = {&d.q_stride_b, &d.q_stride_t, &d.q_stride_h}, *const os[] = {&d.out_stride_b, &d.out_stride_t, &d.out_stride_h};
+    const int64_t lead = 3 - last;                                   // (rows one behind the other have no first axis)
+    for (int64_t i = 0; i < last; ++i) {
+        if (q->size(i) == 1) continue;
+        if (q->stride(i) == 0 || out->stride(i) == 0) Py_RETURN_NONE;
+        *qs[lead + i] = q->stride(i); *os[lead + i] = out->stride(i);
+    }
+    auto p = [](const at::Tensor *t) { return Reader::pointer<int32_t>(t); };
+    const radar_status rc = call(lib.chunk_attention_kvq, q->data_ptr(), layer_of(data, layer), p(tables), p(ctx), p(starts), p(fresh), out->data_ptr(),
+                                 Reader::pointer<float>(lse), &d, ws, ws_bytes, stream());
+    if (rc != RADAR_OK) Py_RETURN_NONE;
+    return made.defined() ? THPVariable_Wrap(std::move(made)) : done(rc, out_obj);
+}
+
 // the library's path: looks its entry points up (it is the copy that ctypes has loaded already)
 PyObject *bind(PyObject *, PyObject *path) {
     const char *p = PyUnicode_AsUTF8(path);
@@ -509,6 +655,9 @@ PyObject *bind(PyObject *, PyObject *path) {
     find(lib.kvq_append, "radar_kvq_append");
     find(lib.kvq_commit, "radar_kvq_commit");
     find(lib.tree_attention_kvq, "radar_tree_attention_kvq");
+    find(lib.rope, "radar_rope");
+    find(lib.kvq_append_rope, "radar_kvq_append_rope");
+    find(lib.chunk_attention_kvq, "radar_chunk_attention_kvq");
     if (!all) { PyErr_Format(PyExc_RuntimeError, "%s lacks an entry point", p); return nullptr; }
     Py_RETURN_NONE;
 }
@@ -517,6 +666,7 @@ PyObject *bind(PyObject *, PyObject *path) {
 PyMethodDef methods[] = {
     FAST(tree_attention), FAST(draft_expand), FAST(draft_rerank), FAST(verify_accept), FAST(verify_accept_q),
     FAST(accept_length_distribution), FAST(policy_step), FAST(kvq_blocks), FAST(kvq_append), FAST(kvq_commit), FAST(tree_attention_kvq),
+    FAST(rope), FAST(kvq_append_rope), FAST(chunk_attention_kvq),
     {"bind", bind, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "argument marshalling of the hot calls", -1, methods, nullptr, nullptr, nullptr, nullptr};

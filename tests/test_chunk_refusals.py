@@ -161,6 +161,66 @@ def test_the_binding_raises():
     assert b.radar_chunk_attention_kvq(empty, cache, i32(2, 4), i32(2), row_starts=i32(3), prepared=True)().shape == empty.shape
 
 
+def test_the_native_half_returns_none(lib):  # noqa: F811
+    """Whatever it cannot take: tensors that are not on a GPU, other objects, too few of them, sizes that are none."""
+    from paper_2512_14069_amd import binding as b
+    n, i32 = b._native, torch.zeros((2, 2), dtype=torch.int32)
+    x, cache, rope = torch.zeros((1, 3, 2, 128), dtype=torch.bfloat16), torch.zeros((1, 4, 2, 16 * 136), dtype=torch.uint8), b.Rope(torch.ones(64))
+    turn = list(rope._native(None, None, None, None, 0))
+    calls = ((n.rope, turn + [x, x, x, x]), (n.kvq_append_rope, turn + [x, x, x, x, i32, cache, 16, 128, 0]),
+             (n.chunk_attention_kvq, [x, cache, 16, 128, i32, i32, None, None, 0, 0, 0, None, None, i32, 0, 0.0]))
+    for f, args in calls:
+        assert f(*args) is None and f() is None
+        for i in range(len(args)):
+            assert f(*args[:i]) is None
+            for other in (None, "no", b"", 1 << 70, -1, object(), x, i32):
+                assert f(*args[:i], other, *args[i + 1:]) is None
+
+
+FAKE = r"""
+import sys
+import warnings
+
+import torch
+from torch._subclasses.fake_tensor import FakeTensorMode
+
+from paper_2512_14069_amd import binding as b
+
+warnings.simplefilter("ignore")
+b.load()
+n = b._native
+with FakeTensorMode():                      # tensors that say they are on a GPU; there is none to allocate on or take a stream from
+    i = lambda *shape: torch.empty(shape, dtype=torch.int32, device="cuda")
+    h = lambda *shape: torch.empty(shape, dtype=torch.bfloat16, device="cuda")
+    inv, cache = torch.empty(32, device="cuda"), torch.empty((1, 4, 2, 16 * 68), dtype=torch.uint8, device="cuda")
+    turn = (inv, 2, bytes(32), 0, 1.0, i(2, 6), i(2), None, None, 0)
+    packed = (inv, 1, bytes(32), 1, 0.5, i(6), i(2), i(3), None, 4)
+    q, k, ends = h(2, 3, 4, 64), h(2, 3, 2, 64), (i(2, 3), cache, 16, 64, 0)
+    calls = [(n.rope, turn + (q, k, h(2, 3, 4, 64), h(2, 3, 2, 64))), (n.rope, turn + (q, None, q, None)), (n.rope, packed + (h(6, 4, 64), h(6, 2, 64)) * 2),
+             (n.kvq_append_rope, turn + (q, k, h(2, 3, 4, 64), k) + ends), (n.kvq_append_rope, turn + (None, k, None, k) + ends),
+             (n.chunk_attention_kvq, (q, cache, 16, 64, i(2, 4), i(2), None, i(2), 0, 0, 0, None, None, None, 0, 0.0)),
+             (n.chunk_attention_kvq, (h(6, 4, 64), cache, 16, 64, i(2, 4), i(2), i(3), None, 4, 0, 9, h(6, 4, 64), None, None, 0, 0.0))]
+sparse = torch.sparse_coo_tensor(torch.zeros((1, 1), dtype=torch.long), torch.ones(1), (4,))
+for f, args in calls:
+    print(f.__name__, flush=True)
+    assert f(*args) is None
+    for at in range(len(args)):
+        for other in (None, "text", torch.zeros(1), torch.zeros(2, dtype=torch.int8), sparse, 1 << 40, b"12"):
+            assert f(*args[:at], other, *args[at + 1:]) is None
+print("done")
+"""
+
+
+def test_nothing_leaves_the_native_half_but_none(lib):  # noqa: F811
+    """In a process of its own: a C++ exception of torch's that escaped would end it."""
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-W", "ignore", "-c", FAKE], cwd=root, env=dict(os.environ, HIP_VISIBLE_DEVICES="-1", PYTHONPATH=root), capture_output=True, text=True,
+                       timeout=300)
+    assert r.returncode == 0 and r.stdout.rstrip().endswith("done"), (r.returncode, r.stdout[-500:], r.stderr[-2000:])
+
+
 def test_under_sanitizers():
     if os.environ.get("RADAR_LIB_SANITIZE") == "1":
         pytest.skip("this is the sanitized run")

@@ -461,3 +461,62 @@ def test_two_streams_with_workspaces_of_their_own():
     for n, (_, _, _, a, st) in enumerate(work):
         check(*a, outs[n][0], row_starts=st)
         assert all(torch.equal(o, outs[n][0]) for o in outs[n][1:])
+
+
+def test_direct_calls_by_the_native_half(monkeypatch):
+    """Direct calls are marshalled natively (attention: with a workspace); they do what ctypes makes them do, and what the native half does not take reaches the
+    other's checks."""
+    from test_gpu_support import _Both
+    b, rng, D, R, Hq, H, T = binding(), seed(930), 64, 16, 8, 2, 6
+    both = _Both(b, monkeypatch)
+    ctx, new = np.array([77, 31, -1], np.int32), [6, 3, 4]
+    tables, cache, _, _, starts, _ = make(rng, ctx, new, Hq, H, D, R, layers=2)
+    wide = torch.randn((3, T, Hq + 2 * H, D), device="cuda").bfloat16()
+    flat = torch.randn((sum(new), Hq + 2 * H, D), device="cuda").bfloat16()
+    dc, dt, dn, ds = dev(ctx), dev(tables), dev(np.array(new, np.int32)), dev(starts)
+    slots = dev(rng.permutation(cache.shape[1] * R)[:3 * T].reshape(3, T).astype(np.int32))
+    ropes = (b.Rope(dev(frequencies(32))), b.Rope(dev(frequencies(8)), axes=3, pair_axis=[2, 1, 0, 0, 1, 2, 1, 0], interleaved=True, scale=1.25))
+    pos = dev(rng.integers(0, 99, (3, 3 * T)).astype(np.int32))
+    ws = None
+    for x, rows in ((wide, dict(n_new=dn)), (wide, dict()), (flat, dict(row_starts=ds, T_max=T)), (flat, dict(row_starts=ds))):
+        q, k, v = x[..., :Hq, :], x[..., Hq:Hq + H, :], x[..., Hq + H:, :]
+        N = q.numel() // (Hq * D)
+        for rope, positions in ((ropes[0], None), (ropes[0], pos[0, :N].contiguous()), (ropes[0], pos[:1, :N].contiguous()), (ropes[1], pos[:, :N].contiguous()),
+                                (ropes[1], pos[:, :N].contiguous().view((3,) + tuple(q.shape[:-2])))):
+            def turn():
+                out = torch.full(q.shape, 3.0, dtype=torch.bfloat16, device="cuda")
+                got = b.radar_rope(q, k, rope, positions=positions, ctx_lens=dc, q_out=out, k_out=torch.zeros(k.shape, dtype=torch.bfloat16, device="cuda"), **rows)
+                assert got[0] is out
+                return [got[0], got[1]]
+            both("rope", turn)
+
+            def append():
+                c, out = gpu_cache(cache, R, D), torch.full(q.shape, 3.0, dtype=torch.bfloat16, device="cuda")
+                kw = {n: t for n, t in rows.items() if n != "T_max"}
+                assert b.radar_kvq_append_rope(c, q, k, v, slots, rope, positions=positions, ctx_lens=dc, layer=1, q_out=out, **kw) is out
+                return [c.data.clone(), out]
+            both("append", append)
+        c = gpu_cache(cache, R, D)
+        ws = b.new_workspace(b.radar_chunk_attention_kvq_workspace_bytes(b.kvq_chunk_desc(q, c, tables.shape[1], 3, T, N))) if ws is None else ws
+        room = torch.zeros((Hq,) + tuple(q.shape[:-2]) + (D,), dtype=torch.bfloat16, device="cuda").movedim(0, -2)
+        for out, S, split, scale in ((None, None, 0, 0.0), (room, 60, 64, 0.2)):
+            def attention():
+                lse = torch.full(q.shape[:-1], 7.0, device="cuda")
+                room.zero_()
+                got = b.radar_chunk_attention_kvq(q, c, dt, dc, layer=1, S_max=S, out=out, lse_out=lse, workspace=ws, rows_per_split=split, softmax_scale=scale, **rows)
+                assert out is None or got is out
+                return [got.clone(), lse]
+            both("attention", attention)
+    both.native = True
+    q, k = wide[:, :, :Hq], wide[:, :, Hq:Hq + H]
+    for bad in (lambda: b.radar_rope(q.float(), None, ropes[0]), lambda: b.radar_rope(q, k[:, :2], ropes[0]), lambda: b.radar_rope(q, k, ropes[1], positions=pos.t().contiguous()),
+                lambda: b.radar_kvq_append_rope(c, q, k, k.contiguous(), slots, ropes[0]), lambda: b.radar_kvq_append_rope(c, q, k, k, slots[:2], ropes[0]),
+                lambda: b.radar_chunk_attention_kvq(q, c, dt[:2], dc, workspace=ws), lambda: b.radar_chunk_attention_kvq(q, c, dt, dc, n_new=dn[:1], workspace=ws),
+                lambda: b.radar_chunk_attention_kvq(q[:1].expand(3, T, Hq, D), c, dt, dc, workspace=ws), lambda: b.radar_chunk_attention_kvq(flat[:, :Hq], c, dt, dc, workspace=ws)):
+        with pytest.raises(ValueError):
+            bad()
+    own = q.contiguous()
+    for bad in (lambda: b.radar_chunk_attention_kvq(own, c, dt, dc, out=own, workspace=ws), lambda: b.radar_chunk_attention_kvq(q, c, dt, dc, S_max=tables.shape[1] * R + 1, workspace=ws),
+                lambda: b.radar_chunk_attention_kvq(q, c, dt, dc, workspace=ws[:4096]), lambda: b.radar_rope(q, None, ropes[0], q_out=wide.flatten()[:q.numel()].view(q.shape))):
+        with pytest.raises(b.RadarError):
+            bad()
