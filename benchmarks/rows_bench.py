@@ -1,6 +1,6 @@
 """Times the entry points that widen the hot path, at the 8B shape (V = 128256, k = 10, 61 tree rows):
 acceptance-length distribution, prediction-model step (alone and fused into the expansion), the
-expansion of 4, 16 and 64 sequences in one launch, verification with draft distributions, and the paged 4-bit cache.  One JSON line per entry point with the per-kernel device
+expansion of 4, 16 and 64 sequences in one launch, verification with draft distributions, the paged 4-bit cache, and prompts and tokens over it.  One JSON line per entry point with the per-kernel device
 durations the library records (radar_profile_begin / radar_profile_end) and the algorithmic bytes.
 
     python -m benchmarks.rows_bench [--reps 100]
@@ -155,6 +155,33 @@ def main():
             timed("radar_kvq_blocks + append + commit " + what, [room, write, move], B * Tq * (4 * H * D + row) + B * 6 * 2 * row,
                   "a verification pass's other calls; bytes: the trees' rows in and the paths' rows")
         del cache
+        torch.cuda.empty_cache()
+
+    # serving steps over it: rows turned by their positions and written, and attention of the new rows (prompts, pieces of them, single tokens)
+    rope = b.Rope((10000.0 ** (-torch.arange(D // 2, dtype=torch.float64) / (D // 2))).float().to(dev))
+    for what, ctxs, news in (("a tree of 60 rows behind 2048", [2048], [60]), ("a prompt of 2048 rows", [0], [2048]), ("a prompt of 16384 rows", [0], [16384]),
+                             ("512 rows behind 16384", [16384], [512]), ("64 tokens behind 2048 to 8192", rng.integers(2048, 8193, 64), [1] * 64),
+                             ("48 tokens and two pieces of 400 rows behind 512 to 8192", rng.integers(512, 8193, 50), [1] * 48 + [400] * 2)):
+        L, n = np.asarray(ctxs, np.int64), np.asarray(news, np.int64)
+        B, rows, most = len(L), int(n.sum()), int(n.max())
+        per, n_blocks = -(-int((L + n).max()) // R), int(sum(-(-int(x) // R) for x in L + n))
+        cache, tables = b.KvqCache(n_blocks, R, H, D), b.KvqTables(B, per, n_blocks, R)
+        cache.data.random_(0, 256, generator=gen)
+        cache.data[..., R * D:].fill_(126)
+        ctx, new, starts = to(L.astype(np.int32)), to(n.astype(np.int32)), to(np.concatenate([[0], np.cumsum(n)]).astype(np.int32))
+        x = torch.randn((rows, Hq + 2 * H, D), generator=gen, device=dev).to(torch.bfloat16)
+        q, kk, vv = x[:, :Hq], x[:, Hq:Hq + H], x[:, Hq + H:]
+        slots, _ = b.radar_kvq_blocks(ctx, tables, most, n_new=new)
+        row, span = H * (D + D // 16), dict(ctx_lens=ctx, row_starts=starts)
+        turn = b.radar_rope(q, kk, rope, T_max=most, prepared=True, **span)
+        timed("radar_rope " + what, [turn], rows * (Hq + H) * D * 4, "q and k, in and out")
+        write = b.radar_kvq_append_rope(cache, q, kk, vv, slots, rope, prepared=True, **span)
+        timed("radar_kvq_append_rope " + what, [write], rows * (Hq * D * 4 + 4 * H * D + row), "q in and out, k and v in, the cache's rows out")
+        attend = b.radar_chunk_attention_kvq(write.out, cache, tables.block_tables, T_max=most, S_max=int((L + n).max()), prepared=True, **span)
+        flop = 4 * Hq * D * float((n * L + n * (n + 1) / 2).sum())
+        timed("radar_chunk_attention_kvq " + what, [attend], int((L + n).sum()) * row + rows * Hq * D * 4,
+              "bytes: the sequences' rows once, queries and outputs; %.3g Gflop" % (flop / 1e9))
+        del cache, x
         torch.cuda.empty_cache()
 
 
