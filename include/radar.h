@@ -697,7 +697,8 @@ radar_status radar_rope(const void *q, const void *k, void *q_out, void *k_out, 
 
 /* radar_rope of q and k, and k and v into one layer's cache, as radar_rope followed by radar_kvq_append would, bit for bit:
  * row i of sequence b goes to slots[b,i] (i32 [B,T_max], as radar_kvq_blocks writes them, also where the rows are one behind the other); a
- * row whose slot is out of range, or that is not there, is not written; q is turned all the same.  v bf16 [N,Hkv,D] with k's strides;
+ * row whose slot is out of range, or that is not there, is not written (of two rows with the same slot either may leave any of its parts there); q is
+ * turned all the same, where its row is there.  v bf16 [N,Hkv,D] with k's strides;
  * q and q_out may both be NULL; k_out's strides are ignored.  cache: the layer's first block.  desc->D and desc->Hkv are the cache's.
  * Limits: those of both calls.  No workspace; one kernel. */
 radar_status radar_kvq_append_rope(const void *q, const void *k, const void *v, void *q_out, const float *inv_freq, const int32_t *positions,
@@ -710,13 +711,14 @@ radar_status radar_kvq_append_rope(const void *q, const void *k, const void *v, 
  *     out[n,h,:] = softmax_j( scale * <q[n,h,:], k[j,h/G,:]> ) . v[j,h/G,:]          lse[n,h] = log sum_j exp(...)
  * Where no row is there to be seen, out is zero and lse -inf.  A row that is not seen has no influence, whatever it holds (NaN blocks
  * included).  Rows of a sequence with ctx_lens[b] < 0 are zero in out and lse, and so are rows i >= n_new[b] of [B,T_max]; rows behind the last
- * sequence of row_starts are left as they were.
+ * sequence of row_starts, and of a sequence behind its T_max-th, are left as they were.
  * q, out bf16 [N,Hq,D] (or [B,T_max,Hq,D]: a stride_b of its own), strides as for radar_tree_attention, stride_b ignored with row_starts; out
  * must not overlap q (the same address is refused); lse_out f32 [N,Hq] dense or NULL; block_tables i32 [B,max_blocks]; S_max: the rows
  * that the call is planned for, at most max_blocks * block_rows (the longest ctx_lens[b] + rows where it is known).
  * Limits: those of the cache; B <= 65535; N < 2^31; Hq <= 65535; the blocks of 64 of a KV head's queries, about (N * Hq / Hkv / 64 + B) * Hkv, < 2^22.
  * One kernel.  The workspace's size depends on D only, and its counters are at its head: one, initialised once, serves calls of any shape that
- * follow each other on one stream. */
+ * follow each other on one stream.  (row_starts that fall are not a batch: nothing outside the tensors is read or written, but the rows'
+ * results are undefined, and the workspace has to be initialised again.) */
 typedef struct radar_kvq_chunk_desc {
     radar_kvq_desc cache;    /* layers and layer_stride are ignored */
     int32_t B, T_max, Hq, max_blocks, S_max;

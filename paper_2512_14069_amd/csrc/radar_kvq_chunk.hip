@@ -702,7 +702,7 @@ static KcPlan plan_chunk(const radar_kvq_chunk_desc *d, bool packed) {
     for (int x = 0; x < (int)(sizeof(kKcKinds) / sizeof(kKcKinds[0])); ++x) {
         const KcKind &k = kKcKinds[x];
         const int64_t units = chunk_blocks(d, packed, 16 * k.most) * d->cache.Hkv;
-        if (units >= (1 << 22) || (k.most > 1 && (int64_t)d->T_max * G <= 8 * k.most)) continue;
+        if (units >= (1 << 22) || (k.most > 1 && p.items > 0 && (int64_t)d->T_max * G <= 8 * k.most)) continue;      // (half empty: only where others are too many)
         const int64_t dealt = std::min(kKcTarget, k.slots) / units, long_enough = (int64_t)hi / least(k);
         const double parts = hi < 4.0 * least(k) ? 1.0 : (double)std::max<int64_t>(std::min(dealt, long_enough), 1);
         const double round = units * parts * k.kw <= 1024 ? k.alone : k.full, join = parts > 1 ? 0.53 + 0.4 * parts * k.most : 0.0;

@@ -254,6 +254,20 @@ def test_more_sequences_than_are_counted_through():
         check(q, cache, R, D, tables, ctx, 6, out, lse, n_new=n_new)
 
 
+def test_as_many_blocks_as_a_call_may_have():
+    """Single tokens of so many sequences and heads that blocks of 16 and 32 columns would be too many.  Every token sees one row, all of them the same one."""
+    b, rng, D, R, B, H = binding(), seed(896), 64, 16, 65535, 63
+    cache = random_cache(rng, 1, 1, H, R, D)
+    q = torch.randn((B, H, D), device="cuda").bfloat16()
+    lse = torch.empty((B, H), device="cuda")
+    out = b.radar_chunk_attention_kvq(q, gpu_cache(cache, R, D), torch.zeros((B, 1), dtype=torch.int32, device="cuda"), torch.zeros(B, dtype=torch.int32, device="cuda"),
+                                      row_starts=torch.arange(B + 1, dtype=torch.int32, device="cuda"), T_max=1, lse_out=lse)
+    k, v, _ = kvq.all_rows(cache, R, D, 0, [0], 1)
+    score = (q.double() * dev(k[0])).sum(-1) / 8.0
+    assert (out.double() == dev(v[0])).all()                         # (its weight is 1 to 2^-20, and its values are bf16's)
+    assert ((lse.double() - score).abs() <= (D + 8) * 2.0 ** -24 * (q.double() * dev(k[0])).abs().sum(-1) / 8.0 + 2.0 ** -19 * (1 + score.abs())).all()
+
+
 def test_a_chunk_beyond_its_most_rows():
     """Rows of a sequence behind its T_max-th are not there: they stay as they were."""
     b, rng, D, R = binding(), seed(894), 64, 16
