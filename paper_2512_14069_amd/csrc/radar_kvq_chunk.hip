@@ -3,6 +3,13 @@
 // Transposed as in radar_kvq_attention.hip, with its step of 32 keys (radar_kvq_step.h): a KV head's queries are counted through as columns,
 // c = row * G + head of the group, and 64 of them are a wavefront's.  Row i sees keys up to ctx + i, so a column's keys are the first so many and only
 // the last steps of a block of columns have anything to mask.
+//
+// Long chunks are bound by vector issue beside the matrix pipe: a step of 32 keys by 64 columns is 64 products and 249 vector instructions, of which about 110 turn
+// codes into operands and as many are the softmax (16384 rows, 64 heads on 8, D = 128: 3.44 ms or 1.28 PFLOP/s of what the mask leaves, the vector units issue in 77% of
+// the cycles, the matrix pipe is busy in 57%; a large library product of bf16 reaches 1.37).  So a block is as wide as the registers allow, 64 columns, wherever there are rows
+// enough.  Short chunks are bound by the way in and out of a block (finding it 0.6 to 2.6 us, its first loads 2 to 4, the merge 3 to 4: 2048 rows of 32 heads 49 us, of which 27
+// would be steps), single tokens by the rows' bytes (64 of them behind 304824 rows 61 us, 5.45 TB/s; a copy of large buffers reaches 5.1, reading and writing).
+// Two or four blocks side by side in one workgroup, for the L1's sake, gained nothing (a batch of 16 ragged chunks 369 us for 366, 16384 rows 1775 for 1779).
 #include <algorithm>
 #include <atomic>
 #include <cmath>

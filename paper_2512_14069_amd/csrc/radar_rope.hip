@@ -6,6 +6,9 @@
 //
 // A workgroup has eight rows and some of the heads.  It finds out once which sequences its rows belong to and works out their sines and cosines (two a
 // lane at D = 128), which lie in LDS until every lane has those of its eight pairs in registers; then a lane turns the same eight pairs of one head after the other.
+//
+// Many rows are bound by their bytes: 8360 rows of 40 heads, 171 MB, 35.4 us or 4.84 TB/s (16384 rows 5.3; a copy 5.1); into the cache 16384 rows of 32 heads on 8, 353 MB,
+// 79.6 us or 4.44 TB/s, as codes are stored four bytes a lane.  Few rows are one launch: 60 rows 4.0 us, into the cache 4.8.
 #include <algorithm>
 #include <cmath>
 
