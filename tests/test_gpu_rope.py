@@ -154,6 +154,45 @@ def test_append_is_a_turn_and_an_append(B, T, packed, Hq, H, D, R, P, axes, inte
     assert torch.equal(again.data, c.data)
 
 
+@pytest.mark.parametrize("D,P,interleaved", [(128, 64, False), (64, 32, True), (96, 40, False)])
+def test_more_rows_than_the_caches_hold(D, P, interleaved):
+    """Rows of more than 64 MB are read and stored past the caches: the same bits as in small calls, some of which are the oracle's, at once, in place and into the 4-bit cache."""
+    b, rng, Hq, H, R = binding(), seed(760 + D), 16, 4, 64
+    N = (64 << 20) // (D * 4 * (Hq + H)) + 77
+    inv, n_some = frequencies(P), 40
+    rope, ctx = b.Rope(dev(inv), interleaved=interleaved), dev(np.array([5], np.int32))
+    fused = torch.randn((N, Hq + 2 * H, D), device="cuda").bfloat16()
+    q, k, v = fused[:, :Hq], fused[:, Hq:Hq + H], fused[:, Hq + H:]
+    starts = dev(np.array([0, N - 3], np.int32))                     # (three rows behind the last sequence)
+    fresh = lambda n, h: torch.full((n, h, D), 3.0, dtype=torch.bfloat16, device="cuda")            # noqa: E731
+    q_out, k_out = b.radar_rope(q, k, rope, ctx_lens=ctx, row_starts=starts, T_max=N, q_out=fresh(N, Hq), k_out=fresh(N, H))
+    assert (q_out[N - 3:] == 3).all() and (k_out[N - 3:] == 3).all()
+    step = 1500
+    for at in range(0, N - 3, step):
+        n = min(step, N - 3 - at)
+        few_q, few_k = b.radar_rope(q[at:at + n][None], k[at:at + n][None], rope, ctx_lens=ctx + at)
+        assert torch.equal(few_q[0], q_out[at:at + n]) and torch.equal(few_k[0], k_out[at:at + n])
+    some = np.concatenate([np.arange(n_some), np.arange(N - 3 - n_some, N - 3)])
+    bits = bf16_bits(fused[dev(some.astype(np.int64))])
+    x = host(fused[dev(some.astype(np.int64))].double())
+    want = np.stack([rounded(kvq.turn(x[j], [5 + int(n)], inv, [0] * P, interleaved)) for j, n in enumerate(some)])
+    want[:, :, 2 * P:] = bits[:, :, 2 * P:]
+    assert np.array_equal(bf16_bits(q_out)[some], want[:, :Hq]) and np.array_equal(bf16_bits(k_out)[some], want[:, Hq:Hq + H])
+    if D in (64, 128):
+        n_blocks = -(-N // R)
+        slots = torch.randperm(n_blocks * R, device="cuda")[:N].int()[None]
+        one, two = b.KvqCache(n_blocks, R, H, D), b.KvqCache(n_blocks, R, H, D)
+        one.data.fill_(0xAA), two.data.fill_(0xAA)
+        turned_q = b.radar_kvq_append_rope(one, q, k, v, slots, rope, ctx_lens=ctx, row_starts=starts, q_out=fresh(N, Hq))
+        assert torch.equal(turned_q, q_out)
+        b.radar_kvq_append(two, k_out[:N - 3], v[:N - 3].contiguous(), slots[0, :N - 3].contiguous())
+        assert torch.equal(one.data, two.data)
+    before = fused.clone()
+    b.radar_rope(q, k, rope, ctx_lens=ctx, row_starts=starts, T_max=N, q_out=q, k_out=k)
+    assert torch.equal(q[:N - 3], q_out[:N - 3]) and torch.equal(k[:N - 3], k_out[:N - 3])
+    assert torch.equal(v, before[:, Hq + H:]) and torch.equal(fused[N - 3:], before[N - 3:])
+
+
 def test_keys_that_are_not_finite_make_blocks_of_nan():
     b, rng, D, R = binding(), seed(760), 128, 16
     x, bits = bf16(rng.normal(size=(5, 6, D)))
