@@ -334,6 +334,28 @@ def test_long_chunks():
     assert torch.equal(again, out)
 
 
+def test_rows_behind_the_32nd_bit():
+    """More than 2^31 values of queries and outputs, and 2^32 bytes: the last sequence's rows are those of a call over it alone, turned and attended to."""
+    b, rng, D, R, Hq, H, B = binding(), seed(911), 128, 64, 64, 1, 520
+    new = [511 + s % 7 for s in range(B)]
+    N, last = sum(new), new[-1]
+    tables, cache, _, _, _, T = make(rng, [40] * 2, [600] * 2, 1, H, D, R)
+    c, ctx = gpu_cache(cache, R, D), np.full(B, 40, np.int32)
+    all_tables = dev(np.concatenate([np.repeat(tables[:1], B - 1, 0), tables[1:]]))
+    starts = dev(np.concatenate([[0], np.cumsum(new)]).astype(np.int32))
+    q = torch.randn((N, Hq, D), device="cuda", dtype=torch.bfloat16)
+    assert (N - last) * Hq * D > 2 ** 31
+    rope, alone = b.Rope(dev(frequencies(64))), q[N - last:].clone()
+    b.radar_rope(q, None, rope, ctx_lens=dev(ctx), row_starts=starts, T_max=max(new), q_out=q)
+    alone, _ = b.radar_rope(alone[None], None, rope, ctx_lens=dev(ctx[:1]))
+    assert torch.equal(alone[0], q[N - last:])
+    lse = torch.empty((N, Hq), device="cuda")
+    out = b.radar_chunk_attention_kvq(q, c, all_tables, dev(ctx), row_starts=starts, T_max=max(new), S_max=600, lse_out=lse)
+    for at, n, table in ((0, 3, 0), (N - last, 3, 1), (N - 3, 3, 1)):                                # (rows of a sequence: those of a shorter one behind more)
+        before = np.array([40 + (at - (N - last) if at == N - 3 else 0)], np.int32)
+        check(host(q[at:at + n].double()), cache, R, D, tables[table:table + 1], before, n, out[at:at + n], lse[at:at + n], row_starts=np.array([0, n], np.int32))
+
+
 # ------------------------------------------------------------------ a serving step
 
 class Step:
