@@ -317,18 +317,24 @@ struct KcShape {
     }
     static constexpr int PART = COLS * D + 2 * COLS;                 // floats of a partial result
 };
-// NC: of the widest block that the kernel takes.
-template <int D, int NC, int KW>
-constexpr int kc_lds_bytes() { return KcShape<D, NC, KW>::room() + (KW + 1) * 16 * NC * 8 + 16 * NC * 4 + KW * kKcState * 4; }
+// Of a kernel whose blocks are 16 * MOST columns wide, or a half or a quarter of that.
+template <int D, int MOST, int KW>
+constexpr int kc_room() {
+    const int half = KcShape<D, MOST == 1 ? 1 : 2, KW>::room(), all = KcShape<D, MOST, KW>::room(), one = KcShape<D, 1, KW>::room();
+    return all > half ? (all > one ? all : one) : (half > one ? half : one);
+}
+template <int D, int MOST, int KW>
+constexpr int kc_lds_bytes() { return kc_room<D, MOST, KW>() + (KW + 1) * 16 * MOST * 8 + 16 * MOST * 4 + KW * kKcState * 4; }
 
 // One item.  KW wavefronts take its steps in turn and meet in LDS at the end.
 template <int D, int NC, int MOST, int KW, bool FAR>
 __device__ __forceinline__ void kc_item(unsigned char *smem, const int *state) {
     using S = KcShape<D, NC, KW>;
     constexpr int THREADS = KW * kWave;
+    static_assert(S::room() <= kc_room<D, MOST, KW>());
     u32x4 *const s_q = reinterpret_cast<u32x4 *>(smem);              // [column block][chunk][lane], the lanes' operands
     float *const s_o = reinterpret_cast<float *>(smem);              // [wavefront][column][ROW]
-    float *const s_m = reinterpret_cast<float *>(smem + KcShape<D, MOST, KW>::room()), *const s_l = s_m + KW * 16 * MOST;
+    float *const s_m = reinterpret_cast<float *>(smem + kc_room<D, MOST, KW>()), *const s_l = s_m + KW * 16 * MOST;
     float *const s_M = s_l + KW * 16 * MOST, *const s_L = s_M + 16 * MOST;
     int *const s_lim = reinterpret_cast<int *>(s_L + 16 * MOST);       // keys that a column sees
     const int lane = lane_id(), w = KW > 1 ? __builtin_amdgcn_readfirstlane(wave_id()) : 0, r = lane & 15, grp = lane >> 4;
