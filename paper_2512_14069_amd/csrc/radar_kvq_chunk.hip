@@ -311,9 +311,9 @@ struct KcShape {
     // The merge is each wavefront's for a share of the columns (2048 rows, four wavefronts: 48.8 us, 50.8 with all of it through LDS; eight: registers spill).
     static constexpr bool SPREAD = NC == 4 && (KW == 2 || KW == 4);
     static constexpr bool AS_HELD = SPREAD || KW == 1;               // partial results as registers hold them: [column block][output][lane], else [column][D]
-    static constexpr int room() {                                    // queries' operands, then the merge's buffer
-        const int q = COLS * D * 2, merge = SPREAD ? NC * KW * NM / 2 * kWave * 16 : KW > 1 ? KW * COLS * ROW * 4 : 0;
-        return q > merge ? q : merge;
+    static constexpr int room() {                                    // queries' operands, then the merge's buffer (spread: behind them, as others may still read them)
+        const int q = COLS * D * 2, merge = KW > 1 ? KW * COLS * ROW * 4 : 0;
+        return SPREAD ? q + NC * (KW - 1) * NM / 2 * kWave * 16 : q > merge ? q : merge;
     }
     static constexpr int PART = COLS * D + 2 * COLS;                 // floats of a partial result
 };
@@ -469,6 +469,49 @@ __device__ __forceinline__ void kc_item(unsigned char *smem, const int *state) {
                 s_l[w * S::COLS + n * 16 + r2] = l;
             }
         }
+        if constexpr (S::SPREAD) {
+            // Every wavefront adds up 16 of the columns, or 32.  The others' shares of them come through LDS as they lie in the registers, half the outputs at a time, and are
+            // scaled where they are added.
+            constexpr int OWN = NC / KW;                             // column blocks of a wavefront
+            floatx4 *const s_x = reinterpret_cast<floatx4 *>(smem + S::COLS * D * 2);                // [column block][wavefront behind the owner][output][lane]
+            auto place = [&](int n, int behind, int m) { return ((n * (KW - 1) + behind - 1) * (S::NM / 2) + m) * kWave + (tid & (kWave - 1)); };
+            float scl[OWN][KW], M[OWN], l[OWN];
+            auto one_half = [&](auto which) {
+                constexpr int M0 = decltype(which)::value;
+                if (M0 > 0) __syncthreads();
+#pragma unroll
+                for (int n = 0; n < NC; ++n)
+#pragma unroll
+                    for (int m = 0; m < S::NM / 2; ++m)
+                        if (w != n / OWN) s_x[place(n, (w - n / OWN) & (KW - 1), m)] = oacc[M0 + m][n];
+                __syncthreads();
+#pragma unroll
+                for (int n = 0; n < NC; ++n) {
+                    if (w != n / OWN) continue;
+                    const int o = n % OWN, col = n * 16 + r2;
+                    if constexpr (M0 == 0) {
+                        M[o] = -kKqNone;
+                        l[o] = 0.f;
+#pragma unroll
+                        for (int x = 0; x < KW; ++x) M[o] = fmaxf(M[o], scl[o][x] = s_m[((w + x) & (KW - 1)) * S::COLS + col]);
+#pragma unroll
+                        for (int x = 0; x < KW; ++x) {
+                            scl[o][x] = __builtin_amdgcn_exp2f(scl[o][x] - M[o]);
+                            l[o] += s_l[((w + x) & (KW - 1)) * S::COLS + col] * scl[o][x];
+                        }
+                    }
+#pragma unroll
+                    for (int m = 0; m < S::NM / 2; ++m) {
+                        oacc[M0 + m][n] *= scl[o][0];
+#pragma unroll
+                        for (int x = 1; x < KW; ++x) oacc[M0 + m][n] += s_x[place(n, x, m)] * scl[o][x];
+                    }
+                    if constexpr (M0 > 0) leave(n, M[o], l[o]);
+                }
+            };
+            one_half(std::integral_constant<int, 0>{});
+            one_half(std::integral_constant<int, S::NM / 2>{});
+        } else {
         __syncthreads();
         if (tid < S::COLS) {
             float m[KW], M = -kKqNone, l = 0.f;
@@ -485,35 +528,6 @@ __device__ __forceinline__ void kc_item(unsigned char *smem, const int *state) {
         float scl[NC];
 #pragma unroll
         for (int n = 0; n < NC; ++n) scl[n] = __builtin_amdgcn_exp2f(s_m[w * S::COLS + n * 16 + r2] - s_M[n * 16 + r2]);
-        if constexpr (S::SPREAD) {
-            // Every wavefront adds up 16 of the columns, or 32.  The others' shares of them come through LDS as they lie in the registers, half the outputs at a time.
-            floatx4 *const s_x = reinterpret_cast<floatx4 *>(smem);  // [column block][wavefront][output][lane]
-            auto owner = [&](int n) { return n / (NC / KW); };
-            auto place = [&](int n, int from, int m) { return ((n * KW + from) * (S::NM / 2) + m) * kWave + (tid & (kWave - 1)); };
-            auto one_half = [&](auto which) {
-                constexpr int M0 = decltype(which)::value;
-                if (M0 > 0) __syncthreads();
-#pragma unroll
-                for (int n = 0; n < NC; ++n)
-#pragma unroll
-                    for (int m = 0; m < S::NM / 2; ++m) {
-                        oacc[M0 + m][n] *= scl[n];
-                        if (w != owner(n)) s_x[place(n, w, m)] = oacc[M0 + m][n];
-                    }
-                __syncthreads();
-#pragma unroll
-                for (int n = 0; n < NC; ++n) {
-                    if (w != owner(n)) continue;
-#pragma unroll
-                    for (int x = 1; x < KW; ++x)
-#pragma unroll
-                        for (int m = 0; m < S::NM / 2; ++m) oacc[M0 + m][n] += s_x[place(n, (w + x) & (KW - 1), m)];
-                    if constexpr (M0 > 0) leave(n, s_M[n * 16 + r2], s_L[n * 16 + r2]);
-                }
-            };
-            one_half(std::integral_constant<int, 0>{});
-            one_half(std::integral_constant<int, S::NM / 2>{});
-        } else {
         constexpr int Q4 = S::DP / 4, TPC = THREADS / S::COLS < Q4 ? THREADS / S::COLS : Q4, IPT = Q4 / TPC;      // fours of a pass; lanes of a column
 #pragma unroll
         for (int pass = 0; pass < S::PASSES; ++pass) {               // of a column: d = D/4 * part + (4 / PASSES * pass + e) * NM + m
