@@ -7,7 +7,7 @@
 // Long chunks are bound by vector issue beside the matrix pipe: a step of 32 keys by 64 columns is 64 products and 249 vector instructions, of which about 110 turn
 // codes into operands and as many are the softmax (16384 rows, 64 heads on 8, D = 128: 3.44 ms or 1.28 PFLOP/s of what the mask leaves, the vector units issue in 77% of
 // the cycles, the matrix pipe is busy in 57%; a large library product of bf16 reaches 1.37).  So a block is as wide as the registers allow, 64 columns, wherever there are rows
-// enough.  Short chunks are bound by the way in and out of a block (finding it 0.6 to 2.6 us, its first loads 2 to 4, the merge 3 to 4: 2048 rows of 32 heads 49 us, of which 27
+// enough.  Short chunks are bound by the way in and out of a block (finding it 0.6 to 2.6 us, its first loads 2 to 4, the merge 3 to 4: 2048 rows of 32 heads 48 us, of which 27
 // would be steps), single tokens by the rows' bytes (64 of them behind 304824 rows 61 us, 5.45 TB/s; a copy of large buffers reaches 5.1, reading and writing).
 // Two or four blocks side by side in one workgroup, for the L1's sake, gained nothing (a batch of 16 ragged chunks 369 us for 366, 16384 rows 1775 for 1779).
 #include <algorithm>
@@ -688,10 +688,10 @@ static radar_status check_chunk(const radar_kvq_chunk_desc *d) {
     return RADAR_OK;
 }
 
-// Blocks of columns of a KV head, at most: of [B,T_max], or of N rows in B sequences.
+// Blocks of columns of a KV head, at most: of [B,T_max], or of N rows in B sequences (as they are counted through, or looked up by where they begin).
 static int64_t chunk_blocks(const radar_kvq_chunk_desc *d, bool packed, int cols) {
-    const int64_t G = d->Hq / d->cache.Hkv;
-    return packed ? d->N * G / cols + d->B : (int64_t)d->B * (((int64_t)d->T_max * G + cols - 1) / cols);
+    const int64_t G = d->Hq / d->cache.Hkv, most = (int64_t)d->B * (((int64_t)d->T_max * G + cols - 1) / cols), begun = d->N * G / cols + d->B;
+    return !packed ? most : d->B <= kKcPlanned ? std::min(most, begun) : begun;
 }
 
 struct KcRoom { size_t off_part, bytes; };
@@ -702,16 +702,20 @@ static KcRoom chunk_room(int D) {
     return r;
 }
 
-// Columns of a block and wavefronts of a workgroup: whichever takes least by a model of rounds (a step of every wavefront), what a block costs besides and
-// what a part costs to join.  Its figures are a fit to the times of all seven kinds in 65 shapes (1 to 16384 rows in 1 to 256 sequences behind 0 to 65536, groups of 1, 4 and 8,
-// D = 64 and 128, one MI355X); what it picks took 1.4% longer than the best one in the mean, 15% at most.  us, best and worst kind: 64 rows 5.6 (16 columns, four
-// wavefronts) to 12; 64 behind 16384 29 (32, eight) to 104; 512 behind 16384 127 (64, eight) to 215; 2048 49 (64, four) to 89; 16384 1829 (64, one) to 3298.
+// Columns of a block, wavefronts of a workgroup, and whether long blocks are divided: whichever takes least by a model of rounds (a step of every wavefront), what a block costs
+// besides and what a part costs to join.  Its figures are a fit to the times of all seven kinds, divided and whole, in 155 shapes (1 to 16384 rows in 1 to 256 sequences behind 0 to
+// 100000, single tokens, trees, prompts and mixtures; groups of 1, 4 and 8, D = 64 and 128, one MI355X); what it picks took 1.4% longer than the best of them in the mean, 26% at most (one
+// piece of a prompt among 15 tokens).  us, best and worst kind: 64 rows 5.6 (16 columns, four wavefronts) to 12; 64 behind 16384 29 (32, eight) to 104; 512 behind 16384 123 (64, eight) to
+// 215; 2048 47 (64, four) to 89; 16384 1764 (64, one) to 3298.  Divided and whole: 128 rows behind 2048 16.7 and 12.8, five rows each of eight sequences behind 2048 16.0 and 13.5, a single
+// token behind 2048 9.2 and 10.9.
 struct KcKind {
     int most, kw, slots;                                   // blocks of 16 * most columns; wavefronts; workgroups that the chip holds at once
-    double alone, full, end;                               // us: a round with one wavefront a SIMD, and with as many as there is room for; what a block costs besides
+    double alone, full, end;                               // us: a round of a workgroup that is alone, and with as many as there is room for; what a block costs besides
 };
-constexpr KcKind kKcKinds[] = {{1, 8, 512, 0.33, 1.32, 4.7}, {1, 4, 1024, 1.08, 1.47, 3.9}, {2, 8, 256, 0.96, 0.94, 5.8},
-                               {4, 8, 256, 0.99, 1.54, 7.3}, {4, 4, 512, 1.18, 1.59, 4.9}, {4, 2, 1024, 1.26, 1.73, 5.0}, {4, 1, 2048, 1.31, 1.37, 4.5}};
+constexpr KcKind kKcKinds[] = {{1, 8, 512, 0.68, 1.33, 4.56}, {1, 4, 1024, 0.81, 1.31, 3.87}, {2, 8, 256, 0.71, 1.01, 5.21},
+                               {4, 8, 256, 1.24, 1.44, 8.8}, {4, 4, 512, 1.0, 1.53, 4.92}, {4, 2, 1024, 1.26, 1.42, 7.42}, {4, 1, 2048, 1.05, 1.38, 6.5}};
+constexpr double kKcAlone = 0.31;                          // a round is as long as alone up to this share of the workgroups that there is room for
+constexpr int kKcWhole = 1 << 28;                          // least steps of a part where nothing is divided
 struct KcPlan {
     int kind, target, least, level_bits;
     int64_t items;
@@ -731,15 +735,16 @@ static KcPlan plan_chunk(const radar_kvq_chunk_desc *d, bool packed) {
         const int64_t units = chunk_blocks(d, packed, 16 * k.most) * d->cache.Hkv;
         if (units >= (1 << 22) || (k.most > 1 && p.items > 0 && (int64_t)d->T_max * G <= 8 * k.most)) continue;      // (half empty: only where others are too many)
         const int64_t dealt = std::min(kKcTarget, k.slots) / units, long_enough = (int64_t)hi / least(k);
-        const double parts = hi < 4.0 * least(k) ? 1.0 : (double)std::max<int64_t>(std::min(dealt, long_enough), 1);
-        const double round = units * parts * k.kw <= 1024 ? k.alone : k.full, join = parts > 1 ? 0.53 + 0.4 * parts * k.most : 0.0;
-        const double one = std::ceil(hi / parts / k.kw) * round + k.end + join, all = units * parts / k.slots * (mid / parts / k.kw * round + k.end + join);
-        const double us = std::max(one, all);
-        if (us < best) { best = us; p.kind = x; p.items = units; }
+        const int64_t divided = hi < 4.0 * least(k) ? 1 : std::max<int64_t>(std::min(dealt, long_enough), 1);
+        for (int64_t parts = divided; parts > 0; parts = parts > 1 && !d->rows_per_split ? 1 : 0) {
+            const double fill = (double)(units * parts) / k.slots, round = k.alone + (k.full - k.alone) * std::max(std::min(fill, 1.0) - kKcAlone, 0.0) / (1.0 - kKcAlone);
+            const double end = k.end + (parts > 1 ? 0.52 + 0.54 * (double)parts * k.most : 0.0), steps = 1.0 / (double)parts / k.kw;
+            const double us = std::max(std::ceil(hi * steps) * round + end, fill * (mid * steps * round + end));          // the longest block; all of them
+            if (us < best) { best = us; p.kind = x; p.items = units; p.least = parts == 1 && divided > 1 ? kKcWhole : least(k); }
+        }
     }
     const KcKind &k = kKcKinds[p.kind];
     p.target = d->B <= kKcPlanned ? std::min(kKcTarget, k.slots) : 0;
-    p.least = least(k);
     p.level_bits = 31;
     if (d->B > 1 && d->B <= kWave)                         // (one sequence's blocks are in that order anyway)
         for (p.level_bits = 5; ((int64_t)d->S_max >> p.level_bits) >= kKcLevels; ++p.level_bits) {}

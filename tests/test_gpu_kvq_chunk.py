@@ -89,10 +89,12 @@ def test_against_the_oracle(ctx, new, Hq, H, D, R, packed):
 
 
 # Sequences, rows of each, heads, the rows that the call is planned for, and the kernel that it comes to, with and without blocks in parts.
-KINDS = [("kvq_chunk_16x8", 1, 7, 2, 1, 20000), ("kvq_chunk_16x8", 17, 5, 2, 2, 20000), ("kvq_chunk_16x4", 17, 1, 16, 16, 2000), ("kvq_chunk_16x4", 17, 1, 8, 8, 300),
-         ("kvq_chunk_32x8", 1, 40, 16, 2, 100000), ("kvq_chunk_32x8", 5, 16, 16, 8, 100000), ("kvq_chunk_64x8", 1, 64, 32, 2, 100000), ("kvq_chunk_64x8", 5, 16, 32, 2, 20000),
-         ("kvq_chunk_64x4", 1, 64, 64, 8, 20000), ("kvq_chunk_64x4", 17, 16, 64, 16, 700), ("kvq_chunk_64x2", 17, 16, 128, 32, 300), ("kvq_chunk_64x2", 1, 40, 256, 64, 100000),
-         ("kvq_chunk_64x1", 17, 5, 512, 64, 300)]
+KINDS = [("kvq_chunk_16x8", 1, 7, 2, 1, 20000), ("kvq_chunk_16x8", 17, 5, 2, 2, 20000), ("kvq_chunk_16x8", 17, 1, 16, 16, 2000), ("kvq_chunk_16x8", 17, 1, 8, 8, 300),
+         ("kvq_chunk_16x4", 3, 64, 64, 8, 300), ("kvq_chunk_16x4", 1, 40, 256, 32, 300),
+         ("kvq_chunk_32x8", 1, 40, 16, 2, 100000), ("kvq_chunk_32x8", 5, 16, 16, 8, 100000), ("kvq_chunk_32x8", 5, 16, 32, 2, 20000),
+         ("kvq_chunk_64x8", 1, 64, 32, 2, 100000), ("kvq_chunk_64x8", 1, 64, 64, 8, 20000), ("kvq_chunk_64x8", 3, 16, 64, 16, 20000),
+         ("kvq_chunk_16x4", 17, 16, 64, 16, 700), ("kvq_chunk_64x4", 3, 16, 128, 16, 20000), ("kvq_chunk_64x4", 17, 16, 128, 32, 300), ("kvq_chunk_64x2", 17, 5, 512, 64, 300),
+         ("kvq_chunk_64x2", 1, 40, 256, 64, 100000), ("kvq_chunk_64x1", 17, 40, 128, 32, 300), ("kvq_chunk_64x1", 40, 5, 512, 64, 300)]
 
 
 @pytest.mark.parametrize("far", [False, True])
