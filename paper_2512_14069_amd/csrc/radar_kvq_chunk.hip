@@ -688,10 +688,10 @@ static radar_status check_chunk(const radar_kvq_chunk_desc *d) {
     return RADAR_OK;
 }
 
-// Blocks of columns of a KV head, at most: of [B,T_max], or of N rows in B sequences (as they are counted through, or looked up by where they begin).
+// Blocks of columns of a KV head, at most: of [B,T_max], or of N rows in B sequences.
 static int64_t chunk_blocks(const radar_kvq_chunk_desc *d, bool packed, int cols) {
-    const int64_t G = d->Hq / d->cache.Hkv, most = (int64_t)d->B * (((int64_t)d->T_max * G + cols - 1) / cols), begun = d->N * G / cols + d->B;
-    return !packed ? most : d->B <= kKcPlanned ? std::min(most, begun) : begun;
+    const int64_t G = d->Hq / d->cache.Hkv;
+    return packed ? d->N * G / cols + d->B : (int64_t)d->B * (((int64_t)d->T_max * G + cols - 1) / cols);
 }
 
 struct KcRoom { size_t off_part, bytes; };
@@ -732,7 +732,8 @@ static KcPlan plan_chunk(const radar_kvq_chunk_desc *d, bool packed) {
     p.items = 0;
     for (int x = 0; x < (int)(sizeof(kKcKinds) / sizeof(kKcKinds[0])); ++x) {
         const KcKind &k = kKcKinds[x];
-        const int64_t units = chunk_blocks(d, packed, 16 * k.most) * d->cache.Hkv;
+        int64_t units = chunk_blocks(d, packed, 16 * k.most) * d->cache.Hkv;
+        if (packed && d->B <= kKcPlanned) units = std::min(units, chunk_blocks(d, false, 16 * k.most) * d->cache.Hkv);      // (counted through, not looked up by where they begin)
         if (units >= (1 << 22) || (k.most > 1 && p.items > 0 && (int64_t)d->T_max * G <= 8 * k.most)) continue;      // (half empty: only where others are too many)
         const int64_t dealt = std::min(kKcTarget, k.slots) / units, long_enough = (int64_t)hi / least(k);
         const int64_t divided = hi < 4.0 * least(k) ? 1 : std::max<int64_t>(std::min(dealt, long_enough), 1);
