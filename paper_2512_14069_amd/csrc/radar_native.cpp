@@ -486,9 +486,11 @@ PyObject *tree_attention_kvq(PyObject *, PyObject *const *args, Py_ssize_t n) {
     return fresh.defined() ? THPVariable_Wrap(std::move(fresh)) : done(rc, out_obj);
 }
 
-// A batch's new rows: [B,T,heads,D], or [N,heads,D] and where each sequence's begin.  most: of a sequence's rows, 0: not given.
+// A batch's new rows: [B,T,heads,D], or [N,heads,D] and where each sequence's begin.  most: of a sequence's rows, 0: not given; what is less than that the
+// other path refuses.
 struct NewRows { int64_t B, T, N; };
 bool new_rows(const at::Tensor *x, const at::Tensor *ctx, const at::Tensor *starts, const at::Tensor *fresh, int32_t most, NewRows *rows) {
+    if (most < 0) return false;
     if (starts) {
         if (x->dim() != 3 || starts->dim() != 1 || starts->numel() < 2 || fresh) return false;
         *rows = NewRows{starts->numel() - 1, most > 0 ? most : x->size(0), x->size(0)};
