@@ -678,7 +678,7 @@ radar_status radar_tree_attention_kvq(const void *q, const void *cache, const in
  * ctx_lens[b] < 0, are left as they were.  q_out may be q, and k_out k, with the same strides; other overlaps of an output are not allowed.
  * q, q_out bf16 [N,Hq,D], k, k_out bf16 [N,Hkv,D], D contiguous, strides in elements, 0 => dense, rows 16-byte aligned; q or k may be NULL
  * with its output; positions i32 [axes,N]; inv_freq f32 [P]; n_new, ctx_lens i32 [B].  No workspace; one kernel.
- * Limits: D and rotary_dim multiples of 16, D <= 256; 1 <= axes <= 4; N / 8 * (3 + (Hq + 2 Hkv) / 8) < 2^24. */
+ * Limits: D and rotary_dim multiples of 16, D <= 256; 1 <= axes <= 4; B <= 2^30; N / 8 * (3 + (Hq + 2 Hkv) / 8) < 2^24. */
 typedef struct radar_rope_desc {
     int32_t B, T_max;
     int32_t Hq, Hkv, D;

@@ -21,6 +21,7 @@ namespace radar {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kRpThreads = 256, kRpRows = 8;
+constexpr int kRpSequences = 1 << 30;          // most: a sequence and a wavefront's lanes behind it are counted in 32 bits
 constexpr int64_t kRpGroups = 512;             // workgroups to aim for (960 rows of trees: 7.4 us with 512, 8.0 with 256, 9.1 with 1024)
 
 struct RpArgs {
@@ -330,7 +331,7 @@ static radar_status rope_args(const void *q, const void *k, const void *v, void 
     if ((q && d->Hq < 1) || (k && d->Hkv < 1) || !std::isfinite(d->scale) || (d->interleaved != 0 && d->interleaved != 1)) return RADAR_INVALID_ARG;
     const int rotary = d->rotary_dim ? d->rotary_dim : d->D;
     if (rotary > d->D) return RADAR_INVALID_ARG;
-    if (d->D % 16 != 0 || d->D > 256 || rotary % 16 != 0 || d->axes > 4 || d->N > INT32_MAX || d->Hq > 65535 || d->Hkv > 65535) return RADAR_UNSUPPORTED_SHAPE;
+    if (d->D % 16 != 0 || d->D > 256 || rotary % 16 != 0 || d->axes > 4 || d->N > INT32_MAX || d->Hq > 65535 || d->Hkv > 65535 || d->B > kRpSequences) return RADAR_UNSUPPORTED_SHAPE;
     g->pairs = rotary / 2;
     for (int j = 0; j < g->pairs; ++j) {
         if (d->pair_axis[j] >= d->axes) return RADAR_INVALID_ARG;

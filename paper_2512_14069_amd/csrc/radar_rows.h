@@ -5,7 +5,7 @@
 
 namespace radar {
 
-// The last of n >= 1 sequences whose value(b) is at most x, -1 if there is none; values that never fall.  Sixty-four are looked at at a time,
+// The last of n (1 to 2^30) sequences whose value(b) is at most x, -1 if there is none; values that never fall.  Sixty-four are looked at at a time,
 // so that up to 64 sequences take one round trip, 4096 two.  The same x in every lane; all lanes call.  Any values keep the result within [-1, n).
 template <typename Value>
 __device__ __forceinline__ int last_at_most(int n, int64_t x, Value value) {
