@@ -1067,8 +1067,8 @@ def radar_kvq_append_rope(cache, q, k, v, slots, rope, positions=None, ctx_lens=
     [B,T_max], as radar_kvq_blocks gives them).  k, v bf16 [B,T,Hkv,D] or [N,Hkv,D] with the same strides; q may be None.  Returns q_out."""
     if slots.dim() != 2:
         raise ValueError(f"slots: expected [B, T_max], got {tuple(slots.shape)}")
-    if tuple(k.shape) != tuple(v.shape) or tuple(k.shape[-2:]) != (cache.Hkv, cache.D) or k.stride() != v.stride():
-        raise ValueError(f"k, v: expected [..., {cache.Hkv}, {cache.D}] with the same strides, got {tuple(k.shape)} and {tuple(v.shape)}")
+    if tuple(k.shape) != tuple(v.shape) or tuple(k.shape[-2:]) != (cache.Hkv, cache.D) or any(n > 1 and x != y for n, x, y in zip(k.shape, k.stride(), v.stride())):
+        raise ValueError(f"k, v: expected [..., {cache.Hkv}, {cache.D}] with the same strides, got {tuple(k.shape)} {k.stride()} and {tuple(v.shape)} {v.stride()}")
     q_out = None if q is None else _same_rows(q_out, q, "q_out")
     if slots.shape[1] != 0 and (native := _direct(prepared)) and native.kvq_append_rope(
             *rope._native(positions, ctx_lens, row_starts, n_new, slots.shape[1]), q, k, q_out, v, slots, cache.data, cache.block_rows, cache.D, layer):

@@ -516,6 +516,13 @@ bool row_strides(const at::Tensor *x, int64_t *row, int64_t *head) {
     return x->size(dims - 2) == 1 || *head != 0;
 }
 
+// of tensors of the same sizes, where an axis has more than one entry
+bool same_strides(const at::Tensor *x, const at::Tensor *y) {
+    for (int64_t i = 0; i < x->dim(); ++i)
+        if (x->size(i) > 1 && x->stride(i) != y->stride(i)) return false;
+    return true;
+}
+
 // inv_freq, axes, pair_axis (bytes), interleaved, scale, positions, ctx_lens, row_starts, n_new, T_max (0: not given), q, k, q_out, k_out: what turns and
 // appends share
 struct RopeCall {
@@ -578,7 +585,7 @@ PyObject *kvq_append_rope(PyObject *, PyObject *const *args, Py_ssize_t n) {
     if (!c.read(r, true)) Py_RETURN_NONE;
     const at::Tensor *v = r.tensor(at::kBFloat16, false), *slots = r.i32(), *data = read_cache(r, &d);
     const int32_t layer = r.integer();
-    if (!r.ok || layer < 0 || layer >= d.layers || v->sizes() != c.k->sizes() || v->strides() != c.k->strides() || !sized(slots, {c.d.B, c.d.T_max}) ||
+    if (!r.ok || layer < 0 || layer >= d.layers || v->sizes() != c.k->sizes() || !same_strides(v, c.k) || !sized(slots, {c.d.B, c.d.T_max}) ||
         c.d.Hkv != d.Hkv || c.d.D != d.D || !here({c.inv, c.positions, c.ctx, c.starts, c.fresh, c.q, c.k, c.q_out, v, slots, data})) Py_RETURN_NONE;
     auto p = [](const at::Tensor *t) { return Reader::pointer<int32_t>(t); };
     return done(call(lib.kvq_append_rope, c.at(c.q), c.at(c.k), v->data_ptr(), c.at(c.q_out), Reader::pointer<float>(c.inv), p(c.positions), p(c.ctx), p(c.starts),

@@ -7,6 +7,7 @@ from gpu_util import dev
 from kvq_util import seed
 from test_gpu_kvq import binding
 from test_gpu_rope import frequencies
+from test_gpu_support import _Both
 
 pytestmark = pytest.mark.gpu
 
@@ -30,3 +31,23 @@ def test_less_than_no_rows_are_refused(packed, T_max):
                 if prepared:
                     got()
     assert (out == 1).all()
+
+
+@pytest.mark.parametrize("Hkv,N", [(2, 1), (1, 4), (1, 1)])
+def test_strides_of_one_entry_say_nothing(Hkv, N, monkeypatch):
+    """Keys and values whose strides differ only where an axis has one entry: the bytes of the same call over dense ones, by the native half and by ctypes."""
+    b, rng, D = binding(), seed(995 + N), 64
+    dense = [torch.from_numpy(rng.normal(size=(1, N, Hkv, D))).bfloat16().cuda() for _ in range(2)]
+    k, v = dense[0], dense[1].as_strided((1, N, Hkv, D), (8 * D * N * Hkv, Hkv * D if N > 1 else 48 * D, D if Hkv > 1 else 16 * D, 1))
+    assert torch.equal(v, dense[1]) and v.stride() != k.stride()
+    rope, slots = b.Rope(dev(frequencies(32))), torch.arange(N, dtype=torch.int32, device="cuda")[None]
+
+    def bytes_of(v):
+        c = b.KvqCache(2, 16, Hkv, D)
+        c.data.fill_(0xAA)
+        b.radar_kvq_append_rope(c, None, k, v, slots, rope)
+        return c.data
+    want = bytes_of(dense[1])
+    got = []
+    _Both(b, monkeypatch)("append", lambda: got.append(bytes_of(v)) or got[-1:])
+    assert len(got) == 2 and all(torch.equal(x, want) for x in got)
