@@ -91,13 +91,14 @@ __device__ __forceinline__ int kc_rows_on(int t, const KcWork &a) {
     return (int)((uint32_t)t * a.by_G >> 16);
 }
 
-// What a workgroup does: a block of columns of a KV head, the first of them of row i0, and the steps [s0, s1) of it, one of `parts` such.
-struct KcItem { int b, hk, cg, i0, n, rows, row0, L, limit, s0, s1, parts, slot, unit; };
+// What a workgroup does: a block of columns of a KV head, the first of them of row i0, and the steps [s0, s1) of it, one of `parts` such, whose results lie one behind the other
+// from `slot` on.
+struct KcItem { int b, hk, cg, i0, n, rows, row0, L, limit, s0, s1, part, parts, slot, unit; };
 constexpr int kKcState = 16;
 
 // Every item in one line, those with the most keys first, so that the workgroups that start last have little to do: by level (eighths or so of the longest
 // context that a block's first row sees), in it sequence by sequence, from the last block of columns to the first, part by part and KV head by KV head (workgroups go
-// to the eight XCDs in turn: a head's rows then stay in one L2).  A sequence's blocks are divided into parts of `per` steps or a little more, which is the batch's
+// to the eight XCDs in turn: a head's rows then stay in one L2).  A sequence's blocks are divided into parts of about `per` steps, none of fewer than `least`; `per` is the batch's
 // work over the workgroups that it is dealt to, so that there are no more items than blocks and workgroups, and no more parts than workgroups.  A step
 // of 16 columns counts for half a step of 64.  The quotients are by reciprocals, rounded to the safe side, as this is a chain that every workgroup goes through.
 // All lanes call; the result is the same in all of them.
@@ -227,21 +228,23 @@ __device__ __forceinline__ bool kc_find(KcItem &x, const KcWork &a, uint32_t ite
     x.unit = (int)unit0 + x.cg * Hkv + x.hk;
     x.slot = 0;
     x.parts = 1;
-    int each = steps;
+    int each = steps, short_ones = 1;          // of x.parts parts the first short_ones have `each` steps, the others one more
     if (p > 1) {
-        // of a sequence that is divided, as many parts as are as long as its last block's
+        // of a sequence that is divided, as many parts as are as long as its last block's, but none of fewer keys than a.least steps have (so the part with the
+        // last keys, whose last step may be half empty, is a longer one where there are any)
         const int longest = (s.total + 31) >> 5, wanted_steps = (longest + p - 1) / p;
-        int wanted = min((steps + wanted_steps - 1) / max(wanted_steps, 1), p);
+        int wanted = max(min(min((steps + wanted_steps - 1) / max(wanted_steps, 1), p), (x.limit >> 5) / a.least), 1);
         x.slot = (int)(slot0 + (uint32_t)(x.cg * Hkv + x.hk) * (uint32_t)p);
         // (there is room by the bounds above; row_starts that falls may break them)
         if (x.cg < 0 || x.slot < 0 || x.slot > kKcTarget - wanted || (uint32_t)x.unit >= (uint32_t)kKcTarget) wanted = 1;
-        each = (steps + wanted - 1) / max(wanted, 1);
-        if (steps > 0) x.parts = (steps + each - 1) / each;
-        x.slot += part;
+        x.parts = wanted;
+        each = steps / wanted;
+        short_ones = wanted - (steps - each * wanted);
     }
     if (x.cg < 0 || part >= x.parts) return false;
-    x.s0 = part * each;
-    x.s1 = min(x.s0 + each, steps);
+    x.part = part;
+    x.s0 = part * each + max(part - short_ones, 0);
+    x.s1 = x.s0 + each + (part >= short_ones ? 1 : 0);
     return true;
 }
 
@@ -419,7 +422,7 @@ __device__ __forceinline__ void kc_item(unsigned char *smem, const int *state) {
     asm volatile("" : "+v"(tid));                                    // (addresses are worked out here, and not kept from the start)
     const int r2 = tid & 15, grp2 = (tid >> 4) & 3;
     const int live = min(p.n * G - p.cg * 16 * MOST, S::COLS);       // columns of the block that there are
-    float *const to = a.part + (size_t)p.slot * KcShape<D, MOST, KW>::PART;
+    float *const to = a.part + (size_t)(p.slot + p.part) * KcShape<D, MOST, KW>::PART;
     auto hand_over = [&](int at, float x0, float x1) {
         store_shared_result(reinterpret_cast<uint64_t *>(to + at), (uint64_t)__float_as_uint(x1) << 32 | __float_as_uint(x0));
     };
@@ -574,8 +577,7 @@ __device__ __forceinline__ void kc_item(unsigned char *smem, const int *state) {
     unsigned int *const counter = a.arrived + p.unit * kKcArrived;
     if ((int)publish_then_ticket(counter, reinterpret_cast<unsigned int *>(s_m)) != p.parts - 1) return;
     if (threadIdx.x == 0) store_shared_result(counter, 0u);
-    const int each = (((p.limit + 31) >> 5) + p.parts - 1) / p.parts;
-    const float *const from = a.part + (size_t)(p.slot - p.s0 / each) * KcShape<D, MOST, KW>::PART;
+    const float *const from = a.part + (size_t)p.slot * KcShape<D, MOST, KW>::PART;
     constexpr size_t apart = KcShape<D, MOST, KW>::PART;
     int first = threadIdx.x;
     asm volatile("" : "+v"(first));

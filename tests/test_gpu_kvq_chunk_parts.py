@@ -78,3 +78,24 @@ def test_parts_in_every_kind(name, ctx, new, Hq, H, split, widths, D, far):
     assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1])
     del c
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("ctx,new,Hq,H,D,split", [([512], [3], 1, 1, 128, 128), ([365], [3], 1, 1, 64, 64), ([11815], [402], 1, 1, 64, 512), ([11815], [402], 1, 1, 128, 448),
+                                                  ([2500], [100], 8, 2, 128, 192), ([4000, 10, 900], [1, 300, 40], 8, 2, 64, 320), ([6000, 5000], [200, 31], 8, 2, 128, 1024),
+                                                  ([5003], [3], 64, 2, 64, 192), ([1300, 1290, 3101], [64, 64, 90], 8, 1, 128, 256)])
+def test_no_part_has_fewer_rows_than_asked_for(ctx, new, Hq, H, D, split):
+    """Queries of zeros weigh every key alike: a part's sum, of the block's last column, is the number of its keys.  Between them the parts have all the keys of their columns."""
+    b, rng, R, ctx = binding(), seed(960 + sum(new) + D), 32, np.array(ctx, np.int32)
+    S = int((ctx + np.array(new)).max())
+    tables, cache, q, bits, starts, T = make(rng, ctx, new, Hq, H, D, R)
+    c = gpu_cache(cache, R, D)
+    ws = workspace(b, bf16_dev(bits), c, tables.shape[1], len(ctx), T, len(q), S)
+    got = {}
+    name, = ran(lambda: got.update(r=attend(b, np.zeros_like(bits), None, tables, ctx, starts, None, T, c=c, R=R, D=D, S_max=S, workspace=ws, rows_per_split=split)))
+    out, lse = got["r"]
+    check(np.zeros_like(q), cache, R, D, tables, ctx, T, out, lse, row_starts=starts)
+    parts = parts_of(ws, D, int(name[len("kvq_chunk_"):].split("x")[0]))
+    assert len(parts) > 1
+    # (a column that is not there has no word: what the bytes before it make is less than zero)
+    keys = np.array([sums[sums >= 0].max() for _, sums in parts])
+    assert (keys == np.round(keys)).all() and keys.min() >= split, (name, np.sort(keys)[:8])
