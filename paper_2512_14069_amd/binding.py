@@ -953,8 +953,8 @@ class Rope:
         P = inv_freq.numel()
         if inv_freq.dim() != 1 or not 1 <= P <= 128:
             raise ValueError(f"inv_freq: expected 1 to 128 frequencies, got shape {tuple(inv_freq.shape)}")
-        if scale == 0.0:
-            raise ValueError("scale must not be 0")
+        if ctypes.c_float(scale).value == 0.0:
+            raise ValueError(f"scale must not be 0 in 32 bits, got {scale}")
         self.pair_axis = [0] * P if pair_axis is None else [int(a) for a in pair_axis]
         if len(self.pair_axis) != P or not all(0 <= a < axes for a in self.pair_axis):
             raise ValueError(f"pair_axis: expected {P} numbers of {axes} axes")

@@ -11,3 +11,13 @@ def test_more_sequences_than_are_counted(lib, B):  # noqa: F811
     assert rope_call(lib, starts=ONE, B=B, N=4) == -2
     assert append_call(lib, 7, ONE, B=B, N=4) == -2                  # (7: row_starts)
     assert rope_call(lib, starts=ONE, B=1 << 30, N=0) == 0           # nothing to do, nothing launched
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.0, 1e-50, -1e-46])
+def test_a_scale_that_32_bits_make_zero(scale):
+    """The descriptor's zero stands for one."""
+    import torch
+    from paper_2512_14069_amd import binding as b
+    with pytest.raises(ValueError):
+        b.Rope(torch.ones(8), scale=scale)
+    assert b.Rope(torch.ones(8), scale=1e-45).desc().scale != 0.0
