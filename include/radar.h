@@ -627,8 +627,10 @@ radar_status radar_kvq_commit(void *cache, const int32_t *block_tables, int32_t 
  * of out and lse are written as zero, as are rows i >= n_nodes[b].  Where no row is
  * allowed, out is zero and lse -inf.  A row that is not allowed has no influence,
  * whatever it holds (NaN blocks included).
- * T_max = 1 is the form for single tokens; parents == NULL: node i hangs under
- * node i - 1 (a chain: causal attention of up to RADAR_T_MAX rows).
+ * T_max = 1 takes single tokens (so does radar_chunk_attention_kvq, which is the
+ * quicker call where they see hundreds of thousands of rows between them); parents
+ * == NULL: node i hangs under node i - 1 (a chain: causal attention of up to
+ * RADAR_T_MAX rows).
  * cache: the layer's first block; block_tables i32 [B,max_blocks]; S_max: the rows
  * that the call is planned for, at most max_blocks * block_rows (the longest
  * ctx_lens[b] + T_max where it is known).  Other arguments and limits as for
@@ -723,7 +725,8 @@ typedef struct radar_kvq_chunk_desc {
     radar_kvq_desc cache;    /* layers and layer_stride are ignored */
     int32_t B, T_max, Hq, max_blocks, S_max;
     int32_t rows_per_split;  /* 0 => chosen by the library; else a multiple of 64: cache rows that one workgroup takes, and no fewer, before
-                                partial results are joined (as many as the workspace has room for) */
+                                partial results are joined (as many as the workspace has room for; rows of fewer than four times as many
+                                are not divided, nor is anything in a call of more than 512 sequences) */
     int64_t N;
     int64_t q_stride_b, q_stride_t, q_stride_h;
     int64_t out_stride_b, out_stride_t, out_stride_h;

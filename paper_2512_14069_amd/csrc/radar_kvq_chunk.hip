@@ -5,11 +5,11 @@
 // the last steps of a block of columns have anything to mask.
 //
 // Long chunks are bound by vector issue beside the matrix pipe: a step of 32 keys by 64 columns is 64 products and 249 vector instructions, of which about 110 turn
-// codes into operands and as many are the softmax (16384 rows, 64 heads on 8, D = 128: 3.44 ms or 1.28 PFLOP/s of what the mask leaves, the vector units issue in 77% of
+// codes into operands and as many are the softmax (16384 rows, 64 heads on 8, D = 128: 3.43 to 3.57 ms by machine, 1.23 to 1.28 PFLOP/s of what the mask leaves, the vector units issue in 77% of
 // the cycles, the matrix pipe is busy in 57%; a large library product of bf16 reaches 1.37).  So a block is as wide as the registers allow, 64 columns, wherever there are rows
 // enough.  Short chunks are bound by the way in and out of a block (finding it 0.6 to 2.6 us, its first loads 2 to 4, the merge 3 to 4: 2048 rows of 32 heads 48 us, of which 27
 // would be steps), single tokens by the rows' bytes (64 of them behind 304824 rows 61 us, 5.45 TB/s; a copy of large buffers reaches 5.1, reading and writing).
-// Two or four blocks side by side in one workgroup, for the L1's sake, gained nothing (a batch of 16 ragged chunks 369 us for 366, 16384 rows 1775 for 1779).
+// Two or four blocks side by side in one workgroup, for the L1's sake, gained nothing (a lighter batch of 16 chunks 369 us for 366, 16384 rows of 32 heads 1775 for 1779).
 #include <algorithm>
 #include <atomic>
 #include <cmath>
@@ -22,7 +22,8 @@ namespace radar {
 
 constexpr int kKcCols = 64;                    // columns of the widest block
 constexpr int kKcTarget = 1024;                // most workgroups that what is divided is dealt to, and most parts
-constexpr int kKcPlanned = 512;                // most sequences whose work every workgroup counts through
+constexpr int kKcPlanned = 512;                // most sequences whose work every workgroup counts through.  Nothing is divided beyond (512 single tokens, one of them behind
+                                               // 65536 rows, 71 us; 513 352)
 constexpr int kKcArrived = 16;                 // counters are 64 bytes apart: atomics on one line wait for each other
 
 struct KcArgs {
@@ -706,12 +707,13 @@ static KcRoom chunk_room(int D) {
 
 // Columns of a block, wavefronts of a workgroup, and whether long blocks are divided: whichever takes least by a model of rounds (a step of every wavefront), what a block costs
 // besides and what a part costs to join.  Its figures are a fit to the times of all seven kinds, divided and whole, in 155 shapes (1 to 16384 rows in 1 to 256 sequences behind 0 to
-// 100000, single tokens, trees, prompts and mixtures; groups of 1, 4 and 8, D = 64 and 128, one MI355X); what it picks took 1.4% longer than the best of them in the mean, 26% at most (one
+// 100000, single tokens, trees, prompts and mixtures; groups of 1, 4 and 8, D = 64 and 128, one MI355X); what it picks took 1.5% longer than the best of them in the mean, 29% at most (one
 // piece of a prompt among 15 tokens).  us, best and worst kind: 64 rows 5.6 (16 columns, four wavefronts) to 12; 64 behind 16384 29 (32, eight) to 104; 512 behind 16384 123 (64, eight) to
 // 215; 2048 47 (64, four) to 89; 16384 1764 (64, one) to 3298.  Divided and whole: 128 rows behind 2048 16.7 and 12.8, five rows each of eight sequences behind 2048 16.0 and 13.5, a single
 // token behind 2048 9.2 and 10.9.
 struct KcKind {
-    int most, kw, slots;                                   // blocks of 16 * most columns; wavefronts; workgroups that the chip holds at once
+    int most, kw, slots;                                   // blocks of 16 * most columns; wavefronts; workgroups that the chip holds at once (at D = 128: D = 64 has registers
+                                                           // for up to 1.75 times as many of 16 columns and twice as many of 32, which the plan leaves unused)
     double alone, full, end;                               // us: a round of a workgroup that is alone, and with as many as there is room for; what a block costs besides
 };
 constexpr KcKind kKcKinds[] = {{1, 8, 512, 0.68, 1.33, 4.56}, {1, 4, 1024, 0.81, 1.31, 3.87}, {2, 8, 256, 0.71, 1.01, 5.21},
